@@ -421,6 +421,139 @@ omnimem_status_t omnimem_lru_stats(const omnimem_lru_t* lru, omnimem_lru_stats_t
 int32_t omnimem_lru_slot_of(const omnimem_lru_t* lru, int32_t head, int32_t chunk);
 
 /*
+ * Sequence cache: many sequences over one page pool, for generation token by token
+ * (or chunk by chunk) of a batch.  A page holds one block of B tokens of every
+ * key/value head, [num_pages][H][B][d] as in omnimem_kv_cache_t, and sequence i owns
+ * the row page_table[i][0 : M] and the length seq_lens[i].  Sequences may share pages
+ * (a common prompt, a fork).  Tokens come in chunks of S = chunk_tokens, chunk-aligned
+ * like the history's: token t lies in block (t div S)*Bpc + (t mod S) div B, slot
+ * (t mod S) mod B, Bpc = ceil(S/B).  With S a multiple of B that is block t div B,
+ * slot t mod B; with S the tokens of a video chunk, row i is the page_table of an
+ * omnimem_kv_cache_t whose num_chunks is seq_lens[i] div S.
+ *
+ * All calls below read the table and the lengths on the device: a length below 0
+ * counts as 0, one beyond the row's capacity as the capacity, M div Bpc chunks and
+ * the M mod Bpc blocks after them; a page id < 0 or >= num_pages is not resident.
+ */
+typedef struct {
+  int32_t num_seqs;     /* N >= 0 */
+  int32_t max_blocks;   /* M >= 1: entries of a row; the capacity in tokens < 2^31 - 1024 */
+  int32_t block_size;   /* B in {64, 128} */
+  int32_t chunk_tokens; /* S >= 1 */
+  int64_t num_pages;    /* pages of the pool, >= 0; < 2^31 */
+  const int32_t* page_table; /* [N][M] */
+  const int32_t* seq_lens;   /* [N] */
+} omnimem_seq_table_t;
+
+typedef struct {
+  omnimem_seq_table_t seqs;
+  int32_t dtype;        /* omnimem_dtype_t */
+  int32_t num_heads;    /* 1 <= H <= 2^20 key/value heads */
+  int32_t head_dim;     /* d in {64, 128} */
+  void* k_pages;        /* [num_pages][H][B][d], 16-byte aligned */
+  void* v_pages;
+} omnimem_seq_cache_t;
+
+/* Bytes of device workspace omnimem_decode_attn needs (0 on invalid arguments); the
+   table, the lengths and the pages may be NULL here. */
+size_t omnimem_decode_workspace_bytes(const omnimem_seq_cache_t* sc, int32_t num_q_heads);
+
+/*
+ * Attention of one new token per sequence: for every sequence i and query head h,
+ * with key/value head h div (num_q_heads/H),
+ *   O[i][h]   = sum_t softmax_t(scale * <q_i, k_t>) v_t
+ *   lse[h][i] = ln sum_t exp(scale * <q_i, k_t>)
+ * over the tokens t of sequence i in [max(0, len - window), len) (window = 0: all)
+ * whose page is resident.  No such token: O = 0 and lse = -inf.  Slots that hold none
+ * of these tokens do not matter, NaN included.
+ * q:   [N][num_q_heads][d] of sc->dtype, row i at q + i*q_stride elements (a multiple of
+ *      16 bytes, >= num_q_heads*d); num_q_heads is a multiple of H.
+ * out: [N][num_q_heads][d] of sc->dtype (out).  lse: [num_q_heads][N] float (out, may be NULL).
+ * workspace: device scratch of at least omnimem_decode_workspace_bytes(), 256-byte
+ * aligned; calls that can overlap need one each.  Nothing in it outlives the call.
+ * The work is split over the sequences' real lengths, so the order of the sums, and the
+ * last bits of O, depend on all lengths of the batch.  bf16: as omnimem_sparse_attn
+ * (P is rounded to bf16 before PV); f32: fp32 arithmetic throughout.
+ */
+omnimem_status_t omnimem_decode_attn(const omnimem_seq_cache_t* sc, const void* q, int64_t q_stride,
+                                     int32_t num_q_heads, int32_t window, float scale, void* out, float* lse,
+                                     void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Writes new tokens' keys and values into the pages of their sequences.  The rows
+ * starts[i] to starts[i+1] of k and v are the last starts[i+1] - starts[i] tokens of
+ * sequence i: seq_lens already counts them, and their blocks have pages of their own
+ * (omnimem_seq_update sees to both).  Rows in front of a sequence's first token,
+ * behind its capacity or in a block that is not resident are dropped, and nothing
+ * else of the pool is written.  Two tokens in one slot (a page listed twice): either.
+ * k, v:   `tokens` rows [H][d] of sc->dtype, row t at k + t*k_stride elements (v: v_stride;
+ *         multiples of 16 bytes, >= H*d; 16-byte aligned; no overlap with the pool).
+ * starts: [N + 1] int32, ascending, values outside [0, tokens] clamped; NULL: one token
+ *         for each sequence (tokens = N).
+ */
+omnimem_status_t omnimem_append_kv(const omnimem_seq_cache_t* sc, const void* k, int64_t k_stride, const void* v,
+                                   int64_t v_stride, int32_t tokens, const int32_t* starts, void* stream);
+
+/*
+ * Copies whole pages: for i < min(*count, max_pairs), page pairs[i][1] = page pairs[i][0],
+ * of the K and V pools of `layers` layers.  A pair with an id < 0 or >= num_pages is
+ * skipped.  No page may be the target of two pairs, or the target of one and the source
+ * of another (the copies run in any order); sources may repeat.
+ * k_pages, v_pages: layer l's pool at + l*layer_stride bytes, num_pages pages of page_bytes
+ *   (H*B*d elements; page_bytes and layer_stride multiples of 16, 16-byte aligned);
+ *   v_pages may be NULL (one pool).
+ * pairs: [max_pairs][2] int32; count: device int32 scalar, NULL = max_pairs.
+ */
+omnimem_status_t omnimem_copy_pages(void* k_pages, void* v_pages, int64_t num_pages, int64_t page_bytes,
+                                    int32_t layers, int64_t layer_stride, const int32_t* pairs, const int32_t* count,
+                                    int32_t max_pairs, void* stream);
+
+/* Bytes of device workspace omnimem_seq_update (for num_new rows) and omnimem_seq_compact
+   (num_new = 0) need (0 on invalid arguments); the table and the lengths may be NULL here. */
+size_t omnimem_seq_workspace_bytes(const omnimem_seq_table_t* st, int32_t num_new);
+
+/*
+ * The next step's sequences from this step's: new row i (i < num_new) is the first keep[i]
+ * tokens of row parent[i] and room for grow[i] tokens more.  Row i of parent itself goes
+ * on, another row forks it, a row that no parent names is freed, a smaller keep drops its
+ * newest tokens, and parent[i] outside [0, N) starts an empty sequence.  keep is clamped
+ * to [0, the parent's length] and grow to >= 0; keep = NULL keeps all, grow = NULL adds none.
+ *   out_table[i] [M], out_lens[i]: the new rows; entries behind a row's last block are -1,
+ *     and so are kept blocks that are not resident.
+ *   Pages: a page that no kept block names is free.  Kept blocks keep their pages, shared
+ *     or not, but for the block that a growing row has begun to fill (its token count is
+ *     no whole number of blocks): of all rows that hold its page, the lowest growing one
+ *     keeps it if all others grow in it too, and each other growing row gets a copy.
+ *     Copies and blocks added take the lowest free pages in ascending order, rows in
+ *     ascending order, a row's copy before its added blocks.
+ *   copies [num_new][2]: (from, to) of the copies, in row order, then -1: for
+ *     omnimem_copy_pages, once for every layer, before any omnimem_append_kv.
+ *   info [4]: copies, pages in use, pages short, rows over capacity.  Where pages are
+ *     short or a row would pass the capacity (such a row asks for no page), no row grows
+ *     and nothing is copied: the new rows are the kept tokens alone.
+ * The outputs overlap neither each other nor the inputs.  out_lens [num_new], all int32.
+ * workspace: omnimem_seq_workspace_bytes(st, num_new), 256-byte aligned.
+ */
+omnimem_status_t omnimem_seq_update(const omnimem_seq_table_t* st, int32_t num_new, const int32_t* parent,
+                                    const int32_t* keep, const int32_t* grow, int32_t* out_table, int32_t* out_lens,
+                                    int32_t* copies, int32_t* info, void* workspace, size_t workspace_bytes,
+                                    void* stream);
+
+/*
+ * Moves the pages in use to the front of the pool, [0, U): with U pages in use, the j-th
+ * used page >= U goes to the j-th free page < U, both in ascending order.
+ *   out_table [N][M]: the rows with the moved ids, -1 behind a row's last block and for
+ *     blocks that are not resident.
+ *   moves [max(1, num_pages div 2)][2]: (from, to), then -1: for omnimem_copy_pages, once for
+ *     every layer.
+ *   info [4]: moves, pages in use, 0, 0.
+ * The outputs overlap neither each other nor the inputs.
+ * workspace: omnimem_seq_workspace_bytes(st, 0), 256-byte aligned.
+ */
+omnimem_status_t omnimem_seq_compact(const omnimem_seq_table_t* st, int32_t* out_table, int32_t* moves, int32_t* info,
+                                     void* workspace, size_t workspace_bytes, void* stream);
+
+/*
  * Binds the calling thread to the NUMA node of GPU `device`'s PCI function (App. B
  * binds generation to the node that owns the GPU's PCIe root): its CPU affinity
  * becomes that node's CPUs among those it may already use, and its memory policy

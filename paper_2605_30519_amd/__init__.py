@@ -14,18 +14,27 @@ from .omnimem import (  # noqa: F401
     SCORE_PROB,
     PagedKVCache,
     Selection,
+    SeqKVCache,
+    SeqUpdate,
     lib,
     library_path,
+    omnimem_append_kv,
     omnimem_awe_active,
     omnimem_blocks_per_chunk,
     omnimem_cmp_attn,
     omnimem_compress_chunk,
+    omnimem_copy_pages,
+    omnimem_decode_attn,
+    omnimem_decode_workspace_bytes,
     omnimem_dense_attn,
     omnimem_gated_combine,
     omnimem_select,
     omnimem_select_compressed,
     omnimem_select_noalloc,
     omnimem_select_workspace_bytes,
+    omnimem_seq_compact,
+    omnimem_seq_update,
+    omnimem_seq_workspace_bytes,
     omnimem_sparse_attn,
     omnimem_status_string,
     omnimem_union_gather_attn,

@@ -9,11 +9,13 @@ CSRC = os.path.join(PKG, "csrc")
 OBJ_DIR = os.path.join(PKG, "_build")
 LIB = os.path.join(PKG, "libomnimem.so")
 PROBE_LIB = os.path.join(PKG, "libomnimem_probe.so")
-SOURCES = ["api.hip", "select.hip", "prob.hip", "attention.hip", "union_gather.hip", "fuse.hip", "offload.hip"]
+SOURCES = ["api.hip", "select.hip", "prob.hip", "attention.hip", "union_gather.hip", "fuse.hip", "offload.hip",
+           "decode.hip", "pages.hip"]
 # host-only C++ (no HIP): argument checks, work plans, the LRU bookkeeping and the
 # NUMA binding, built by the host compiler; tests also build them under sanitizers
-HOST_SOURCES = ["validate.cpp", "plan.cpp", "lru_core.cpp", "numa.cpp"]
-HEADERS = ["device_common.h", "launch.h", "plan.h", "validate.h", "lru_core.h", "numa.h"]
+HOST_SOURCES = ["validate.cpp", "plan.cpp", "seq.cpp", "lru_core.cpp", "numa.cpp"]
+HEADERS = ["device_common.h", "launch.h", "plan.h", "validate.h", "seq.h", "seq_launch.h", "lru_core.h",
+           "numa.h"]
 CXX = os.environ.get("CXX", "g++")
 HOST_FLAGS = ["-O2", "-std=c++17", "-fPIC", "-fvisibility=hidden", "-Wall"]
 

@@ -7,6 +7,7 @@
 
 #include "../../include/omnimem.h"
 #include "launch.h"
+#include "seq_launch.h"
 #include "validate.h"
 
 #define OMNIMEM_API extern "C" __attribute__((visibility("default")))
@@ -179,6 +180,70 @@ OMNIMEM_API omnimem_status_t omnimem_union_gather_attn(const omnimem_kv_cache_t*
                                                           union_blocks, workspace, workspace_bytes, g, up, a);
   if (st != OMNIMEM_OK || lq == 0) return st;
   return hip_status(omnimem::launch_union_gather(g, up, a, union_blocks, workspace, as_stream(stream)));
+}
+
+OMNIMEM_API size_t omnimem_decode_workspace_bytes(const omnimem_seq_cache_t* sc, int32_t num_q_heads) {
+  return omnimem::decode_workspace_bytes(sc, num_q_heads);
+}
+
+OMNIMEM_API omnimem_status_t omnimem_decode_attn(const omnimem_seq_cache_t* sc, const void* q, int64_t q_stride,
+                                                 int32_t num_q_heads, int32_t window, float scale, void* out,
+                                                 float* lse, void* workspace, size_t workspace_bytes, void* stream) {
+  omnimem::SeqGeom g;
+  omnimem::DecodePlan p;
+  omnimem::DecodeLaunch a;
+  const omnimem_status_t st = omnimem::check_decode_attn(sc, q, q_stride, num_q_heads, window, scale, out, lse,
+                                                         workspace, workspace_bytes, g, p, a);
+  if (st != OMNIMEM_OK || g.N == 0) return st;
+  return hip_status(omnimem::launch_decode(g, p, a, workspace, as_stream(stream)));
+}
+
+OMNIMEM_API omnimem_status_t omnimem_append_kv(const omnimem_seq_cache_t* sc, const void* k, int64_t k_stride,
+                                               const void* v, int64_t v_stride, int32_t tokens, const int32_t* starts,
+                                               void* stream) {
+  omnimem::SeqGeom g;
+  omnimem::AppendLaunch a;
+  const omnimem_status_t st = omnimem::check_append_kv(sc, k, k_stride, v, v_stride, tokens, starts, g, a);
+  if (st != OMNIMEM_OK || tokens == 0 || g.N == 0) return st;
+  return hip_status(omnimem::launch_append_kv(g, a, as_stream(stream)));
+}
+
+OMNIMEM_API omnimem_status_t omnimem_copy_pages(void* k_pages, void* v_pages, int64_t num_pages, int64_t page_bytes,
+                                                int32_t layers, int64_t layer_stride, const int32_t* pairs,
+                                                const int32_t* count, int32_t max_pairs, void* stream) {
+  omnimem::CopyLaunch a;
+  const omnimem_status_t st = omnimem::check_copy_pages(k_pages, v_pages, num_pages, page_bytes, layers, layer_stride,
+                                                        pairs, count, max_pairs, a);
+  if (st != OMNIMEM_OK || num_pages == 0 || layers == 0 || max_pairs == 0) return st;
+  return hip_status(omnimem::launch_copy_pages(a, as_stream(stream)));
+}
+
+OMNIMEM_API size_t omnimem_seq_workspace_bytes(const omnimem_seq_table_t* st, int32_t num_new) {
+  return omnimem::seq_workspace_bytes(st, num_new);
+}
+
+OMNIMEM_API omnimem_status_t omnimem_seq_update(const omnimem_seq_table_t* st, int32_t num_new, const int32_t* parent,
+                                                const int32_t* keep, const int32_t* grow, int32_t* out_table,
+                                                int32_t* out_lens, int32_t* copies, int32_t* info, void* workspace,
+                                                size_t workspace_bytes, void* stream) {
+  omnimem::SeqGeom g;
+  omnimem::SeqPlan p;
+  omnimem::SeqUpdateLaunch a;
+  const omnimem_status_t s = omnimem::check_seq_update(st, num_new, parent, keep, grow, out_table, out_lens, copies,
+                                                       info, workspace, workspace_bytes, g, p, a);
+  if (s != OMNIMEM_OK) return s;
+  return hip_status(omnimem::launch_seq_update(g, p, a, workspace, as_stream(stream)));
+}
+
+OMNIMEM_API omnimem_status_t omnimem_seq_compact(const omnimem_seq_table_t* st, int32_t* out_table, int32_t* moves,
+                                                 int32_t* info, void* workspace, size_t workspace_bytes,
+                                                 void* stream) {
+  omnimem::SeqGeom g;
+  omnimem::SeqPlan p;
+  omnimem::SeqUpdateLaunch a;
+  const omnimem_status_t s = omnimem::check_seq_compact(st, out_table, moves, info, workspace, workspace_bytes, g, p, a);
+  if (s != OMNIMEM_OK) return s;
+  return hip_status(omnimem::launch_seq_compact(g, p, a, workspace, as_stream(stream)));
 }
 
 OMNIMEM_API const char* omnimem_status_string(int32_t status) { return omnimem::status_string(status); }

@@ -5,15 +5,18 @@ include/omnimem.h.  PyTorch supplies device memory and the current stream.
 The functions carry the C names: omnimem_select, omnimem_sparse_attn,
 omnimem_dense_attn, omnimem_union_gather_attn, the compressed-history calls
 omnimem_compress_chunk, omnimem_select_compressed and omnimem_cmp_attn, Eq. 1's
-gated fusion omnimem_gated_combine, plus the host-side helpers.
+gated fusion omnimem_gated_combine, the sequence cache's omnimem_decode_attn,
+omnimem_append_kv, omnimem_copy_pages, omnimem_seq_update and omnimem_seq_compact, plus
+the host-side helpers.
 """
 from __future__ import annotations
 
 import ctypes
+import functools
 import math
 import os
 import threading
-from dataclasses import dataclass
+from dataclasses import dataclass, replace
 from typing import Optional
 
 import torch
@@ -90,6 +93,29 @@ class omnimem_cmp_cache_t(ctypes.Structure):
     ]
 
 
+class omnimem_seq_table_t(ctypes.Structure):
+    _fields_ = [
+        ("num_seqs", ctypes.c_int32),
+        ("max_blocks", ctypes.c_int32),
+        ("block_size", ctypes.c_int32),
+        ("chunk_tokens", ctypes.c_int32),
+        ("num_pages", ctypes.c_int64),
+        ("page_table", ctypes.c_void_p),
+        ("seq_lens", ctypes.c_void_p),
+    ]
+
+
+class omnimem_seq_cache_t(ctypes.Structure):
+    _fields_ = [
+        ("seqs", omnimem_seq_table_t),
+        ("dtype", ctypes.c_int32),
+        ("num_heads", ctypes.c_int32),
+        ("head_dim", ctypes.c_int32),
+        ("k_pages", ctypes.c_void_p),
+        ("v_pages", ctypes.c_void_p),
+    ]
+
+
 EXPORTED = [
     "omnimem_blocks_per_chunk",
     "omnimem_awe_active",
@@ -113,6 +139,13 @@ EXPORTED = [
     "omnimem_lru_stats",
     "omnimem_lru_slot_of",
     "omnimem_numa_bind",
+    "omnimem_decode_workspace_bytes",
+    "omnimem_decode_attn",
+    "omnimem_append_kv",
+    "omnimem_copy_pages",
+    "omnimem_seq_workspace_bytes",
+    "omnimem_seq_update",
+    "omnimem_seq_compact",
 ]
 
 
@@ -185,6 +218,22 @@ def _configure(L, required: bool = True):
     L.omnimem_selected_chunks.restype = i32
     L.omnimem_numa_bind.argtypes = [i32, ctypes.POINTER(i32)]
     L.omnimem_numa_bind.restype = i32
+    scp = ctypes.POINTER(omnimem_seq_cache_t)
+    stp = ctypes.POINTER(omnimem_seq_table_t)
+    L.omnimem_decode_workspace_bytes.argtypes = [scp, i32]
+    L.omnimem_decode_workspace_bytes.restype = sz
+    L.omnimem_decode_attn.argtypes = [scp, vp, i64, i32, i32, f32, vp, vp, vp, sz, vp]
+    L.omnimem_decode_attn.restype = i32
+    L.omnimem_append_kv.argtypes = [scp, vp, i64, vp, i64, i32, vp, vp]
+    L.omnimem_append_kv.restype = i32
+    L.omnimem_copy_pages.argtypes = [vp, vp, i64, i64, i32, i64, vp, vp, i32, vp]
+    L.omnimem_copy_pages.restype = i32
+    L.omnimem_seq_workspace_bytes.argtypes = [stp, i32]
+    L.omnimem_seq_workspace_bytes.restype = sz
+    L.omnimem_seq_update.argtypes = [stp, i32, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+    L.omnimem_seq_update.restype = i32
+    L.omnimem_seq_compact.argtypes = [stp, vp, vp, vp, vp, sz, vp]
+    L.omnimem_seq_compact.restype = i32
     return L
 
 
@@ -724,6 +773,272 @@ def omnimem_gated_combine(o_cmp: Optional[torch.Tensor], o_slc: Optional[torch.T
                                      _ptr(gate_logits), _ptr(out), _stream(stream))
     _check(st, "omnimem_gated_combine")
     return out
+
+
+# ----------------------------------------------------------- sequence cache
+
+def _on_stream(fn):
+    """Runs fn with the GPU of its first argument as the current device and `stream` (a
+    torch stream or a raw handle; None: that GPU's current stream) as its current stream, so
+    that buffers made inside belong to the stream the kernels run on."""
+    @functools.wraps(fn)
+    def call(first, *args, stream=None, **kw):
+        t = first.k_pages if isinstance(first, SeqKVCache) else first
+        if not (isinstance(t, torch.Tensor) and t.is_cuda):
+            return fn(first, *args, **kw)     # refused there
+        if stream is None:
+            if t.get_device() == torch.cuda.current_device():
+                return fn(first, *args, **kw)
+            with torch.cuda.device(t.device):
+                return fn(first, *args, **kw)
+        if not isinstance(stream, torch.cuda.Stream):
+            handle = int(stream)
+            stream = torch.cuda.ExternalStream(handle, device=t.device) if handle else torch.cuda.default_stream(t.device)
+        _need(stream.device == t.device, f"stream must belong to {t.device}, not {stream.device}")
+        with torch.cuda.stream(stream):
+            return fn(first, *args, **kw)
+    return call
+
+
+def _seq_table(page_table, seq_lens, num_pages: int, block_size: int, chunk_tokens: int) -> omnimem_seq_table_t:
+    _need(isinstance(page_table, torch.Tensor) and page_table.dim() == 2, "page_table must be an [N, max_blocks] tensor")
+    n, m = page_table.shape
+    _check_tensor("page_table", page_table, (n, m), torch.int32)
+    _check_tensor("seq_lens", seq_lens, (n,), torch.int32)
+    return omnimem_seq_table_t(n, m, block_size, chunk_tokens or block_size, num_pages, page_table.data_ptr(),
+                               seq_lens.data_ptr())
+
+
+@dataclass
+class SeqKVCache:
+    """One layer's keys and values of many sequences over one page pool (device tensors owned
+    by the caller).
+
+    k_pages, v_pages: [num_pages, H, B, d] (bf16 or fp32); page_table: [N, max_blocks] int32,
+    row i the pages of sequence i's blocks (negative = not resident); seq_lens: [N] int32
+    tokens.  chunk_tokens: tokens come in chunks that begin in a block of their own (0: in
+    one run)."""
+    k_pages: torch.Tensor
+    v_pages: torch.Tensor
+    page_table: torch.Tensor
+    seq_lens: torch.Tensor
+    chunk_tokens: int = 0
+
+    def descriptor(self) -> omnimem_seq_cache_t:
+        kp, vp = self.k_pages, self.v_pages
+        shape, code = kp.shape, _DTYPES.get(kp.dtype)
+        if code is None or vp.dtype is not kp.dtype:
+            raise TypeError(f"unsupported page dtype {kp.dtype}")
+        if len(shape) != 4 or vp.shape != shape:
+            raise ValueError("k_pages and v_pages must share one [num_pages, H, B, d] shape")
+        if not (kp.is_contiguous() and vp.is_contiguous()):
+            raise ValueError("cache tensors must be contiguous")
+        num_pages, H, B, d = shape
+        seqs = _seq_table(self.page_table, self.seq_lens, num_pages, B, self.chunk_tokens)
+        _on_gpu(kp, v_pages=vp, page_table=self.page_table, seq_lens=self.seq_lens)
+        return omnimem_seq_cache_t(seqs, code, H, d, kp.data_ptr(), vp.data_ptr())
+
+    def after(self, update: "SeqUpdate") -> "SeqKVCache":
+        """The same pool under the tables of an update."""
+        return replace(self, page_table=update.page_table, seq_lens=update.seq_lens)
+
+    def chunks(self, seq: int, num_chunks: int) -> PagedKVCache:
+        """The first num_chunks whole chunks of a sequence as the history of a chunk step."""
+        S = self.chunk_tokens or int(self.k_pages.shape[2])
+        bpc = -(-S // int(self.k_pages.shape[2]))
+        _need(0 <= num_chunks * bpc <= self.page_table.shape[1], "num_chunks exceeds the sequence's row")
+        return PagedKVCache(self.k_pages, self.v_pages, self.page_table[seq, :num_chunks * bpc].view(num_chunks, bpc), S)
+
+
+@dataclass
+class SeqUpdate:
+    page_table: torch.Tensor  # [num_new, max_blocks] int32
+    seq_lens: torch.Tensor    # [num_new] int32
+    copies: torch.Tensor      # [.., 2] int32 (from, to), -1 behind the last one
+    info: torch.Tensor        # [4] int32: copies, pages in use, pages short, rows over capacity
+
+
+def _row_stride(name: str, t: torch.Tensor, rows: int, heads: int, d: int) -> int:
+    """Elements from row to row of a [rows, heads, d] tensor whose rows are contiguous."""
+    if t.is_contiguous():
+        return heads * d
+    s = t.stride()
+    _need((s[2] == 1 or d == 1) and (s[1] == d or heads == 1), f"{name} must have contiguous [H, d] rows")
+    return s[0] if rows > 1 else heads * d
+
+
+def _rows_of(name: str, t, heads: Optional[int], d: int, dtype) -> int:
+    _need(isinstance(t, torch.Tensor) and t.dim() == 3, f"{name} must be a [rows, H, d] tensor")
+    n, h, e = t.shape
+    _need((heads is None or h == heads) and e == d, f"{name} must have shape {(n, heads or h, d)}, not {tuple(t.shape)}")
+    _need(t.dtype is dtype, f"{name} must be {dtype}, not {t.dtype}")
+    return n
+
+
+def omnimem_decode_workspace_bytes(cache: SeqKVCache, num_q_heads: int) -> int:
+    return int(lib().omnimem_decode_workspace_bytes(ctypes.byref(cache.descriptor()), int(num_q_heads)))
+
+
+@_on_stream
+def omnimem_decode_attn(cache: SeqKVCache, q: torch.Tensor, scale: Optional[float] = None, *, window: int = 0,
+                        out: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None, want_lse: bool = True,
+                        workspace: Optional[torch.Tensor] = None):
+    """Attention of one new token per sequence: q [N, Hq, d] (rows may be strided, as a slice of a
+    fused projection is), Hq a multiple of the cache's heads.  window > 0: the last so many
+    tokens only.  Returns out [N, Hq, d] and lse [Hq, N].  Takes stream=."""
+    kp = cache.k_pages
+    H, d = kp.shape[1], kp.shape[3]
+    n = _rows_of("q", q, None, d, kp.dtype)
+    hq = q.shape[1]
+    _need(hq >= 1 and hq % H == 0, f"q must have a multiple of {H} heads, not {hq}")
+    _need(n == cache.page_table.shape[0], f"q must have {cache.page_table.shape[0]} rows, not {n}")
+    stride = _row_stride("q", q, n, hq, d)
+    _check_outputs(q, out, lse)
+    desc = cache.descriptor()
+    _on_gpu(kp, q=q, out=out, lse=lse)
+    L = lib()
+    need = L.omnimem_decode_workspace_bytes(ctypes.byref(desc), hq)
+    if workspace is None:
+        workspace = workspace_tensor(need, q.device)
+    else:
+        _check_workspace(workspace, need, q)
+    if out is None:
+        out = torch.empty((n, hq, d), dtype=q.dtype, device=q.device)
+    if lse is None and want_lse:
+        lse = torch.empty((hq, n), dtype=torch.float32, device=q.device)
+    sc = 1.0 / math.sqrt(d) if scale is None else float(scale)
+    st = L.omnimem_decode_attn(ctypes.byref(desc), q.data_ptr(), stride, hq, int(window), sc, out.data_ptr(), _ptr(lse),
+                               workspace.data_ptr(), workspace.numel(), _current_raw_stream())
+    _check(st, "omnimem_decode_attn")
+    return out, lse
+
+
+@_on_stream
+def omnimem_append_kv(cache: SeqKVCache, k: torch.Tensor, v: torch.Tensor, starts: Optional[torch.Tensor] = None) -> None:
+    """Writes new tokens into their sequences' pages: rows starts[i] to starts[i + 1] of k and v
+    [T, H, d] (rows may be strided) are the last tokens of sequence i, which cache.seq_lens
+    already counts; starts [N + 1] int32, None: one token per sequence.  Takes stream=."""
+    kp = cache.k_pages
+    _, H, _, d = kp.shape
+    n = _rows_of("k", k, H, d, kp.dtype)
+    _need(_rows_of("v", v, H, d, kp.dtype) == n, "k and v must have as many rows")
+    ks, vs = _row_stride("k", k, n, H, d), _row_stride("v", v, n, H, d)
+    seqs = cache.page_table.shape[0]
+    if starts is None:
+        _need(n == seqs, f"k and v must have {seqs} rows (one per sequence) without starts")
+    else:
+        _check_tensor("starts", starts, (seqs + 1,), torch.int32)
+    desc = cache.descriptor()
+    _on_gpu(kp, k=k, v=v, starts=starts)
+    _check(lib().omnimem_append_kv(ctypes.byref(desc), k.data_ptr(), ks, v.data_ptr(), vs, n, _ptr(starts),
+                                   _current_raw_stream()), "omnimem_append_kv")
+
+
+@_on_stream
+def omnimem_copy_pages(k_pages: torch.Tensor, v_pages: Optional[torch.Tensor], pairs: torch.Tensor,
+                       count: Optional[torch.Tensor] = None) -> None:
+    """Copies page pairs[i][0] to page pairs[i][1] for the first count[0] pairs [n, 2] int32 (None:
+    all), in pools [num_pages, H, B, d] or, for several layers in one call, [layers, num_pages,
+    H, B, d].  count: int32 tensor (SeqUpdate.info serves).  Takes stream=."""
+    dims = k_pages.dim()
+    _need(dims in (4, 5), "k_pages must be [num_pages, H, B, d] or [layers, num_pages, H, B, d]")
+    layers = k_pages.shape[0] if dims == 5 else 1
+    pages = k_pages.shape[-4]
+    step = k_pages.stride(0) if dims == 5 and layers > 1 else 0
+    for name, t in (("k_pages", k_pages), ("v_pages", v_pages)):
+        if t is None:
+            continue
+        _need(t.shape == k_pages.shape and t.dtype is k_pages.dtype, f"{name} must match k_pages in shape and dtype")
+        _need((t[0] if dims == 5 and layers > 0 else t).is_contiguous() and (step == 0 or t.stride(0) == step),
+              f"{name} must be contiguous")
+    _need(isinstance(pairs, torch.Tensor) and pairs.dim() == 2, "pairs must be an [n, 2] tensor")
+    _check_tensor("pairs", pairs, (pairs.shape[0], 2), torch.int32)
+    if count is not None:
+        _need(isinstance(count, torch.Tensor) and count.dtype is torch.int32 and count.numel() >= 1 and
+              count.is_contiguous(), "count must be an int32 tensor")
+    eb = k_pages.element_size()
+    page_bytes = k_pages.shape[-3] * k_pages.shape[-2] * k_pages.shape[-1] * eb
+    _on_gpu(k_pages, "k_pages", v_pages=v_pages, pairs=pairs, count=count)
+    _check(lib().omnimem_copy_pages(k_pages.data_ptr(), _ptr(v_pages), pages, page_bytes, layers, step * eb,
+                                    pairs.data_ptr(), _ptr(count), pairs.shape[0], _current_raw_stream()),
+           "omnimem_copy_pages")
+
+
+def omnimem_seq_workspace_bytes(page_table: torch.Tensor, seq_lens: torch.Tensor, num_pages: int, block_size: int,
+                                num_new: int = 0, *, chunk_tokens: int = 0) -> int:
+    desc = _seq_table(page_table, seq_lens, num_pages, block_size, chunk_tokens)
+    return int(lib().omnimem_seq_workspace_bytes(ctypes.byref(desc), int(num_new)))
+
+
+def _seq_out(out: Optional[SeqUpdate], n: int, m: int, pairs: int, lens, dev) -> SeqUpdate:
+    if out is None:
+        return SeqUpdate(torch.empty((n, m), dtype=torch.int32, device=dev),
+                         torch.empty(n, dtype=torch.int32, device=dev) if lens is None else lens,
+                         torch.empty((pairs, 2), dtype=torch.int32, device=dev),
+                         torch.empty(4, dtype=torch.int32, device=dev))
+    _check_tensor("out.page_table", out.page_table, (n, m), torch.int32)
+    _check_tensor("out.seq_lens", out.seq_lens, (n,), torch.int32)
+    _check_tensor("out.copies", out.copies, (pairs, 2), torch.int32)
+    _check_tensor("out.info", out.info, (4,), torch.int32)
+    return out
+
+
+@_on_stream
+def omnimem_seq_update(page_table: torch.Tensor, seq_lens: torch.Tensor, num_pages: int, block_size: int,
+                       parent: torch.Tensor, keep: Optional[torch.Tensor] = None, grow: Optional[torch.Tensor] = None, *,
+                       chunk_tokens: int = 0, out: Optional[SeqUpdate] = None,
+                       workspace: Optional[torch.Tensor] = None) -> SeqUpdate:
+    """The next step's sequences: new row i is the first keep[i] tokens (None: all) of row
+    parent[i] (-1: an empty sequence) and room for grow[i] more (None: none); rows that no parent
+    names are freed.  The copies that rows with a shared page need before they are
+    appended to are result.copies, for omnimem_copy_pages(..., result.copies, result.info) on
+    every layer.  Where info[2] (pages short) or info[3] (rows over capacity) is not 0, no row
+    grew.  Takes stream=."""
+    desc = _seq_table(page_table, seq_lens, int(num_pages), int(block_size), int(chunk_tokens))
+    _need(isinstance(parent, torch.Tensor) and parent.dim() == 1, "parent must be a 1-D tensor")
+    n = parent.shape[0]
+    for name, t in (("parent", parent), ("keep", keep), ("grow", grow)):
+        if t is not None:
+            _check_tensor(name, t, (n,), torch.int32)
+    dev = page_table.device
+    made = _seq_out(out, n, page_table.shape[1], n, None, dev)
+    _on_gpu(page_table, "page_table", seq_lens=seq_lens, parent=parent, keep=keep, grow=grow, out_table=made.page_table,
+            out_lens=made.seq_lens, copies=made.copies, info=made.info)
+    L = lib()
+    need = L.omnimem_seq_workspace_bytes(ctypes.byref(desc), n)
+    if workspace is None:
+        workspace = workspace_tensor(need, dev)
+    else:
+        _check_workspace(workspace, need, page_table)
+    st = L.omnimem_seq_update(ctypes.byref(desc), n, _ptr(parent), _ptr(keep), _ptr(grow), _ptr(made.page_table),
+                              _ptr(made.seq_lens), _ptr(made.copies), _ptr(made.info), workspace.data_ptr(),
+                              workspace.numel(), _current_raw_stream())
+    _check(st, "omnimem_seq_update")
+    return made
+
+
+@_on_stream
+def omnimem_seq_compact(page_table: torch.Tensor, seq_lens: torch.Tensor, num_pages: int, block_size: int, *,
+                        chunk_tokens: int = 0, out: Optional[SeqUpdate] = None,
+                        workspace: Optional[torch.Tensor] = None) -> SeqUpdate:
+    """The tables with all pages in use moved to the front of the pool; the moves to make are
+    result.copies, for omnimem_copy_pages(..., result.copies, result.info) on every layer, and
+    result.info[1] pages are in use.  The lengths stay (result.seq_lens is seq_lens).  Takes stream=."""
+    desc = _seq_table(page_table, seq_lens, int(num_pages), int(block_size), int(chunk_tokens))
+    dev = page_table.device
+    n, m = page_table.shape
+    made = _seq_out(out, n, m, max(1, int(num_pages) // 2), seq_lens, dev)
+    _on_gpu(page_table, "page_table", seq_lens=seq_lens, out_table=made.page_table, moves=made.copies, info=made.info)
+    L = lib()
+    need = L.omnimem_seq_workspace_bytes(ctypes.byref(desc), 0)
+    if workspace is None:
+        workspace = workspace_tensor(need, dev)
+    else:
+        _check_workspace(workspace, need, page_table)
+    st = L.omnimem_seq_compact(ctypes.byref(desc), _ptr(made.page_table), _ptr(made.copies), _ptr(made.info),
+                               workspace.data_ptr(), workspace.numel(), _current_raw_stream())
+    _check(st, "omnimem_seq_compact")
+    return made
 
 
 # ------------------------------------------------------------ LRU hot cache
