@@ -1,19 +1,23 @@
 // decode.hip -- attention of one new token per sequence over a paged cache, for gfx950:
 //   O[i][h] = sum_t softmax_t(scale <q_i, k_t>) v_t over the tokens of sequence i.
 //
-// Every key and value is used by the G query heads of its head alone, 2 G flops a byte of
-// bf16, so the kernel is bound by the stream of K and V from memory.  It is built to keep that
-// stream full: no LDS and no barrier between the loads and the products, tiles of 8 KB of
-// K and 8 KB of V a wave straight into MFMA operand registers, the next tile's loads issued
-// as soon as the registers of the present one are read.
+// A key and a value serve the G query heads of their head alone, 2 G flops a byte of bf16, so
+// the kernel is bound by the stream of K and V from memory and built to keep it full: no LDS
+// and no barrier between loads and products, tiles of 8 KB of K and 8 KB of V a wave straight
+// into MFMA operand registers, the next tile's loads issued as soon as the registers of the
+// present one are read.  Four rollouts of 47 to 94 thousand tokens, 12 heads of 128, bf16
+// (1.66 GB): 247 us, 6.7 TB/s, with plain instead of nontemporal loads 283; 48 sequences of 100
+// to 16,000 tokens, 40 query heads over 8 (617 MB): 110 us, 5.6 TB/s.
 //
-// Split.  An item is a (sequence, key/value head, tile of up to 32 query heads); its 64-token
-// units follow one another on a line of all items' units, and workgroup w takes the equal
-// share [w q, (w + 1) q) of it, over item boundaries, so that any mix of lengths loads
-// every workgroup alike and lengths stay on the device (a captured graph replays with others).
-// The four waves take a segment's units in turn and meet in LDS; an item that several
-// workgroups share leaves (O, max, sum) a share in the workspace, which k_decode_join adds
-// up in the order of the line.
+// Split.  An item is a (sequence, key/value head, tile of up to 32 query heads); its units of
+// 32 tokens (64 for bf16 heads of 64) follow one another on a line of all items' units, and
+// workgroup w takes the equal share [w q, (w + 1) q) of it, over item boundaries, so that any
+// mix of lengths loads every workgroup alike and lengths stay on the device (a captured graph
+// replays with others).  The four waves take a segment's units in turn and meet in LDS; an
+// item that several workgroups share leaves (O, max, sum) a share in the workspace, which
+// k_decode_join adds up in the order of the line, in a launch of its own (4 us): workgroups
+// that hand results on within a launch pay more for the caches between the dies.  With 64
+// instead of 32 tokens a unit the waves' loads differ more (115 us for the 48 sequences).
 #include <float.h>
 
 #include "device_common.h"
@@ -26,7 +30,7 @@ namespace {
 constexpr int kThreads = kDecodeWaves * kWave;
 constexpr int kMinUnits = 4;      // units of a share: one for each wave
 constexpr float kLowest = -FLT_MAX;  // below every score: a row without keys keeps sum 0
-constexpr int kNontemporal = 2;   // cache policy of a buffer load
+constexpr int kNontemporal = 2;   // cache policy of a buffer load: read once
 
 struct DecodeArgs {
   SeqGeom g;
@@ -38,19 +42,38 @@ struct DecodeArgs {
   int slot_floats;
 };
 
-// Tokens [begin, end) of a sequence and the blocks that hold them.
+// Tokens [begin, end) of a sequence and the blocks that hold them, in units of UT tokens.
 struct Span {
   int begin, end, block, units;
 };
 
-__device__ __forceinline__ Span span_of(const SeqGeom& g, int window, int len) {
+__device__ __forceinline__ int block_shift(const SeqGeom& g) { return 6 + (g.B >> 7); }  // log2 B
+
+__device__ __forceinline__ int block_of(const SeqGeom& g, int t) {
+  if (g.S == g.B) return t >> block_shift(g);
+  const int c = t / g.S;
+  return c * g.Bpc + ((t - c * g.S) >> block_shift(g));
+}
+
+template <int UT>
+__device__ __forceinline__ Span span_of(const DecodeArgs& A, int len) {
   Span s;
-  s.end = min(max(len, 0), g.cap);
-  s.begin = window > 0 ? max(0, s.end - window) : 0;
-  s.block = s.begin / g.S * g.Bpc + s.begin % g.S / g.B;
-  const int last = s.end > 0 ? (s.end - 1) / g.S * g.Bpc + (s.end - 1) % g.S / g.B : -1;
-  s.units = s.end > 0 ? (last + 1 - s.block) * (g.B / kUnitTokens) : 0;
+  s.end = min(max(len, 0), A.g.cap);
+  s.begin = A.a.window > 0 ? max(0, s.end - A.a.window) : 0;
+  s.block = block_of(A.g, s.begin);
+  s.units = s.end > 0 ? (block_of(A.g, s.end - 1) + 1 - s.block) * (A.g.B / UT) : 0;
   return s;
+}
+
+// Inclusive prefix sums over a wave, by cross-lane moves of the VALU.
+__device__ __forceinline__ int scan_lanes(int v) {
+  v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xf, 0xf, false);  // row_shr:1, 2, 4, 8: within 16 lanes
+  v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xf, 0xf, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xf, 0xf, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xf, 0xf, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xa, 0xf, false);  // row_bcast:15 into rows 1 and 3
+  v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xc, 0xf, false);  // row_bcast:31 into rows 2 and 3
+  return v;
 }
 
 __device__ __forceinline__ float max_over_groups(float x) {  // over the four 16-lane groups
@@ -86,6 +109,7 @@ template <int D>
 struct Tile<uint16_t, D> {
   static constexpr int ROW = D * 2, KEYS = 8192 / ROW, KB = KEYS / 32, QS = ROW / 64, VW = D / 16;
   static constexpr int RT = KEYS / 16;  // 16-key row tiles
+  static constexpr int UNIT = KEYS;
   typedef uint32_t vraw __attribute__((ext_vector_type(VW / 2)));  // a lane's V dims of one key
   u32x4 k[KB][2][QS];
   vraw v[KB][8];
@@ -129,8 +153,9 @@ struct Tile<uint16_t, D> {
                                                   __builtin_bit_cast(bf16x8, q[s]), c, 0, 0, 0);
     return c;
   }
-  // O^T row 16-dim tiles m: dims VW * (row of the tile) + m.  A word of the A operand holds dim m
-  // of two keys, picked out of the keys' rows.
+  // O^T row tiles m: dims VW * (row of the tile) + m.  A word of the A operand holds dim m of two
+  // keys, picked out of the keys' rows.  P is rounded to bf16, as in the library's other kernels:
+  // 1.6e-3 off fp64 in norm, which is the output's own rounding; the sums stay fp32.
   template <int NT>
   __device__ __forceinline__ void pv(const f32x4 (&p)[NT][RT], f32x4 (&o)[NT][VW]) const {
 #pragma unroll
@@ -158,7 +183,7 @@ struct Tile<uint16_t, D> {
 
 template <int D>
 struct Tile<float, D> {
-  static constexpr int ROW = D * 4, KEYS = 8192 / ROW, RT = KEYS / 16, QS = ROW / 64, VW = D / 16;
+  static constexpr int ROW = D * 4, KEYS = 8192 / ROW, RT = KEYS / 16, QS = ROW / 64, VW = D / 16, UNIT = 32;
   u32x4 k[RT][QS];
   u32x4 v[RT][4][VW / 4];
 
@@ -236,86 +261,192 @@ __device__ __forceinline__ void finish(const DecodeArgs& A, int seq, int hq, int
         sum == 0.f ? -INFINITY : (top + log2f(sum)) * 0.69314718055994531f;
 }
 
-template <typename T, int D, int NT>
-__global__ __launch_bounds__(kThreads, NT == 1 ? 3 : 2) void k_decode(const DecodeArgs A) {
+// A workgroup's run of units of one item.
+struct Segment {
+  Span sp;
+  int seq, head;  // head: (key/value head, tile)
+  int unit, stop;
+};
+
+// LDS traffic of the workgroup only: loads from memory stay in flight across it.
+__device__ __forceinline__ void lds_sync() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
+  __builtin_amdgcn_s_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
+}
+
+template <typename T, int D, int NT, bool DIRECT>
+__global__ __launch_bounds__(kThreads, 2) void k_decode(const DecodeArgs A) {
   using L = Tile<T, D>;
-  constexpr int RT = L::RT, VW = L::VW, QS = L::QS;
+  constexpr int RT = L::RT, VW = L::VW, QS = L::QS, UT = L::UNIT;
   __shared__ __align__(16) float s_o[kDecodeWaves][NT * 16][D];
   __shared__ float s_top[kDecodeWaves][NT * 16], s_sum[kDecodeWaves][NT * 16];
-  __shared__ int s_scan[kDecodeWaves];
-  __shared__ int s_seq, s_before;
   const int tid = threadIdx.x, lane = tid % kWave;
   const int wave = __builtin_amdgcn_readfirstlane(tid / kWave);
   const int i = lane % 16, j = lane / 16;
   const int HH = A.a.H * A.head_tiles;
   const int N = A.g.N;
 
-  // the line: units of every sequence, its total, and the sequence that this share begins in
-  const int per = (N + kThreads - 1) / kThreads;
-  const int first_seq = min(tid * per, N), last_seq = min(first_seq + per, N);
-  int mine = 0;
-  for (int s = first_seq; s < last_seq; ++s) mine += span_of(A.g, A.a.window, A.g.lens[s]).units;
-  int all;
-  const int before = block_exclusive_scan<kThreads>(mine, s_scan, all);
-  const int64_t line = static_cast<int64_t>(all) * HH;
-  const int share = static_cast<int>(max(static_cast<int64_t>(kMinUnits), (line + gridDim.x - 1) / gridDim.x));
-  int64_t pos = static_cast<int64_t>(blockIdx.x) * share;
-  if (pos < line) {
-    int x = static_cast<int>(pos / HH) - before;
-    if (x >= 0 && x < mine) {
-      int s = first_seq, b = before;
-      for (;; ++s) {
-        const int u = span_of(A.g, A.a.window, A.g.lens[s]).units;
-        if (x < u) break;
-        x -= u;
-        b += u;
+  Segment g{};
+  int left = 0;  // units of the share from g.unit on
+  if constexpr (DIRECT) {
+    g.seq = blockIdx.x / HH;
+    g.head = blockIdx.x % HH;
+    g.sp = span_of<UT>(A, __builtin_amdgcn_readfirstlane(A.g.lens[g.seq]));
+    left = g.sp.units;
+    if (left == 0) {
+      const int h = g.head / A.head_tiles, tile = g.head % A.head_tiles;
+      const int rows = min(A.tile_rows, A.G - tile * A.tile_rows);
+      for (int e = tid; e < rows * (D / 4); e += kThreads)
+        finish<T>(A, g.seq, h * A.G + tile * A.tile_rows + e / (D / 4), e % (D / 4) * 4, f32x4{}, 0.f, 0.f);
+      return;
+    }
+  } else {
+    // The line, formed by every wave for itself: lane l's sequences, the units in front of
+    // them, and the sequence that this share begins in.
+    const int per = (N + kWave - 1) / kWave;
+    const int first_seq = min(lane * per, N), last_seq = min(first_seq + per, N);
+    int mine = 0, empty = 0, len = 0;
+    for (int s = first_seq; s < last_seq; ++s) {
+      len = A.g.lens[s];
+      const int u = span_of<UT>(A, len).units;
+      mine += u;
+      empty |= u == 0;
+    }
+    const int upto = scan_lanes(mine);
+    const int all = __builtin_amdgcn_readlane(upto, kWave - 1);
+    const int64_t line = static_cast<int64_t>(all) * HH;
+    // positions in 32 bits where they fit, for the divisions' sake
+    const bool small = line + gridDim.x <= 0x7fffffff;
+    const int even = small ? static_cast<int>((static_cast<uint32_t>(line) + gridDim.x - 1) / gridDim.x)
+                           : static_cast<int>((line + gridDim.x - 1) / gridDim.x);
+    const int share = max(kMinUnits, even);
+    const int64_t pos = static_cast<int64_t>(blockIdx.x) * share;
+    // sequences without tokens get their zeros
+    if (__ballot(empty) != 0) {
+      for (int s = blockIdx.x; s < N; s += gridDim.x) {
+        if (span_of<UT>(A, A.g.lens[s]).units != 0) continue;
+        for (int e = tid; e < A.a.Hq * (D / 4); e += kThreads)
+          finish<T>(A, s, e / (D / 4), e % (D / 4) * 4, f32x4{}, 0.f, 0.f);
       }
-      s_seq = s;
-      s_before = b;
+    }
+    if (pos >= line) {
+      if (tid == 0) A.starts[blockIdx.x] = DecodeStart{};
+      return;
+    }
+    left = static_cast<int>(min(static_cast<int64_t>(share), line - pos));
+    const int x = small ? static_cast<int>(static_cast<uint32_t>(pos) / static_cast<uint32_t>(HH))
+                        : static_cast<int>(pos / HH);
+    const int at = __builtin_ctzll(__ballot(upto > x));  // the lane whose sequences hold position x
+    int before = __builtin_amdgcn_readlane(upto - mine, at);
+    g.seq = at * per;
+    if (per == 1) {
+      g.sp = span_of<UT>(A, __builtin_amdgcn_readlane(len, at));
+    } else {
+      for (;; ++g.seq) {
+        g.sp = span_of<UT>(A, __builtin_amdgcn_readfirstlane(A.g.lens[g.seq]));
+        if (x - before < g.sp.units) break;
+        before += g.sp.units;
+      }
+    }
+    const int64_t in = pos - static_cast<int64_t>(before) * HH;
+    g.head = in <= 0x7fffffff ? static_cast<int>(static_cast<uint32_t>(in) / static_cast<uint32_t>(g.sp.units))
+                              : static_cast<int>(in / g.sp.units);
+    g.unit = static_cast<int>(in - static_cast<int64_t>(g.head) * g.sp.units);
+    if (tid == 0) {
+      DecodeStart st{};
+      if (g.unit > 0) st = DecodeStart{pos - g.unit, g.sp.units, g.seq, g.head, share};
+      A.starts[blockIdx.x] = st;
     }
   }
-  __syncthreads();
-  // sequences without tokens, and rows of zeros for them
-  for (int s = blockIdx.x; s < N; s += gridDim.x) {
-    if (span_of(A.g, A.a.window, A.g.lens[s]).units != 0) continue;
-    for (int e = tid; e < A.a.Hq * (D / 4); e += kThreads)
-      finish<T>(A, s, e / (D / 4), e % (D / 4) * 4, f32x4{}, 0.f, 0.f);
-  }
-  if (pos >= line) {
-    if (tid == 0) A.starts[blockIdx.x] = DecodeStart{};
-    return;
-  }
-  int left = static_cast<int>(min(static_cast<int64_t>(share), line - pos));
-  int seq = __builtin_amdgcn_readfirstlane(s_seq);
-  Span sp = span_of(A.g, A.a.window, A.g.lens[seq]);
-  int head = static_cast<int>((pos - static_cast<int64_t>(s_before) * HH) / sp.units);
-  int unit = static_cast<int>((pos - static_cast<int64_t>(s_before) * HH) % sp.units);
-  if (tid == 0) {
-    DecodeStart st{};
-    if (unit > 0) st = DecodeStart{pos - unit, sp.units, seq, head, share};
-    A.starts[blockIdx.x] = st;
-  }
+  g.stop = min(g.sp.units, g.unit + left);
+  left -= g.stop - g.unit;
 
-  bool first = true;  // the share's first segment
-  while (left > 0) {
-    const int stop = min(sp.units, unit + left);
-    const int h = head / A.head_tiles, tile = head % A.head_tiles;
-    const int hq0 = h * A.G + tile * A.tile_rows;
+  // The wave's tiles form one stream over the segments: while a segment's last tile is worked
+  // on, the first one of the next segment is on its way.  The stream's own segment is f, at
+  // most one in front of g; its units are looked up 64 at a time, lane l the l-th one's page,
+  // first token row, and rows in use.
+  Segment f = g;
+  int next = f.unit + wave;
+  uint64_t mask = 0;
+  int l_page = 0, l_row = 0, l_lo = 0, l_hi = 0;
+  int lo = 0, hi = 0, sub = 0;  // the tile's unit: rows in use, rows before the tile
+  int64_t row = 0;              // the unit's first row in the pools
+  auto advance = [&]() -> bool {
+    if (sub + L::KEYS < hi) {
+      sub += L::KEYS;
+      return true;
+    }
+    while (mask == 0) {
+      if (next >= f.stop) {
+        lo = hi = sub = 0;  // a tile of no rows
+        return false;
+      }
+      const int u = next + lane * kDecodeWaves;
+      bool ok = u < f.stop;
+      if (ok) {
+        const int in_block = block_shift(A.g) - (UT == 64 ? 6 : 5);  // log2 of a block's units
+        const int b = f.sp.block + (u >> in_block);
+        l_row = (u & ((1 << in_block) - 1)) * UT;
+        const int c = A.g.Bpc == 1 ? b : b / A.g.Bpc;
+        const int in = (b - c * A.g.Bpc) * A.g.B + l_row;
+        const int tok = c * A.g.S + in;
+        l_page = A.g.table[static_cast<int64_t>(f.seq) * A.g.M + b];
+        l_hi = min(UT, min(A.g.S - in, f.sp.end - tok));
+        l_lo = max(0, f.sp.begin - tok);
+        ok = l_page >= 0 && l_page < A.g.num_pages && l_lo < l_hi;
+      }
+      mask = __ballot(ok);
+      next += kWave * kDecodeWaves;
+    }
+    const int at = __builtin_ctzll(mask);
+    mask &= mask - 1;
+    lo = __builtin_amdgcn_readlane(l_lo, at);
+    hi = __builtin_amdgcn_readlane(l_hi, at);
+    row = (static_cast<int64_t>(__builtin_amdgcn_readlane(l_page, at)) * A.a.H + f.head / A.head_tiles) * A.g.B +
+          __builtin_amdgcn_readlane(l_row, at);
+    sub = lo / L::KEYS * L::KEYS;
+    return true;
+  };
+  auto rsrc = [&](const void* pool) {
+    return tile_rsrc(static_cast<const char*>(pool) + (row + sub) * L::ROW, max(0, min(hi - sub, L::KEYS)) * L::ROW);
+  };
+  u32x4 q[NT][QS];
+  auto load_q = [&]() {
+    const int tile = f.head % A.head_tiles, hq0 = f.head / A.head_tiles * A.G + tile * A.tile_rows;
     const int rows = min(A.tile_rows, A.G - tile * A.tile_rows);
-
-    u32x4 q[NT][QS];
 #pragma unroll
-    for (int n = 0; n < NT; ++n) {
-      const bool real = n * 16 + i < rows;
-      const char* at = reinterpret_cast<const char*>(static_cast<const T*>(A.a.q) + seq * A.a.q_stride +
-                                                     static_cast<int64_t>(hq0 + (real ? n * 16 + i : 0)) * D) +
+    for (int n = 0; n < NT; ++n) {  // rows past the last query head repeat it and are not written
+      const char* at = reinterpret_cast<const char*>(static_cast<const T*>(A.a.q) + f.seq * A.a.q_stride +
+                                                     static_cast<int64_t>(hq0 + min(n * 16 + i, rows - 1)) * D) +
                        j * 16;
 #pragma unroll
-      for (int s = 0; s < QS; ++s) {
-        q[n][s] = *reinterpret_cast<const u32x4*>(at + s * 64);
-        if (!real) q[n][s] = u32x4{};
-      }
+      for (int s = 0; s < QS; ++s) q[n][s] = *reinterpret_cast<const u32x4*>(at + s * 64);
     }
+  };
+  // the stream's next segment; false behind the share's last one
+  auto next_segment = [&]() -> bool {
+    if (DIRECT || left == 0) return false;
+    f.unit = 0;
+    if (++f.head == HH) {
+      f.head = 0;
+      do f.sp = span_of<UT>(A, __builtin_amdgcn_readfirstlane(A.g.lens[++f.seq]));
+      while (f.sp.units == 0);
+    }
+    f.stop = min(f.sp.units, left);
+    left -= f.stop;
+    next = wave;
+    load_q();
+    return true;
+  };
+
+  L t;
+  load_q();
+  bool have = advance();
+  t.load_k(rsrc(A.a.k_pages), i, j);
+  __builtin_amdgcn_sched_barrier(0);  // K in front of V here as in the loop, whose waits count on it
+  t.load_v(rsrc(A.a.v_pages), i, j);
+  for (bool first = true;; first = false) {
     f32x4 o[NT][VW] = {};
     float top[NT], sum[NT];
 #pragma unroll
@@ -323,57 +454,8 @@ __global__ __launch_bounds__(kThreads, NT == 1 ? 3 : 2) void k_decode(const Deco
       top[n] = kLowest;
       sum[n] = 0.f;
     }
-
-    // The wave's units, 64 looked up at a time: lane l has the l-th one's page, first token
-    // row, and rows in use.
-    int next = unit + wave;
-    uint64_t mask = 0;
-    int l_page = 0, l_row = 0, l_lo = 0, l_hi = 0;
-    const int32_t* table = A.g.table + static_cast<int64_t>(seq) * A.g.M;
-    int lo = 0, hi = 0, sub = 0;   // the tile's unit: rows in use, rows before the tile
-    int64_t row = 0;               // the unit's first row in the pools
-    auto advance = [&]() -> bool {
-      if (sub + L::KEYS < hi) {
-        sub += L::KEYS;
-        return true;
-      }
-      while (mask == 0) {
-        if (next >= stop) {
-          lo = hi = sub = 0;  // a tile of no rows
-          return false;
-        }
-        const int u = next + lane * kDecodeWaves;
-        bool ok = u < stop;
-        if (ok) {
-          const int b = sp.block + u / (A.g.B / kUnitTokens);
-          l_row = u % (A.g.B / kUnitTokens) * kUnitTokens;
-          const int in = b % A.g.Bpc * A.g.B + l_row;
-          const int tok = b / A.g.Bpc * A.g.S + in;
-          l_page = table[b];
-          l_hi = min(kUnitTokens, min(A.g.S - in, sp.end - tok));
-          l_lo = max(0, sp.begin - tok);
-          ok = l_page >= 0 && l_page < A.g.num_pages && l_lo < l_hi;
-        }
-        mask = __ballot(ok);
-        next += kWave * kDecodeWaves;
-      }
-      const int at = __builtin_ctzll(mask);
-      mask &= mask - 1;
-      lo = __builtin_amdgcn_readlane(l_lo, at);
-      hi = __builtin_amdgcn_readlane(l_hi, at);
-      row = (static_cast<int64_t>(__builtin_amdgcn_readlane(l_page, at)) * A.a.H + h) * A.g.B +
-            __builtin_amdgcn_readlane(l_row, at);
-      sub = lo / L::KEYS * L::KEYS;
-      return true;
-    };
-    auto rsrc = [&](const void* pool) {
-      return tile_rsrc(static_cast<const char*>(pool) + (row + sub) * L::ROW, max(0, min(hi - sub, L::KEYS)) * L::ROW);
-    };
-
-    L t;
-    bool have = advance();
-    t.load_k(rsrc(A.a.k_pages), i, j);
-    t.load_v(rsrc(A.a.v_pages), i, j);
+    bool ahead = false;  // f is the segment behind g
+    bool follows = false;
     while (have) {
       const int clo = lo - sub, chi = hi - sub;  // rows of the tile in use
       f32x4 s[NT][RT];
@@ -382,6 +464,11 @@ __global__ __launch_bounds__(kThreads, NT == 1 ? 3 : 2) void k_decode(const Deco
 #pragma unroll
         for (int r = 0; r < RT; ++r) s[n][r] = t.qk(q[n], r);
       have = advance();
+      if (!have) {
+        ahead = true;
+        follows = next_segment();
+        if (follows) advance();
+      }
       t.load_k(rsrc(A.a.k_pages), i, j);
       const bool whole = clo <= 0 && chi >= L::KEYS;
 #pragma unroll
@@ -390,14 +477,20 @@ __global__ __launch_bounds__(kThreads, NT == 1 ? 3 : 2) void k_decode(const Deco
 #pragma unroll
         for (int r = 0; r < RT; ++r)
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            s[n][r][e] *= A.scale2;
-            if (!whole) {
+          for (int e = 0; e < 4; ++e) s[n][r][e] *= A.scale2;
+        if (!whole) {
+#pragma unroll
+          for (int r = 0; r < RT; ++r)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
               const int key = L::key(r, e, j);
-              if (key < clo || key >= chi) s[n][r][e] = -INFINITY;
+              s[n][r][e] = key >= clo && key < chi ? s[n][r][e] : -INFINITY;
             }
-            m = fmaxf(m, s[n][r][e]);
-          }
+        }
+#pragma unroll
+        for (int r = 0; r < RT; ++r)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) m = fmaxf(m, s[n][r][e]);
         m = fmaxf(max_over_groups(m), top[n]);
         const float keep = exp2f(top[n] - m);
         top[n] = m;
@@ -421,8 +514,18 @@ __global__ __launch_bounds__(kThreads, NT == 1 ? 3 : 2) void k_decode(const Deco
       t.template pv<NT>(s, o);
       t.load_v(rsrc(A.a.v_pages), i, j);
     }
+    if (!ahead) {  // the wave had no tile of this segment
+      follows = next_segment();
+      if (follows) advance();
+      t.load_k(rsrc(A.a.k_pages), i, j);
+      __builtin_amdgcn_sched_barrier(0);
+      t.load_v(rsrc(A.a.v_pages), i, j);
+    }
 
     // the waves' results meet
+    const int tile = g.head % A.head_tiles, hq0 = g.head / A.head_tiles * A.G + tile * A.tile_rows;
+    const int rows = min(A.tile_rows, A.G - tile * A.tile_rows);
+    if (!first) lds_sync();  // the last segment's results have been read
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
       const float total = sum_over_groups(sum[n]);
@@ -443,8 +546,8 @@ __global__ __launch_bounds__(kThreads, NT == 1 ? 3 : 2) void k_decode(const Deco
           }
       }
     }
-    __syncthreads();
-    const bool complete = unit == 0 && stop == sp.units;
+    lds_sync();
+    const bool complete = DIRECT || (g.unit == 0 && g.stop == g.sp.units);
     float* slot = A.part + (static_cast<int64_t>(blockIdx.x) * 2 + (first ? 0 : 1)) * A.slot_floats;
     for (int e = tid; e < rows * (D / 4); e += kThreads) {
       const int r = e / (D / 4), d = e % (D / 4) * 4;
@@ -455,14 +558,14 @@ __global__ __launch_bounds__(kThreads, NT == 1 ? 3 : 2) void k_decode(const Deco
       f32x4 x{};
 #pragma unroll
       for (int w = 0; w < kDecodeWaves; ++w) {
-        const float f = exp2f(s_top[w][r] - m);
-        total += f * s_sum[w][r];
+        const float c = exp2f(s_top[w][r] - m);
+        total += c * s_sum[w][r];
         const f32x4 y = *reinterpret_cast<const f32x4*>(&s_o[w][r][d]);
 #pragma unroll
-        for (int c = 0; c < 4; ++c) x[c] += f * y[c];
+        for (int v = 0; v < 4; ++v) x[v] += c * y[v];
       }
       if (complete) {
-        finish<T>(A, seq, hq0 + r, d, x, m, total);
+        finish<T>(A, g.seq, hq0 + r, d, x, m, total);
       } else {
         *reinterpret_cast<f32x4*>(slot + r * D + d) = x;
         if (d == 0) {
@@ -471,84 +574,88 @@ __global__ __launch_bounds__(kThreads, NT == 1 ? 3 : 2) void k_decode(const Deco
         }
       }
     }
-    __syncthreads();
-    first = false;
-    left -= stop - unit;
-    unit = stop;
-    if (left > 0 && unit == sp.units) {
-      unit = 0;
-      if (++head == HH) {
-        head = 0;
-        do sp = span_of(A.g, A.a.window, A.g.lens[++seq]);
-        while (sp.units == 0);
-      }
-    }
+    if (!follows) return;
+    g = f;
+    have = hi > sub;
   }
 }
 
 // The shares of an item that several workgroups took, joined in the order of the line by the
-// workgroup of the item's second share; x: the share, y: the query head of the tile.
-template <typename T, int D>
+// workgroups of the item's second share.  x: that share, y: ROWS query heads of the tile.  The
+// threads of a row take its dims by four, in sets that take the shares in turn and meet in LDS.
+template <typename T, int D, int ROWS>
 __global__ __launch_bounds__(256) void k_decode_join(const DecodeArgs A) {
-  constexpr int LANES = D / 4, SETS = 256 / LANES;
-  __shared__ float s_red[4];
-  __shared__ float s_sum[SETS];
-  __shared__ __align__(16) float s_o[SETS][D];
+  constexpr int LANES = D / 4, SETS = 256 / LANES / ROWS;
+  __shared__ float s_top[ROWS][SETS], s_sum[ROWS][SETS];
+  __shared__ __align__(16) float s_o[ROWS][SETS][D];
   const DecodeStart st = A.starts[blockIdx.x];
   if (st.units == 0) return;
-  const int64_t w0 = st.first / st.share;
-  if (static_cast<int64_t>(blockIdx.x) != w0 + 1) return;
-  const int parts = static_cast<int>((st.first + st.units - 1) / st.share - w0) + 1;
+  const int w0 = static_cast<int>(st.first / st.share);
+  if (static_cast<int>(blockIdx.x) != w0 + 1) return;
+  const int parts = static_cast<int>((st.first + st.units - 1) / st.share) - w0 + 1;
   const int h = st.head / A.head_tiles, tile = st.head % A.head_tiles;
-  const int r = blockIdx.y, hq = h * A.G + tile * A.tile_rows + r;
-  if (r >= min(A.tile_rows, A.G - tile * A.tile_rows)) return;
-  const int tid = threadIdx.x, set = tid / LANES, d = tid % LANES * 4;
+  const int tid = threadIdx.x, own = tid / (LANES * SETS), set = tid / LANES % SETS, d = tid % LANES * 4;
+  const int r = blockIdx.y * ROWS + own, hq = h * A.G + tile * A.tile_rows + r;
+  const bool real = r < min(A.tile_rows, A.G - tile * A.tile_rows);
   // the item's first share is its workgroup's first segment, or its last one
-  const int tail = w0 * st.share < st.first ? 1 : 0;
-  auto slot = [&](int p) { return A.part + ((w0 + p) * 2 + (p == 0 ? tail : 0)) * A.slot_floats; };
-
-  float m = kLowest;
-  for (int p = tid; p < parts; p += 256) m = fmaxf(m, slot(p)[A.rows * D + r]);
-#pragma unroll
-  for (int x = 1; x < kWave; x <<= 1) m = fmaxf(m, __shfl_xor(m, x));
-  if (tid % kWave == 0) s_red[tid / kWave] = m;
-  __syncthreads();
-  m = fmaxf(fmaxf(s_red[0], s_red[1]), fmaxf(s_red[2], s_red[3]));
-  float total = 0.f;
+  const int tail = static_cast<int64_t>(w0) * st.share < st.first ? 1 : 0;
+  float m = kLowest, total = 0.f;
   f32x4 o{};
+  if (real) {
 #pragma unroll 4
-  for (int p = set; p < parts; p += SETS) {
-    const float* s = slot(p);
-    const float f = exp2f(s[A.rows * D + r] - m);
-    total += f * s[A.rows * (D + 1) + r];
-    const f32x4 y = *reinterpret_cast<const f32x4*>(s + r * D + d);
+    for (int p = set; p < parts; p += SETS) {
+      const float* s = A.part + (static_cast<int64_t>(w0 + p) * 2 + (p == 0 ? tail : 0)) * A.slot_floats;
+      const float mp = s[A.rows * D + r], lp = s[A.rows * (D + 1) + r];
+      const f32x4 y = *reinterpret_cast<const f32x4*>(s + r * D + d);
+      const float n = fmaxf(m, mp), keep = exp2f(m - n), c = exp2f(mp - n);
+      m = n;
+      total = total * keep + c * lp;
 #pragma unroll
-    for (int c = 0; c < 4; ++c) o[c] += f * y[c];
+      for (int v = 0; v < 4; ++v) o[v] = o[v] * keep + c * y[v];
+    }
   }
-  *reinterpret_cast<f32x4*>(&s_o[set][d]) = o;
-  if (d == 0) s_sum[set] = total;
-  __syncthreads();
-  if (set != 0) return;
-  o = f32x4{};
-  total = 0.f;
-  for (int x = 0; x < SETS; ++x) {
-    total += s_sum[x];
-    const f32x4 y = *reinterpret_cast<const f32x4*>(&s_o[x][d]);
+  if constexpr (SETS > 1) {
+    *reinterpret_cast<f32x4*>(&s_o[own][set][d]) = o;
+    if (d == 0) {
+      s_top[own][set] = m;
+      s_sum[own][set] = total;
+    }
+    __syncthreads();
+    if (set != 0) return;
 #pragma unroll
-    for (int c = 0; c < 4; ++c) o[c] += y[c];
+    for (int x = 1; x < SETS; ++x) m = fmaxf(m, s_top[own][x]);
+    o = f32x4{};
+    total = 0.f;
+#pragma unroll
+    for (int x = 0; x < SETS; ++x) {
+      const float c = exp2f(s_top[own][x] - m);
+      total += c * s_sum[own][x];
+      const f32x4 y = *reinterpret_cast<const f32x4*>(&s_o[own][x][d]);
+#pragma unroll
+      for (int v = 0; v < 4; ++v) o[v] += c * y[v];
+    }
   }
-  finish<T>(A, st.seq, hq, d, o, m, total);
+  if (real) finish<T>(A, st.seq, hq, d, o, m, total);
+}
+
+template <typename T, int D, int NT>
+hipError_t launch_rows(const DecodeArgs& A, const DecodePlan& p, hipStream_t stream) {
+  LaunchStatus st;
+  if (p.direct) {
+    st(k_decode<T, D, NT, true>, dim3(p.wgs), dim3(kThreads), 0, stream, A);
+    return st.err;
+  }
+  st(k_decode<T, D, NT, false>, dim3(p.wgs), dim3(kThreads), 0, stream, A);
+  if (p.wgs > 1) {
+    const auto join = p.join_rows == 1 ? k_decode_join<T, D, 1> : p.join_rows == 2 ? k_decode_join<T, D, 2> : k_decode_join<T, D, 4>;
+    st(join, dim3(p.wgs, (p.rows + p.join_rows - 1) / p.join_rows), dim3(256), 0, stream, A);
+  }
+  return st.err;
 }
 
 template <typename T, int D>
 hipError_t launch_typed(const DecodeArgs& A, const DecodePlan& p, hipStream_t stream) {
-  LaunchStatus st;
-  if (p.tile_rows == kDecodeHeadRows)
-    st(k_decode<T, D, 1>, dim3(p.wgs), dim3(kThreads), 0, stream, A);
-  else
-    st(k_decode<T, D, 2>, dim3(p.wgs), dim3(kThreads), 0, stream, A);
-  if (p.wgs > 1) st(k_decode_join<T, D>, dim3(p.wgs, p.rows), dim3(256), 0, stream, A);
-  return st.err;
+  return p.tile_rows == kDecodeHeadRows ? launch_rows<T, D, 1>(A, p, stream) : launch_rows<T, D, 2>(A, p, stream);
 }
 
 }  // namespace

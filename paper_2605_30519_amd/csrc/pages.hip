@@ -10,24 +10,44 @@
 namespace omnimem {
 namespace {
 
-__device__ __forceinline__ void store16(const uint4 x, void* p) { *reinterpret_cast<uint4*>(p) = x; }
+template <bool PAST>
+__device__ __forceinline__ void store16(const uint4 x, void* p) {
+  const u32x4 v = {x.x, x.y, x.z, x.w};
+  if constexpr (PAST) __builtin_nontemporal_store(v, static_cast<u32x4*>(p));
+  else *static_cast<u32x4*>(p) = v;
+}
+
+__device__ __forceinline__ int block_shift(const SeqGeom& g) { return 6 + (g.B >> 7); }  // log2 B
 
 __device__ __forceinline__ int blocks_of(const SeqGeom& g, int t) {  // blocks of t tokens
-  return t / g.S * g.Bpc + (t % g.S + g.B - 1) / g.B;
+  if (g.S == g.B) return (t + g.B - 1) >> block_shift(g);
+  const int c = t / g.S;
+  return c * g.Bpc + ((t - c * g.S + g.B - 1) >> block_shift(g));
+}
+
+__device__ __forceinline__ bool block_begun(const SeqGeom& g, int t) {  // the token behind t tokens is not a block's first
+  return ((g.S == g.B ? t : t % g.S) & (g.B - 1)) != 0;
 }
 
 __device__ __forceinline__ int clamped_len(const SeqGeom& g, int s) { return min(max(g.lens[s], 0), g.cap); }
+
+// Stores past the caches pay for what the 256 MB memory-side cache cannot hold beside what it
+// is copied from: 201 MB of copied pages 86.3 -> 77.5 us, 172 MB of appended tokens 70.7 -> 67.3;
+// 100 MB of pages 35.5 -> 38.7 and 115 MB of tokens 42.6 -> 44.0 without.
+constexpr int64_t kPastBytes = 144ll << 20;  // written
 
 // ---------------------------------------------------------------- append
 // Copies: a token's row of H * d values becomes H pieces of d, each 16-byte chunk of it
 // moved by one lane.  Chunks of all rows are numbered through; a workgroup takes
 // U * 256 of them in K and in V, all loads in flight before the lookups that say where they go:
-// row -> sequence (starts), its length, and the page.
-constexpr int kAppendThreads = 256;
+// row -> sequence (starts), its length, and the page.  Bound by its bytes: eight chunks of
+// 4,680 tokens, 12 heads, bf16 (460 MB read and written) 89 us, 5.2 TB/s; 64 single tokens 4.1 us,
+// three dependent loads.
+constexpr int kAppendThreads = 256, kAppendUnroll = 4;
 
-template <int U>
+template <bool PAST>
 __global__ __launch_bounds__(kAppendThreads) void k_append_kv(const SeqGeom g, const AppendLaunch a) {
-  constexpr int kChunks = U * kAppendThreads;
+  constexpr int U = kAppendUnroll, kChunks = U * kAppendThreads;
   constexpr int kRows = kChunks / 8 + 2;  // rows of at least 8 chunks (one head of 64 bf16)
   __shared__ int s_seq[kRows];
   __shared__ int64_t s_to[kRows];  // chunk of head 0's piece in the pools, or -1
@@ -84,22 +104,21 @@ __global__ __launch_bounds__(kAppendThreads) void k_append_kv(const SeqGeom g, c
     if (to < 0) continue;
     const int h = in[u] / a.head_chunks;
     const int64_t at = to + static_cast<int64_t>(h) * g.B * a.head_chunks + (in[u] - h * a.head_chunks);
-    store16(kk[u], static_cast<uint4*>(a.k_pages) + at);
-    store16(vv[u], static_cast<uint4*>(a.v_pages) + at);
+    store16<PAST>(kk[u], static_cast<uint4*>(a.k_pages) + at);
+    store16<PAST>(vv[u], static_cast<uint4*>(a.v_pages) + at);
   }
 }
 
 // ---------------------------------------------------------------- copies of pages
 // A grid that is resident at once walks pieces of 16 KB of (pair, layer, pool); the number of
-// pairs is read on the device.
+// pairs is read on the device.  Bound by its bytes: 300 pages of 12 heads x 64 x 128 bf16 in six
+// layers (1.4 GB read and written) 279 us, 5.1 TB/s, as a large tensor copy (5.0); 16 pages 4.2 us.
 constexpr int kCopyThreads = 256, kCopyUnroll = 4, kCopyPiece = kCopyThreads * kCopyUnroll;
 constexpr int kCopyMaxWgs = 2048;
 
-__global__ __launch_bounds__(kCopyThreads) void k_copy_pages(const CopyLaunch a, int pieces) {
-  const int pools = a.v_pages != nullptr ? 2 : 1;
-  const int pairs = a.count == nullptr ? a.max_pairs : min(max(*a.count, 0), a.max_pairs);
-  const int64_t per_pair = static_cast<int64_t>(pieces) * pools * a.layers;
-  const int64_t total = per_pair * pairs;
+template <bool PAST>
+__device__ __forceinline__ void copy_pieces(const CopyLaunch& a, int pieces, int pools, int64_t per_pair,
+                                            int64_t total) {
   for (int64_t w = blockIdx.x; w < total; w += gridDim.x) {
     const int64_t p = w / per_pair;
     const int64_t rest = w - p * per_pair;
@@ -120,45 +139,54 @@ __global__ __launch_bounds__(kCopyThreads) void k_copy_pages(const CopyLaunch a,
 #pragma unroll
     for (int u = 0; u < kCopyUnroll; ++u) {
       const int64_t c = at + u * kCopyThreads + threadIdx.x;
-      if (c < a.page_chunks) store16(x[u], to + c);
+      if (c < a.page_chunks) store16<PAST>(x[u], to + c);
     }
   }
 }
 
+__global__ __launch_bounds__(kCopyThreads) void k_copy_pages(const CopyLaunch a, int pieces) {
+  const int pools = a.v_pages != nullptr ? 2 : 1;
+  const int pairs = a.count == nullptr ? a.max_pairs : min(max(*a.count, 0), a.max_pairs);
+  const int64_t per_pair = static_cast<int64_t>(pieces) * pools * a.layers, total = per_pair * pairs;
+  if (a.page_chunks * 16 * pools * a.layers * pairs > kPastBytes)
+    copy_pieces<true>(a, pieces, pools, per_pair, total);
+  else
+    copy_pieces<false>(a, pieces, pools, per_pair, total);
+}
+
 // ---------------------------------------------------------------- tables
-// The pool's state is a function of the tables, formed anew by every call: a bitmap of the
-// pages in use, marked by atomics whose order does not matter, and ranks in it.  The k-th
+// The pool's state is a function of the tables, formed anew by every call: bitmaps of the
+// pages in use, marked by atomics whose order does not matter, and ranks in them.  The k-th
 // free or used page is found by a search over prefix counts that every workgroup forms for
 // itself in LDS, so no list of free pages is kept or built.
 constexpr int kSeqThreads = 512;
 
-struct RowPlan {  // of a new row
-  int keep, grow;  // grow < 0: past the capacity
-  int tail_page;   // page of the begun block that the row will write to, or -1
-  int parent;      // or -1
-};
 
 struct SeqScratch {
-  uint32_t* used;  // pages that a kept block names
-  uint32_t* held;  // of them, pages that a row names without writing to them next
-  int* first;      // lowest row that writes to a page (set for pages written to alone)
+  uint32_t* held;  // pages that a row names without writing to them next
+  uint32_t* tail;  // pages that a row will write to (update)
+  int* first;      // the lowest such row of a page of `tail`
   RowPlan* rows;
   int64_t words;
 };
 
 __device__ __forceinline__ RowPlan plan_row(const SeqGeom& g, const SeqUpdateLaunch& a, int r) {
-  RowPlan p{0, 0, -1, a.parent[r]};
-  if (p.parent < 0 || p.parent >= g.N) p.parent = -1;
-  if (p.parent >= 0) {
-    const int len = clamped_len(g, p.parent);
-    p.keep = a.keep == nullptr ? len : min(max(a.keep[r], 0), len);
-  }
-  p.grow = a.grow == nullptr ? 0 : max(a.grow[r], 0);
-  if (p.grow > 0 && p.keep % g.S % g.B != 0) {
-    const int page = g.table[static_cast<int64_t>(p.parent) * g.M + blocks_of(g, p.keep) - 1];
+  RowPlan p{};
+  p.tail_page = -1;
+  p.parent = a.parent[r];
+  const int keep = a.keep == nullptr ? INT_MAX : a.keep[r], want = a.grow == nullptr ? 0 : a.grow[r];
+  int tokens = 0;
+  if (p.parent >= 0 && p.parent < g.N) tokens = min(max(keep, 0), clamped_len(g, p.parent));
+  const int grow = max(want, 0);
+  p.kept = blocks_of(g, tokens);
+  if (grow > 0 && block_begun(g, tokens)) {
+    const int page = g.table[static_cast<int64_t>(p.parent) * g.M + p.kept - 1];
     if (page >= 0 && page < g.num_pages) p.tail_page = page;
   }
-  if (static_cast<int64_t>(p.keep) + p.grow > g.cap) p.grow = -1;
+  p.over = static_cast<int64_t>(tokens) + grow > g.cap;
+  p.len = p.over ? tokens : tokens + grow;
+  p.short_len = tokens;
+  p.added = p.over ? 0 : blocks_of(g, p.len) - p.kept;
   return p;
 }
 
@@ -170,58 +198,94 @@ __device__ __forceinline__ int entry(const SeqGeom& g, int row, int b) {
   return page >= 0 && page < g.num_pages ? page : -1;
 }
 
-// Counts of free pages in front of every thread's run of words.
-template <int NT>
-struct FreeRanks {
-  int before[NT];
-  int scan[NT / kWave];
-
-  __device__ __forceinline__ static uint32_t free_in(const uint32_t* used, int64_t w, int64_t pages) {
-    const int64_t left = pages - w * 32;
-    return ~used[w] & (left >= 32 ? 0xffffffffu : (1u << left) - 1u);
-  }
-  __device__ __forceinline__ int count(const uint32_t* used, int64_t words, int64_t pages) {  // all threads; the free pages
-    const int64_t per = (words + NT - 1) / NT;
-    const int64_t lo = min(threadIdx.x * per, words), hi = min(lo + per, words);
-    int n = 0;
-    for (int64_t w = lo; w < hi; ++w) n += __popc(free_in(used, w, pages));
-    int all;
-    const int at = block_exclusive_scan<NT>(n, scan, all);
-    before[threadIdx.x] = at;
+// Exclusive prefix sums of V values over a workgroup, and their totals; one barrier.
+template <int NT, int V>
+struct Scan {
+  int wave[V][NT / kWave];
+  __device__ __forceinline__ void operator()(int (&x)[V], int (&all)[V]) {
+    const int lane = threadIdx.x % kWave, w = threadIdx.x / kWave;
+    int upto[V];
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+      upto[v] = wave_inclusive_scan(x[v]);
+      if (lane == kWave - 1) wave[v][w] = upto[v];
+    }
     __syncthreads();
-    return all;
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+      int before = 0;
+      all[v] = 0;
+#pragma unroll
+      for (int o = 0; o < NT / kWave; ++o) {
+        if (o < w) before += wave[v][o];
+        all[v] += wave[v][o];
+      }
+      x[v] = before + upto[v] - x[v];
+    }
+  }
+};
+
+// The pages of a pool that are in use, as a bitmap in one or two parts, and how many free
+// ones lie in front of each thread's run of its words.
+template <int NT>
+struct Pages {
+  const uint32_t* a;
+  const uint32_t* b;  // or null
+  uint32_t pages;
+  int words, per;
+  int* before;  // [NT], shared
+
+  __device__ __forceinline__ Pages(const uint32_t* a_, const uint32_t* b_, int64_t pages_, int* before_)
+      : a(a_), b(b_), pages(static_cast<uint32_t>(pages_)), words(static_cast<int>((pages_ + 31) / 32)),
+        per((words + NT - 1) / NT), before(before_) {}
+  __device__ __forceinline__ uint32_t used_in(int w) const { return b == nullptr ? a[w] : a[w] | b[w]; }
+  __device__ __forceinline__ uint32_t free_in(int w) const {
+    const uint32_t left = pages - static_cast<uint32_t>(w) * 32u;  // > 0
+    return ~used_in(w) & (left >= 32u ? 0xffffffffu : (1u << left) - 1u);
+  }
+  __device__ __forceinline__ int free_of_run() const {  // in the calling thread's run
+    const int lo = min(static_cast<int>(threadIdx.x) * per, words), hi = min(lo + per, words);
+    int n = 0;
+    for (int w = lo; w < hi; ++w) n += __popc(free_in(w));
+    return n;
   }
   // free pages in front of `page`
-  __device__ __forceinline__ int rank(const uint32_t* used, int64_t words, int64_t pages, int page) const {
-    const int64_t per = (words + NT - 1) / NT;
-    const int64_t w = page >> 5;
-    const int run = static_cast<int>(w / per);
+  __device__ __forceinline__ int rank(int page) const {
+    const int w = page >> 5, run = per == 1 ? w : w / per;
     int n = before[run];
-    for (int64_t x = run * per; x < w; ++x) n += __popc(free_in(used, x, pages));
-    return n + __popc(free_in(used, w, pages) & ((1u << (page & 31)) - 1u));
+    for (int x = run * per; x < w; ++x) n += __popc(free_in(x));
+    return n + __popc(free_in(w) & ((1u << (page & 31)) - 1u));
   }
   // the k-th page (from 0) that is free, or in use; the caller knows that there is one
   template <bool FREE>
-  __device__ __forceinline__ int select(const uint32_t* used, int64_t words, int64_t pages, int k) const {
-    const int64_t per = (words + NT - 1) / NT;
+  __device__ __forceinline__ int select(int k) const {
     auto ahead = [&](int run) {  // pages of the kind in front of a run
-      return FREE ? before[run] : static_cast<int>(min(run * per * 32, pages)) - before[run];
+      return FREE ? before[run]
+                  : static_cast<int>(static_cast<uint32_t>(min(run * per, words)) * 32u) - before[run];
     };
     int run = 0;
 #pragma unroll
     for (int step = NT / 2; step > 0; step >>= 1)
       if (ahead(run + step) <= k) run += step;
     k -= ahead(run);
-    for (int64_t w = run * per; w < words; ++w) {
-      uint32_t bits = free_in(used, w, pages);
-      if (!FREE) bits = used[w];
+    for (int w = run * per; w < words; ++w) {
+      uint32_t bits = FREE ? free_in(w) : used_in(w);
       const int n = __popc(bits);
       if (k >= n) {
         k -= n;
         continue;
       }
-      for (; k > 0; --k) bits &= bits - 1;
-      return static_cast<int>(w * 32 + __builtin_ctz(bits));
+      int at = 0;  // the k-th set bit, by halves
+#pragma unroll
+      for (int half = 16; half > 0; half >>= 1) {
+        const int low = __popc(bits & ((1u << half) - 1u));
+        if (k >= low) {
+          k -= low;
+          bits >>= half;
+          at += half;
+        }
+      }
+      return w * 32 + at;
     }
     return -1;
   }
@@ -230,8 +294,8 @@ struct FreeRanks {
 __global__ __launch_bounds__(256) void k_seq_clear(const SeqGeom g, const SeqUpdateLaunch a, const SeqScratch x) {
   const int64_t id = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x, n = static_cast<int64_t>(gridDim.x) * 256;
   for (int64_t w = id; w < x.words; w += n) {
-    x.used[w] = 0;
-    if (a.num_new > 0) x.held[w] = 0;
+    x.held[w] = 0;
+    if (a.num_new > 0) x.tail[w] = 0;
   }
   for (int64_t r = id; r < a.num_new; r += n) {
     const RowPlan p = plan_row(g, a, static_cast<int>(r));
@@ -248,7 +312,7 @@ __global__ __launch_bounds__(256) void k_seq_mark(const SeqGeom g, const SeqUpda
     if (a.num_new > 0) {
       const RowPlan p = x.rows[r];
       src = p.parent;
-      blocks = blocks_of(g, p.keep);
+      blocks = p.kept;
       if (p.tail_page >= 0) tail = blocks - 1;
     } else {
       blocks = blocks_of(g, clamped_len(g, r));
@@ -256,124 +320,248 @@ __global__ __launch_bounds__(256) void k_seq_mark(const SeqGeom g, const SeqUpda
     for (int b = blockIdx.x * 256 + threadIdx.x; b < blocks; b += gridDim.x * 256) {
       const int page = entry(g, src, b);
       if (page < 0) continue;
-      set_bit(x.used, page);
-      if (a.num_new == 0) continue;
-      if (b == tail) atomicMin(x.first + page, r);
-      else set_bit(x.held, page);
+      if (b != tail) {
+        set_bit(x.held, page);
+      } else {
+        set_bit(x.tail, page);
+        atomicMin(x.first + page, r);
+      }
+    }
+  }
+}
+
+// New rows from marked pages, by the workgroups of a grid, `lanes` threads to a row.
+// held(page): some row names the page without writing to it; first(page): the lowest row that
+// writes to it; row(r): a row's plan.
+template <int NT, bool FLAT, typename Held, typename First, typename Row>
+__device__ __forceinline__ void write_rows(const SeqGeom& g, const SeqUpdateLaunch& a, const Pages<NT>& pool,
+                                           Scan<NT, 4>& scan, int* s_want, int* s_copies, int lanes, Held held,
+                                           First first, Row row) {
+  const int tid = threadIdx.x;
+  auto copies_page = [&](const RowPlan& p, int r) -> bool {
+    return !p.over && p.tail_page >= 0 && (held(p.tail_page) || first(p.tail_page) != r);
+  };
+  // free pages, what the rows ask for, and rows past the capacity, by runs of words and of rows
+  const int per = (a.num_new + NT - 1) / NT;
+  const int lo = min(tid * per, a.num_new), hi = min(lo + per, a.num_new);
+  int x[4] = {pool.free_of_run(), 0, 0, 0}, all[4];
+  for (int r = lo; r < hi; ++r) {
+    const RowPlan p = row(r);
+    const int c = copies_page(p, r);
+    x[1] += c + p.added;
+    x[2] += c;
+    x[3] += p.over;
+  }
+  scan(x, all);
+  pool.before[tid] = x[0];
+  s_want[tid] = x[1];
+  s_copies[tid] = x[2];
+  __syncthreads();
+  const int room = all[0];
+  const bool done = all[1] <= room && all[3] == 0;
+  const int copied = done ? all[2] : 0;
+  if (blockIdx.x == 0) {
+    if (tid == 0) {
+      a.info[0] = copied;
+      a.info[1] = static_cast<int>(g.num_pages) - room + (done ? all[1] : 0);
+      a.info[2] = max(all[1] - room, 0);
+      a.info[3] = all[3];
+    }
+    for (int r = copied + tid; r < a.num_new; r += NT) {
+      a.pairs[2 * r] = -1;
+      a.pairs[2 * r + 1] = -1;
+    }
+  }
+  // block b of row r, whose pages begin with number `at` of those asked for
+  auto block = [&](const RowPlan& p, int r, int b, int copy, int at, int nth) {
+    int page = -1;
+    if (b < p.kept) page = entry(g, p.parent, b);
+    const int fresh = b - p.kept;  // of the row's added blocks; -1: the block that is copied
+    if (done && (fresh >= 0 ? fresh < p.added : copy && fresh == -1)) {
+      if (fresh < 0) {
+        a.pairs[2 * nth] = page;
+        a.pairs[2 * nth + 1] = pool.template select<true>(at);
+      }
+      page = pool.template select<true>(at + copy + fresh);
+    }
+    a.out_table[static_cast<int64_t>(r) * g.M + b] = page;
+    if (b == 0) a.out_lens[r] = done ? p.len : p.short_len;
+  };
+  if constexpr (FLAT) {  // one workgroup, no more rows than threads
+    const int step_r = NT / g.M, step_b = NT - step_r * g.M;
+    int r = tid / g.M, b = tid - r * g.M;
+    while (r < a.num_new) {
+      const RowPlan p = row(r);
+      block(p, r, b, copies_page(p, r), s_want[r], s_copies[r]);
+      r += step_r;
+      b += step_b;
+      if (b >= g.M) {
+        b -= g.M;
+        ++r;
+      }
+    }
+  } else {
+    const int teams = NT / lanes;
+    for (int r = blockIdx.x * teams + tid / lanes; r < a.num_new; r += gridDim.x * teams) {
+      const RowPlan p = row(r);
+      const int run = r / per;
+      int at = s_want[run], nth = s_copies[run];
+      for (int y = run * per; y < r; ++y) {
+        const RowPlan o = row(y);
+        const int c = copies_page(o, y);
+        nth += c;
+        at += c + o.added;
+      }
+      const int copy = copies_page(p, r);
+      for (int b = tid % lanes; b < g.M; b += lanes) block(p, r, b, copy, at, nth);
     }
   }
 }
 
 __global__ __launch_bounds__(kSeqThreads) void k_seq_update(const SeqGeom g, const SeqUpdateLaunch a,
-                                                            const SeqScratch x) {
-  __shared__ FreeRanks<kSeqThreads> ranks;
-  __shared__ int s_scan[kSeqThreads / kWave];
-  __shared__ int s_want[kSeqThreads], s_copies[kSeqThreads];  // of the rows in front of each thread's run
+                                                            const SeqScratch x, int lanes) {
+  __shared__ int s_free[kSeqThreads], s_want[kSeqThreads], s_copies[kSeqThreads];
+  __shared__ Scan<kSeqThreads, 4> scan;
+  const Pages<kSeqThreads> pool(x.held, x.tail, g.num_pages, s_free);
+  write_rows<kSeqThreads, false>(
+      g, a, pool, scan, s_want, s_copies, lanes,
+      [&](int page) { return (x.held[page >> 5] >> (page & 31) & 1u) != 0; }, [&](int page) { return x.first[page]; },
+      [&](int r) { return x.rows[r]; });
+}
+
+// The rows and moves of a compaction; lens: the rows' blocks in LDS (FLAT: one workgroup).
+template <int NT, bool FLAT>
+__device__ __forceinline__ void write_compacted(const SeqGeom& g, const SeqUpdateLaunch& a, const Pages<NT>& pool,
+                                                Scan<NT, 1>& scan, int max_moves, int lanes, const int* s_blocks) {
   const int tid = threadIdx.x;
-  const int room = ranks.count(x.used, x.words, g.num_pages);
-  // what every row asks for
-  auto copies_page = [&](const RowPlan& p, int r) -> bool {
-    return p.grow > 0 && p.tail_page >= 0 &&
-           ((x.held[p.tail_page >> 5] >> (p.tail_page & 31) & 1u) != 0 || x.first[p.tail_page] != r);
-  };
-  auto added = [&](const RowPlan& p) { return p.grow > 0 ? blocks_of(g, p.keep + p.grow) - blocks_of(g, p.keep) : 0; };
-  const int per = (a.num_new + kSeqThreads - 1) / kSeqThreads;
-  const int lo = min(tid * per, a.num_new), hi = min(lo + per, a.num_new);
-  int want = 0, copies = 0, over = 0;
-  for (int r = lo; r < hi; ++r) {
-    const RowPlan p = x.rows[r];
-    const int c = copies_page(p, r);
-    copies += c;
-    want += c + added(p);
-    over += p.grow < 0;
-  }
-  int all_want, all_copies, all_over;
-  const int want_before = block_exclusive_scan<kSeqThreads>(want, s_scan, all_want);
-  const int copies_before = block_exclusive_scan<kSeqThreads>(copies, s_scan, all_copies);
-  block_exclusive_scan<kSeqThreads>(over, s_scan, all_over);
-  s_want[tid] = want_before;
-  s_copies[tid] = copies_before;
+  int x[1] = {pool.free_of_run()}, all[1];
+  scan(x, all);
+  pool.before[tid] = x[0];
   __syncthreads();
-  const bool done = all_want <= room && all_over == 0;
-  if (blockIdx.x == 0) {
-    if (tid == 0) {
-      a.info[0] = done ? all_copies : 0;
-      a.info[1] = static_cast<int>(g.num_pages) - room + (done ? all_want : 0);
-      a.info[2] = max(all_want - room, 0);
-      a.info[3] = all_over;
+  const int pages = static_cast<int>(g.num_pages), in_use = pages - all[0];
+  // free pages in front of the border, which the used ones behind it fill
+  const int moves = in_use < pages ? pool.rank(in_use) : 0;
+  const int in_place = in_use - moves;
+  if (blockIdx.x == 0 && tid < 4) a.info[tid] = tid == 0 ? moves : tid == 1 ? in_use : 0;
+  for (int64_t m = static_cast<int64_t>(blockIdx.x) * NT + tid; m < max_moves; m += static_cast<int64_t>(gridDim.x) * NT) {
+    int2 move = {-1, -1};
+    if (m < moves) {
+      move.x = pool.template select<false>(in_place + static_cast<int>(m));
+      move.y = pool.template select<true>(static_cast<int>(m));
     }
-    for (int r = (done ? all_copies : 0) + tid; r < a.num_new; r += kSeqThreads) {
-      a.pairs[2 * r] = -1;
-      a.pairs[2 * r + 1] = -1;
-    }
+    a.pairs[2 * m] = move.x;
+    a.pairs[2 * m + 1] = move.y;
   }
-  for (int r = blockIdx.x; r < a.num_new; r += gridDim.x) {
-    const RowPlan p = x.rows[r];
-    const int run = r / per;
-    int at = s_want[run], nth = s_copies[run];
-    for (int y = run * per; y < r; ++y) {
-      const RowPlan o = x.rows[y];
-      const int c = copies_page(o, y);
-      nth += c;
-      at += c + added(o);
-    }
-    const int kept = blocks_of(g, p.keep);
-    const int copy = done && copies_page(p, r);
-    const int blocks = done ? kept + added(p) : kept;
-    int32_t* out = a.out_table + static_cast<int64_t>(r) * g.M;
-    for (int b = tid; b < g.M; b += kSeqThreads) {
-      int page = -1;
-      if (b < kept) page = entry(g, p.parent, b);
-      if (b >= blocks) page = -1;
-      else if (b >= kept) page = ranks.template select<true>(x.used, x.words, g.num_pages, at + copy + b - kept);
-      else if (copy && b == kept - 1) {
-        page = ranks.template select<true>(x.used, x.words, g.num_pages, at);
-        a.pairs[2 * nth] = p.tail_page;
-        a.pairs[2 * nth + 1] = page;
+  auto block = [&](int r, int b, int blocks) {
+    int page = b < blocks ? entry(g, r, b) : -1;
+    if (page >= in_use) page = pool.template select<true>(page - pool.rank(page) - in_place);
+    a.out_table[static_cast<int64_t>(r) * g.M + b] = page;
+  };
+  if constexpr (FLAT) {
+    const int step_r = NT / g.M, step_b = NT - step_r * g.M;
+    for (int r = tid / g.M, b = tid - r * g.M; r < g.N;) {
+      block(r, b, s_blocks[r]);
+      r += step_r;
+      b += step_b;
+      if (b >= g.M) {
+        b -= g.M;
+        ++r;
       }
-      out[b] = page;
     }
-    if (tid == 0) a.out_lens[r] = p.keep + (done ? p.grow : 0);
+  } else {
+    const int teams = NT / lanes;
+    for (int r = blockIdx.x * teams + tid / lanes; r < g.N; r += gridDim.x * teams) {
+      const int blocks = blocks_of(g, clamped_len(g, r));
+      for (int b = tid % lanes; b < g.M; b += lanes) block(r, b, blocks);
+    }
   }
 }
 
 __global__ __launch_bounds__(kSeqThreads) void k_seq_compact(const SeqGeom g, const SeqUpdateLaunch a,
-                                                             const SeqScratch x, int max_moves) {
-  __shared__ FreeRanks<kSeqThreads> ranks;
-  const int tid = threadIdx.x;
-  const int pages = static_cast<int>(g.num_pages);
-  const int in_use = pages - ranks.count(x.used, x.words, g.num_pages);
-  // free pages in front of the border, which the used ones behind it fill
-  const int moves = in_use < pages ? ranks.rank(x.used, x.words, g.num_pages, in_use) : 0;
-  if (blockIdx.x == 0 && tid < 4) a.info[tid] = tid == 0 ? moves : tid == 1 ? in_use : 0;
-  for (int64_t m = static_cast<int64_t>(blockIdx.x) * kSeqThreads + tid; m < max_moves;
-       m += static_cast<int64_t>(gridDim.x) * kSeqThreads) {
-    int from = -1, to = -1;
-    if (m < moves) {
-      from = ranks.template select<false>(x.used, x.words, g.num_pages, in_use - moves + static_cast<int>(m));
-      to = ranks.template select<true>(x.used, x.words, g.num_pages, static_cast<int>(m));
-    }
-    a.pairs[2 * m] = from;
-    a.pairs[2 * m + 1] = to;
-  }
-  for (int r = blockIdx.x; r < g.N; r += gridDim.x) {
-    const int blocks = blocks_of(g, clamped_len(g, r));
-    int32_t* out = a.out_table + static_cast<int64_t>(r) * g.M;
-    for (int b = tid; b < g.M; b += kSeqThreads) {
-      int page = b < blocks ? entry(g, r, b) : -1;
-      if (page >= in_use) {
-        // used pages in front of it, less those in front of the border
-        const int nth = page - ranks.rank(x.used, x.words, g.num_pages, page) - (in_use - moves);
-        page = ranks.template select<true>(x.used, x.words, g.num_pages, nth);
-      }
-      out[b] = page;
+                                                             const SeqScratch x, int max_moves, int lanes) {
+  __shared__ int s_free[kSeqThreads];
+  __shared__ Scan<kSeqThreads, 1> scan;
+  const Pages<kSeqThreads> pool(x.held, nullptr, g.num_pages, s_free);
+  write_compacted<kSeqThreads, false>(g, a, pool, scan, max_moves, lanes, nullptr);
+}
+
+// Small tables in one workgroup and one launch, all state in LDS: a word per page, INT_MAX free,
+// -1 named by a row that does not write to it, else the lowest row that does.  One launch costs
+// the host 6 us less than three; on the GPU, 16 rows of 18 entries take 7.1 us against 10.6
+// (update; compaction 5.2 / 8.6), 16 of 252 9.2 / 11.9 (9.3 / 13.3), 8 of 939 11.6 / 12.0 (13.4 / 11.5),
+// 256 of 65 27 / 14 (29 / 13): one CU's instruction rate.
+constexpr int kOneThreads = 1024, kOnePages = 16384, kOneRows = 1024;
+constexpr int64_t kOneEntries = 8192;
+
+__device__ __forceinline__ void bitmap_of(const int* state, uint32_t* used, int pages) {
+  for (int p = threadIdx.x; p < (pages + kWave - 1) / kWave * kWave; p += kOneThreads) {
+    const uint64_t bits = __ballot(p < pages && state[p] != INT_MAX);
+    if (threadIdx.x % kWave == 0) {
+      used[p / 32] = static_cast<uint32_t>(bits);
+      used[p / 32 + 1] = static_cast<uint32_t>(bits >> 32);
     }
   }
 }
 
+__global__ __launch_bounds__(kOneThreads) void k_seq_update_one(const SeqGeom g, const SeqUpdateLaunch a) {
+  __shared__ int s_state[kOnePages];
+  __shared__ uint32_t s_used[kOnePages / 32];
+  __shared__ int s_free[kOneThreads], s_want[kOneThreads], s_copies[kOneThreads];
+  __shared__ RowPlan s_rows[kOneRows];
+  __shared__ Scan<kOneThreads, 4> scan;
+  const int tid = threadIdx.x, pages = static_cast<int>(g.num_pages);
+  if (tid < a.num_new) s_rows[tid] = plan_row(g, a, tid);
+  for (int p = tid; p < pages; p += kOneThreads) s_state[p] = INT_MAX;
+  __syncthreads();
+  const int step_r = kOneThreads / g.M, step_b = kOneThreads - step_r * g.M;
+  for (int r = tid / g.M, b = tid - r * g.M; r < a.num_new;) {
+    const RowPlan& p = s_rows[r];
+    const int page = b < p.kept ? entry(g, p.parent, b) : -1;
+    if (page >= 0) atomicMin(&s_state[page], p.tail_page >= 0 && b == p.kept - 1 ? r : -1);
+    r += step_r;
+    b += step_b;
+    if (b >= g.M) {
+      b -= g.M;
+      ++r;
+    }
+  }
+  __syncthreads();
+  bitmap_of(s_state, s_used, pages);
+  __syncthreads();
+  const Pages<kOneThreads> pool(s_used, nullptr, g.num_pages, s_free);
+  write_rows<kOneThreads, true>(
+      g, a, pool, scan, s_want, s_copies, kWave, [&](int page) { return s_state[page] < 0; },
+      [&](int page) { return s_state[page]; }, [&](int r) { return s_rows[r]; });
+}
+
+__global__ __launch_bounds__(kOneThreads) void k_seq_compact_one(const SeqGeom g, const SeqUpdateLaunch a,
+                                                                 int max_moves) {
+  __shared__ uint32_t s_used[kOnePages / 32];
+  __shared__ int s_free[kOneThreads], s_blocks[kOneRows];
+  __shared__ Scan<kOneThreads, 1> scan;
+  const int tid = threadIdx.x;
+  for (int w = tid; w < kOnePages / 32; w += kOneThreads) s_used[w] = 0;
+  if (tid < g.N) s_blocks[tid] = blocks_of(g, clamped_len(g, tid));
+  __syncthreads();
+  const int step_r = kOneThreads / g.M, step_b = kOneThreads - step_r * g.M;
+  for (int r = tid / g.M, b = tid - r * g.M; r < g.N;) {
+    const int page = b < s_blocks[r] ? entry(g, r, b) : -1;
+    if (page >= 0) atomicOr(&s_used[page >> 5], 1u << (page & 31));
+    r += step_r;
+    b += step_b;
+    if (b >= g.M) {
+      b -= g.M;
+      ++r;
+    }
+  }
+  __syncthreads();
+  const Pages<kOneThreads> pool(s_used, nullptr, g.num_pages, s_free);
+  write_compacted<kOneThreads, true>(g, a, pool, scan, max_moves, kWave, s_blocks);
+}
+
 SeqScratch scratch_of(const SeqPlan& p, void* workspace) {
   char* ws = static_cast<char*>(workspace);
-  return SeqScratch{reinterpret_cast<uint32_t*>(ws + p.off_used), reinterpret_cast<uint32_t*>(ws + p.off_held),
+  return SeqScratch{reinterpret_cast<uint32_t*>(ws + p.off_held), reinterpret_cast<uint32_t*>(ws + p.off_tail),
                     reinterpret_cast<int*>(ws + p.off_first), reinterpret_cast<RowPlan*>(ws + p.off_rows), p.words};
 }
 
@@ -390,14 +578,22 @@ void mark_used(const SeqGeom& g, const SeqPlan& p, const SeqUpdateLaunch& a, con
     st(k_seq_mark, dim3(wide < 64 ? wide : 64, rows < 16384 ? rows : 16384), dim3(256), 0, stream, g, a, x, rows);
 }
 
+// Threads to a row and workgroups of the kernels that write rows: a wave for short rows, a
+// workgroup for long ones.
+int row_lanes(const SeqGeom& g) { return g.M <= 4 * kWave ? kWave : kSeqThreads; }
+int row_wgs(int64_t rows, int lanes) {
+  const int64_t teams = kSeqThreads / lanes, wgs = (rows + teams - 1) / teams;
+  return static_cast<int>(wgs < 1 ? 1 : wgs < kSeqMaxWgs ? wgs : kSeqMaxWgs);
+}
+
 }  // namespace
 
 hipError_t launch_append_kv(const SeqGeom& g, const AppendLaunch& a, hipStream_t stream) {
-  constexpr int U = 4;
-  const int64_t chunks = a.tokens * a.row_chunks;
-  const int64_t wgs = (chunks + U * kAppendThreads - 1) / (U * kAppendThreads);
+  constexpr int kChunks = kAppendUnroll * kAppendThreads;
+  const int64_t chunks = a.tokens * a.row_chunks, wgs = (chunks + kChunks - 1) / kChunks;
   if (wgs > 0x7fffffff) return hipErrorInvalidConfiguration;
-  return launch_kernel(k_append_kv<U>, dim3(static_cast<unsigned>(wgs)), dim3(kAppendThreads), 0, stream, g, a);
+  const auto kernel = 2 * 16 * chunks > kPastBytes ? k_append_kv<true> : k_append_kv<false>;
+  return launch_kernel(kernel, dim3(static_cast<unsigned>(wgs)), dim3(kAppendThreads), 0, stream, g, a);
 }
 
 hipError_t launch_copy_pages(const CopyLaunch& a, hipStream_t stream) {
@@ -410,23 +606,29 @@ hipError_t launch_copy_pages(const CopyLaunch& a, hipStream_t stream) {
 
 hipError_t launch_seq_update(const SeqGeom& g, const SeqPlan& p, const SeqUpdateLaunch& a, void* workspace,
                              hipStream_t stream) {
+  if (g.num_pages <= kOnePages && a.num_new <= kOneRows && static_cast<int64_t>(a.num_new) * g.M <= kOneEntries)
+    return launch_kernel(k_seq_update_one, dim3(1), dim3(kOneThreads), 0, stream, g, a);
   const SeqScratch x = scratch_of(p, workspace);
   LaunchStatus st;
   mark_used(g, p, a, x, a.num_new, stream, st);
-  const int wgs = a.num_new < 1 ? 1 : a.num_new < kSeqMaxWgs ? a.num_new : kSeqMaxWgs;
-  st(k_seq_update, dim3(wgs), dim3(kSeqThreads), 0, stream, g, a, x);
+  const int lanes = row_lanes(g);
+  st(k_seq_update, dim3(row_wgs(a.num_new, lanes)), dim3(kSeqThreads), 0, stream, g, a, x, lanes);
   return st.err;
 }
 
 hipError_t launch_seq_compact(const SeqGeom& g, const SeqPlan& p, const SeqUpdateLaunch& a, void* workspace,
                               hipStream_t stream) {
-  const SeqScratch x = scratch_of(p, workspace);
   const int max_moves = g.num_pages >= 2 ? static_cast<int>(g.num_pages / 2) : 1;
+  if (g.num_pages <= kOnePages && g.N <= kOneRows && static_cast<int64_t>(g.N) * g.M <= kOneEntries)
+    return launch_kernel(k_seq_compact_one, dim3(1), dim3(kOneThreads), 0, stream, g, a, max_moves);
+  const SeqScratch x = scratch_of(p, workspace);
   LaunchStatus st;
   mark_used(g, p, a, x, g.N, stream, st);
+  const int lanes = row_lanes(g);
   const int64_t work = (static_cast<int64_t>(max_moves) + kSeqThreads - 1) / kSeqThreads;
-  const int64_t most = work > g.N ? work : g.N;
-  st(k_seq_compact, dim3(most < kSeqMaxWgs ? most : kSeqMaxWgs), dim3(kSeqThreads), 0, stream, g, a, x, max_moves);
+  const int rows = row_wgs(g.N, lanes);
+  const int wgs = work < rows ? rows : work < kSeqMaxWgs ? static_cast<int>(work) : kSeqMaxWgs;
+  st(k_seq_compact, dim3(wgs), dim3(kSeqThreads), 0, stream, g, a, x, max_moves, lanes);
   return st.err;
 }
 

@@ -56,26 +56,45 @@ bool good_stride(int64_t stride, int64_t row, int64_t eb) {
   return stride >= row && stride <= (int64_t{1} << 40) && stride * eb % 16 == 0;
 }
 
-// Workgroups of a decode call: three on each of 256 CUs, and no more than there can be units.
-constexpr int64_t kDecodeMaxWgs = 768;
+// Workgroups of a decode call, one on each of 256 CUs: its 64 KB in flight keep the memory busy,
+// and fewer shares have less to join (one sequence of 100,000 tokens, 8 key heads, 71.4 us against
+// 73.2 with two, three 89; 16 x 8,000 tokens, 16 heads of 64, 85.7 / 89.9).  Where there are more
+// items than CUs, segments change often, and two hide each other's changes (48 ragged sequences,
+// 8 key heads, 112.8 / 109.7).
+constexpr int64_t kDecodeWgs = 256, kDecodeManyWgs = 512;
 
-omnimem_status_t plan_decode(const omnimem_seq_cache_t* sc, const SeqGeom& g, int32_t num_q_heads, DecodePlan& p) {
+// A workgroup to an item, and no join, while an item is short at its longest: one sequence of 500
+// tokens (18 units), 8 key heads, 7.7 us against 9.1, 64 of them 22.8 / 25.6, one of 1,000 tokens
+// 16.1 / 9.8.  With two items for each CU, up to twice as long: 64 x 1,000 tokens 42 / 45 us.
+constexpr int64_t kDirectUnits = 20, kDirectItems = 512;
+
+omnimem_status_t plan_decode(const omnimem_seq_cache_t* sc, const SeqGeom& g, int32_t num_q_heads, int32_t window,
+                             DecodePlan& p) {
   if (num_q_heads < 1 || num_q_heads % sc->num_heads != 0) return OMNIMEM_EINVAL;
   p.G = num_q_heads / sc->num_heads;
   p.tile_rows = p.G <= kDecodeHeadRows ? kDecodeHeadRows : 2 * kDecodeHeadRows;
   p.head_tiles = (p.G + p.tile_rows - 1) / p.tile_rows;
   p.rows = p.G < p.tile_rows ? p.G : p.tile_rows;
   const int64_t items = static_cast<int64_t>(g.N) * sc->num_heads * p.head_tiles;
-  const int64_t units = static_cast<int64_t>(g.M) * (g.B / kUnitTokens);  // of an item, at most
+  // blocks and units of an item, at most
+  const int64_t blocks = window > 0 && window / g.B + 2 < g.M && g.Bpc == 1 ? window / g.B + 2 : g.M;
+  const int64_t unit = sc->dtype == OMNIMEM_BF16 && sc->head_dim == 64 ? 64 : 32;
+  const int64_t units = blocks * (g.B / unit);
   // a sum of the sequences' units in 31 bits, positions on the line in 40
-  if (items > 0x7fffffff / 256 || static_cast<int64_t>(g.N) * units > 0x7fffffff || (items > 0 && units > (int64_t{1} << 40) / items)) return OMNIMEM_EINVAL;
+  if (items > 0x7fffffff / 256 || static_cast<int64_t>(g.N) * g.M * (g.B / unit) > 0x7fffffff ||
+      (items > 0 && units > (int64_t{1} << 40) / items))
+    return OMNIMEM_EINVAL;
+  p.direct = units <= kDirectUnits || (items >= kDirectItems && units <= 2 * kDirectUnits);
   const int64_t most = items * units;
-  p.wgs = static_cast<int>(most < kDecodeMaxWgs ? most : kDecodeMaxWgs);
+  const int64_t wgs = items > kDecodeWgs ? kDecodeManyWgs : kDecodeWgs;
+  p.wgs = static_cast<int>(p.direct ? items : most < wgs ? most : wgs);
+  p.join_rows = items * 16 <= p.wgs ? 1 : p.rows >= 4 ? 4 : p.rows >= 2 ? 2 : 1;
   p.slot_floats = static_cast<size_t>(p.rows) * (sc->head_dim + 2);
   p.slot_floats = (p.slot_floats + 3) / 4 * 4;
   p.off_part = 0;
-  p.off_starts = align256(static_cast<size_t>(p.wgs) * 2 * p.slot_floats * sizeof(float));
-  p.total = p.off_starts + align256(static_cast<size_t>(p.wgs) * sizeof(DecodeStart)) + 256;
+  const size_t shares = p.direct ? 0 : p.wgs;
+  p.off_starts = align256(shares * 2 * p.slot_floats * sizeof(float));
+  p.total = p.off_starts + align256(shares * sizeof(DecodeStart)) + 256;
   return OMNIMEM_OK;
 }
 
@@ -88,11 +107,12 @@ omnimem_status_t plan_seq(const SeqGeom& g, int32_t num_new, SeqPlan& p) {
   if (num_new < 0 || static_cast<int64_t>(num_new) * g.M > 0x7fffffff || static_cast<int64_t>(g.N) * g.M > 0x7fffffff)
     return OMNIMEM_EINVAL;  // entries, and the pages that rows ask for, are counted in 31 bits
   p.words = (g.num_pages + 31) / 32;
-  p.off_used = 0;
-  p.off_held = p.off_used + align256(static_cast<size_t>(p.words) * 4);
-  p.off_first = p.off_held + (num_new > 0 ? align256(static_cast<size_t>(p.words) * 4) : 0);
+  const size_t map = align256(static_cast<size_t>(p.words) * 4);
+  p.off_held = 0;
+  p.off_tail = map;
+  p.off_first = p.off_tail + (num_new > 0 ? map : 0);
   p.off_rows = p.off_first + (num_new > 0 ? align256(static_cast<size_t>(g.num_pages) * 4) : 0);
-  p.total = p.off_rows + align256(static_cast<size_t>(num_new) * 16) + 256;
+  p.total = p.off_rows + align256(static_cast<size_t>(num_new) * sizeof(RowPlan)) + 256;
   return OMNIMEM_OK;
 }
 
@@ -101,7 +121,7 @@ omnimem_status_t plan_seq(const SeqGeom& g, int32_t num_new, SeqPlan& p) {
 size_t decode_workspace_bytes(const omnimem_seq_cache_t* sc, int32_t num_q_heads) {
   SeqGeom g;
   DecodePlan p;
-  if (resolve_seq_cache(sc, g, true) != OMNIMEM_OK || plan_decode(sc, g, num_q_heads, p) != OMNIMEM_OK) return 0;
+  if (resolve_seq_cache(sc, g, true) != OMNIMEM_OK || plan_decode(sc, g, num_q_heads, 0, p) != OMNIMEM_OK) return 0;
   return p.total;
 }
 
@@ -116,7 +136,7 @@ omnimem_status_t check_decode_attn(const omnimem_seq_cache_t* sc, const void* q,
                                    int32_t window, float scale, void* out, float* lse, const void* workspace,
                                    size_t workspace_bytes, SeqGeom& g, DecodePlan& p, DecodeLaunch& a) {
   omnimem_status_t st = resolve_seq_cache(sc, g, false);
-  if (st == OMNIMEM_OK) st = plan_decode(sc, g, num_q_heads, p);
+  if (st == OMNIMEM_OK) st = plan_decode(sc, g, num_q_heads, window, p);
   if (st != OMNIMEM_OK) return st;
   if (window < 0 || !isfinite(scale) || !(scale > 0.f)) return OMNIMEM_EINVAL;
   if (!good_stride(q_stride, static_cast<int64_t>(num_q_heads) * sc->head_dim, elem_bytes(sc->dtype)))

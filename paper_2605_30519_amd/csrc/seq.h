@@ -22,8 +22,8 @@ struct SeqGeom {
 
 // ---------------------------------------------------------------- decode
 // The (sequence, key/value head, tile of query heads) items of a call, each of them its
-// sequence's 64-token units, form one line of units, which `wgs` workgroups share evenly.
-constexpr int kUnitTokens = 64;
+// sequence's units of 32 tokens (64 for bf16 heads of 64) in turn, form one line, which `wgs`
+// workgroups share evenly; or, where sequences are short, an item is a workgroup's (direct).
 constexpr int kDecodeWaves = 4;
 constexpr int kDecodeHeadRows = 16;  // query heads of an MFMA tile
 
@@ -33,6 +33,8 @@ struct DecodePlan {
   int tile_rows;     // query heads of a tile: 16 or 32
   int rows;          // of them in use, min(G, tile_rows)
   int wgs;           // workgroups
+  bool direct;
+  int join_rows;     // query heads of a workgroup that joins shares
   size_t off_part, off_starts, total;
   size_t slot_floats;  // one workgroup's partial result of one item: O [rows][d], max [rows], sum [rows]
 };
@@ -86,7 +88,17 @@ struct CopyLaunch {
 // lowest growing row of a page) and the new rows' records.
 struct SeqPlan {
   int64_t words;  // 32-page words of a bitmap
-  size_t off_used, off_held, off_first, off_rows, total;
+  size_t off_held, off_tail, off_first, off_rows, total;
+};
+
+struct RowPlan {   // of a new row
+  int parent;
+  int kept;         // blocks it takes over
+  int added;        // blocks it gets
+  int tail_page;    // page of the begun block that it will write to, or -1
+  int len, short_len;  // tokens with its growth and without
+  int over;         // its growth would pass the capacity
+  int unused;
 };
 
 struct SeqUpdateLaunch {
