@@ -12,7 +12,6 @@ the host-side helpers.
 from __future__ import annotations
 
 import ctypes
-import functools
 import math
 import os
 import threading
@@ -777,34 +776,35 @@ def omnimem_gated_combine(o_cmp: Optional[torch.Tensor], o_slc: Optional[torch.T
 
 # ----------------------------------------------------------- sequence cache
 
-def _on_stream(fn):
-    """Runs fn with the GPU of its first argument as the current device and `stream` (a
-    torch stream or a raw handle; None: that GPU's current stream) as its current stream, so
-    that buffers made inside belong to the stream the kernels run on."""
-    @functools.wraps(fn)
-    def call(first, *args, stream=None, **kw):
-        t = first.k_pages if isinstance(first, SeqKVCache) else first
-        if not (isinstance(t, torch.Tensor) and t.is_cuda):
-            return fn(first, *args, **kw)     # refused there
-        if stream is None:
-            if t.get_device() == torch.cuda.current_device():
-                return fn(first, *args, **kw)
-            with torch.cuda.device(t.device):
-                return fn(first, *args, **kw)
-        if not isinstance(stream, torch.cuda.Stream):
-            handle = int(stream)
-            stream = torch.cuda.ExternalStream(handle, device=t.device) if handle else torch.cuda.default_stream(t.device)
-        _need(stream.device == t.device, f"stream must belong to {t.device}, not {stream.device}")
-        with torch.cuda.stream(stream):
-            return fn(first, *args, **kw)
-    return call
+try:
+    _current_device = torch._C._cuda_getDevice   # without building any Python object
+except AttributeError:
+    _current_device = torch.cuda.current_device
+
+
+def _elsewhere(like: torch.Tensor, stream):
+    """The context for work of a call on another GPU than the current one, or on `stream` (a torch
+    stream or a raw handle): there that GPU is the current device and that stream its
+    current stream, so that buffers made inside belong to the stream the kernels run on."""
+    if stream is None:
+        return torch.cuda.device(like.device)
+    if not isinstance(stream, torch.cuda.Stream):
+        handle = int(stream)
+        stream = (torch.cuda.ExternalStream(handle, device=like.device) if handle
+                  else torch.cuda.default_stream(like.device))
+    _need(stream.device == like.device, f"stream must belong to {like.device}, not {stream.device}")
+    return torch.cuda.stream(stream)
 
 
 def _seq_table(page_table, seq_lens, num_pages: int, block_size: int, chunk_tokens: int) -> omnimem_seq_table_t:
-    _need(isinstance(page_table, torch.Tensor) and page_table.dim() == 2, "page_table must be an [N, max_blocks] tensor")
+    # the common case, without building any message
+    if not (isinstance(page_table, torch.Tensor) and isinstance(seq_lens, torch.Tensor) and page_table.dim() == 2 and
+            page_table.dtype is torch.int32 and seq_lens.dtype is torch.int32 and page_table.is_contiguous() and
+            seq_lens.is_contiguous() and seq_lens.shape == page_table.shape[:1]):
+        _need(isinstance(page_table, torch.Tensor) and page_table.dim() == 2, "page_table must be an [N, max_blocks] tensor")
+        _check_tensor("page_table", page_table, page_table.shape, torch.int32)
+        _check_tensor("seq_lens", seq_lens, page_table.shape[:1], torch.int32)
     n, m = page_table.shape
-    _check_tensor("page_table", page_table, (n, m), torch.int32)
-    _check_tensor("seq_lens", seq_lens, (n,), torch.int32)
     return omnimem_seq_table_t(n, m, block_size, chunk_tokens or block_size, num_pages, page_table.data_ptr(),
                                seq_lens.data_ptr())
 
@@ -825,17 +825,20 @@ class SeqKVCache:
     chunk_tokens: int = 0
 
     def descriptor(self) -> omnimem_seq_cache_t:
-        kp, vp = self.k_pages, self.v_pages
-        shape, code = kp.shape, _DTYPES.get(kp.dtype)
-        if code is None or vp.dtype is not kp.dtype:
-            raise TypeError(f"unsupported page dtype {kp.dtype}")
+        kp, vp, pt, sl = self.k_pages, self.v_pages, self.page_table, self.seq_lens
+        dtype, shape = kp.dtype, kp.shape
+        code = _DTYPES.get(dtype)
+        if code is None or vp.dtype is not dtype:
+            raise TypeError(f"unsupported page dtype {dtype}")
         if len(shape) != 4 or vp.shape != shape:
             raise ValueError("k_pages and v_pages must share one [num_pages, H, B, d] shape")
         if not (kp.is_contiguous() and vp.is_contiguous()):
             raise ValueError("cache tensors must be contiguous")
         num_pages, H, B, d = shape
-        seqs = _seq_table(self.page_table, self.seq_lens, num_pages, B, self.chunk_tokens)
-        _on_gpu(kp, v_pages=vp, page_table=self.page_table, seq_lens=self.seq_lens)
+        seqs = _seq_table(pt, sl, num_pages, B, self.chunk_tokens)
+        dev = kp.get_device()
+        if dev < 0 or not vp.get_device() == dev == pt.get_device() == sl.get_device():
+            _on_gpu(kp, v_pages=vp, page_table=pt, seq_lens=sl)
         return omnimem_seq_cache_t(seqs, code, H, d, kp.data_ptr(), vp.data_ptr())
 
     def after(self, update: "SeqUpdate") -> "SeqKVCache":
@@ -858,110 +861,128 @@ class SeqUpdate:
     info: torch.Tensor        # [4] int32: copies, pages in use, pages short, rows over capacity
 
 
-def _row_stride(name: str, t: torch.Tensor, rows: int, heads: int, d: int) -> int:
-    """Elements from row to row of a [rows, heads, d] tensor whose rows are contiguous."""
+def _rows_stride(name: str, t, heads: Optional[int], like: torch.Tensor) -> int:
+    """Checks rows [n, H, d] of like's type and GPU, each row contiguous; elements from row to row."""
+    if not isinstance(t, torch.Tensor) or t.dim() != 3:
+        raise ValueError(f"{name} must be a [rows, H, d] tensor")
+    n, h, d = t.shape
+    want = like.shape[3]
+    if d != want or (heads is not None and h != heads):
+        raise ValueError(f"{name} must have shape {(n, heads or h, want)}, not {tuple(t.shape)}")
+    if t.dtype is not like.dtype:
+        raise ValueError(f"{name} must be {like.dtype}, not {t.dtype}")
+    if t.get_device() != like.get_device():
+        _on_gpu(like, **{name: t})
     if t.is_contiguous():
-        return heads * d
-    s = t.stride()
-    _need((s[2] == 1 or d == 1) and (s[1] == d or heads == 1), f"{name} must have contiguous [H, d] rows")
-    return s[0] if rows > 1 else heads * d
-
-
-def _rows_of(name: str, t, heads: Optional[int], d: int, dtype) -> int:
-    _need(isinstance(t, torch.Tensor) and t.dim() == 3, f"{name} must be a [rows, H, d] tensor")
-    n, h, e = t.shape
-    _need((heads is None or h == heads) and e == d, f"{name} must have shape {(n, heads or h, d)}, not {tuple(t.shape)}")
-    _need(t.dtype is dtype, f"{name} must be {dtype}, not {t.dtype}")
-    return n
+        return h * d
+    s0, s1, s2 = t.stride()
+    _need((s2 == 1 or d == 1) and (s1 == d or h == 1), f"{name} must have contiguous [H, d] rows")
+    return s0 if n > 1 else h * d
 
 
 def omnimem_decode_workspace_bytes(cache: SeqKVCache, num_q_heads: int) -> int:
     return int(lib().omnimem_decode_workspace_bytes(ctypes.byref(cache.descriptor()), int(num_q_heads)))
 
 
-@_on_stream
 def omnimem_decode_attn(cache: SeqKVCache, q: torch.Tensor, scale: Optional[float] = None, *, window: int = 0,
                         out: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None, want_lse: bool = True,
-                        workspace: Optional[torch.Tensor] = None):
+                        workspace: Optional[torch.Tensor] = None, stream=None):
     """Attention of one new token per sequence: q [N, Hq, d] (rows may be strided, as a slice of a
     fused projection is), Hq a multiple of the cache's heads.  window > 0: the last so many
-    tokens only.  Returns out [N, Hq, d] and lse [Hq, N].  Takes stream=."""
+    tokens only.  Returns out [N, Hq, d] and lse [Hq, N]."""
     kp = cache.k_pages
-    H, d = kp.shape[1], kp.shape[3]
-    n = _rows_of("q", q, None, d, kp.dtype)
-    hq = q.shape[1]
-    _need(hq >= 1 and hq % H == 0, f"q must have a multiple of {H} heads, not {hq}")
-    _need(n == cache.page_table.shape[0], f"q must have {cache.page_table.shape[0]} rows, not {n}")
-    stride = _row_stride("q", q, n, hq, d)
-    _check_outputs(q, out, lse)
-    desc = cache.descriptor()
-    _on_gpu(kp, q=q, out=out, lse=lse)
+    dev = kp.get_device()
+    if dev >= 0 and (stream is not None or dev != _current_device()):
+        with _elsewhere(kp, stream):
+            return omnimem_decode_attn(cache, q, scale, window=window, out=out, lse=lse, want_lse=want_lse,
+                                       workspace=workspace)
+    stride = _rows_stride("q", q, None, kp)
+    n, hq, d = q.shape
+    H = kp.shape[1]
+    _need(hq >= 1 and hq % H == 0, "q must have a multiple of the cache's heads")
+    _need(n == cache.page_table.shape[0], "q must have one row per sequence")
+    if out is not None or lse is not None:
+        _check_outputs(q, out, lse)
+    desc = ctypes.byref(cache.descriptor())
+    if out is not None or lse is not None:
+        _on_gpu(kp, out=out, lse=lse)
     L = lib()
-    need = L.omnimem_decode_workspace_bytes(ctypes.byref(desc), hq)
+    need = L.omnimem_decode_workspace_bytes(desc, hq)
     if workspace is None:
-        workspace = workspace_tensor(need, q.device)
+        workspace = torch.empty(need or 256, dtype=torch.uint8, device=q.device)
     else:
         _check_workspace(workspace, need, q)
     if out is None:
         out = torch.empty((n, hq, d), dtype=q.dtype, device=q.device)
     if lse is None and want_lse:
         lse = torch.empty((hq, n), dtype=torch.float32, device=q.device)
-    sc = 1.0 / math.sqrt(d) if scale is None else float(scale)
-    st = L.omnimem_decode_attn(ctypes.byref(desc), q.data_ptr(), stride, hq, int(window), sc, out.data_ptr(), _ptr(lse),
-                               workspace.data_ptr(), workspace.numel(), _current_raw_stream())
-    _check(st, "omnimem_decode_attn")
+    st = L.omnimem_decode_attn(desc, q.data_ptr(), stride, hq, window, d ** -0.5 if scale is None else scale,
+                               out.data_ptr(), _ptr(lse), workspace.data_ptr(), workspace.numel(), _current_raw_stream())
+    if st != 0:
+        _check(st, "omnimem_decode_attn")
     return out, lse
 
 
-@_on_stream
-def omnimem_append_kv(cache: SeqKVCache, k: torch.Tensor, v: torch.Tensor, starts: Optional[torch.Tensor] = None) -> None:
+def omnimem_append_kv(cache: SeqKVCache, k: torch.Tensor, v: torch.Tensor, starts: Optional[torch.Tensor] = None, *,
+                      stream=None) -> None:
     """Writes new tokens into their sequences' pages: rows starts[i] to starts[i + 1] of k and v
     [T, H, d] (rows may be strided) are the last tokens of sequence i, which cache.seq_lens
-    already counts; starts [N + 1] int32, None: one token per sequence.  Takes stream=."""
+    already counts; starts [N + 1] int32, None: one token per sequence."""
     kp = cache.k_pages
-    _, H, _, d = kp.shape
-    n = _rows_of("k", k, H, d, kp.dtype)
-    _need(_rows_of("v", v, H, d, kp.dtype) == n, "k and v must have as many rows")
-    ks, vs = _row_stride("k", k, n, H, d), _row_stride("v", v, n, H, d)
-    seqs = cache.page_table.shape[0]
+    dev = kp.get_device()
+    if dev >= 0 and (stream is not None or dev != _current_device()):
+        with _elsewhere(kp, stream):
+            return omnimem_append_kv(cache, k, v, starts)
+    H, seqs = kp.shape[1], cache.page_table.shape[0]
+    ks, vs = _rows_stride("k", k, H, kp), _rows_stride("v", v, H, kp)
+    n = k.shape[0]
+    _need(v.shape[0] == n, "k and v must have as many rows")
     if starts is None:
-        _need(n == seqs, f"k and v must have {seqs} rows (one per sequence) without starts")
+        _need(n == seqs, "k and v must have one row per sequence without starts")
     else:
         _check_tensor("starts", starts, (seqs + 1,), torch.int32)
     desc = cache.descriptor()
-    _on_gpu(kp, k=k, v=v, starts=starts)
-    _check(lib().omnimem_append_kv(ctypes.byref(desc), k.data_ptr(), ks, v.data_ptr(), vs, n, _ptr(starts),
-                                   _current_raw_stream()), "omnimem_append_kv")
+    if starts is not None and starts.get_device() != dev:
+        _on_gpu(kp, starts=starts)
+    st = lib().omnimem_append_kv(ctypes.byref(desc), k.data_ptr(), ks, v.data_ptr(), vs, n, _ptr(starts),
+                                 _current_raw_stream())
+    if st != 0:
+        _check(st, "omnimem_append_kv")
 
 
-@_on_stream
 def omnimem_copy_pages(k_pages: torch.Tensor, v_pages: Optional[torch.Tensor], pairs: torch.Tensor,
-                       count: Optional[torch.Tensor] = None) -> None:
+                       count: Optional[torch.Tensor] = None, *, stream=None) -> None:
     """Copies page pairs[i][0] to page pairs[i][1] for the first count[0] pairs [n, 2] int32 (None:
     all), in pools [num_pages, H, B, d] or, for several layers in one call, [layers, num_pages,
-    H, B, d].  count: int32 tensor (SeqUpdate.info serves).  Takes stream=."""
-    dims = k_pages.dim()
-    _need(dims in (4, 5), "k_pages must be [num_pages, H, B, d] or [layers, num_pages, H, B, d]")
-    layers = k_pages.shape[0] if dims == 5 else 1
-    pages = k_pages.shape[-4]
-    step = k_pages.stride(0) if dims == 5 and layers > 1 else 0
+    H, B, d].  count: int32 tensor (SeqUpdate.info serves)."""
+    dev = k_pages.get_device()
+    if dev >= 0 and (stream is not None or dev != _current_device()):
+        with _elsewhere(k_pages, stream):
+            return omnimem_copy_pages(k_pages, v_pages, pairs, count)
+    shape = k_pages.shape
+    _need(len(shape) in (4, 5), "k_pages must be [num_pages, H, B, d] or [layers, num_pages, H, B, d]")
+    layers, step = (1, 0) if len(shape) == 4 else (shape[0], k_pages.stride(0))
     for name, t in (("k_pages", k_pages), ("v_pages", v_pages)):
         if t is None:
             continue
-        _need(t.shape == k_pages.shape and t.dtype is k_pages.dtype, f"{name} must match k_pages in shape and dtype")
-        _need((t[0] if dims == 5 and layers > 0 else t).is_contiguous() and (step == 0 or t.stride(0) == step),
-              f"{name} must be contiguous")
+        _need(t.shape == shape and t.dtype is k_pages.dtype, "v_pages must match k_pages in shape and dtype")
+        if not t.is_contiguous():   # layers may lie apart
+            _need(len(shape) == 5 and layers > 0 and t[0].is_contiguous(), f"{name} must be contiguous")
+        _need(layers <= 1 or t.stride(0) == step, "v_pages must have k_pages' distance between layers")
     _need(isinstance(pairs, torch.Tensor) and pairs.dim() == 2, "pairs must be an [n, 2] tensor")
-    _check_tensor("pairs", pairs, (pairs.shape[0], 2), torch.int32)
+    n = pairs.shape[0]
+    _check_tensor("pairs", pairs, (n, 2), torch.int32)
     if count is not None:
         _need(isinstance(count, torch.Tensor) and count.dtype is torch.int32 and count.numel() >= 1 and
               count.is_contiguous(), "count must be an int32 tensor")
     eb = k_pages.element_size()
-    page_bytes = k_pages.shape[-3] * k_pages.shape[-2] * k_pages.shape[-1] * eb
-    _on_gpu(k_pages, "k_pages", v_pages=v_pages, pairs=pairs, count=count)
-    _check(lib().omnimem_copy_pages(k_pages.data_ptr(), _ptr(v_pages), pages, page_bytes, layers, step * eb,
-                                    pairs.data_ptr(), _ptr(count), pairs.shape[0], _current_raw_stream()),
-           "omnimem_copy_pages")
+    if dev < 0 or pairs.get_device() != dev or v_pages is not None or count is not None:
+        _on_gpu(k_pages, "k_pages", v_pages=v_pages, pairs=pairs, count=count)
+    st = lib().omnimem_copy_pages(k_pages.data_ptr(), _ptr(v_pages), shape[-4], shape[-3] * shape[-2] * shape[-1] * eb,
+                                  layers, step * eb if layers > 1 else 0, pairs.data_ptr(), _ptr(count), n,
+                                  _current_raw_stream())
+    if st != 0:
+        _check(st, "omnimem_copy_pages")
 
 
 def omnimem_seq_workspace_bytes(page_table: torch.Tensor, seq_lens: torch.Tensor, num_pages: int, block_size: int,
@@ -971,11 +992,12 @@ def omnimem_seq_workspace_bytes(page_table: torch.Tensor, seq_lens: torch.Tensor
 
 
 def _seq_out(out: Optional[SeqUpdate], n: int, m: int, pairs: int, lens, dev) -> SeqUpdate:
+    """The caller's buffers, checked, or new ones, cut from one allocation (lens: given)."""
     if out is None:
-        return SeqUpdate(torch.empty((n, m), dtype=torch.int32, device=dev),
-                         torch.empty(n, dtype=torch.int32, device=dev) if lens is None else lens,
-                         torch.empty((pairs, 2), dtype=torch.int32, device=dev),
-                         torch.empty(4, dtype=torch.int32, device=dev))
+        own = n if lens is None else 0
+        table, l, copies, info = torch.empty(n * m + own + 2 * pairs + 4, dtype=torch.int32, device=dev).split(
+            [n * m, own, 2 * pairs, 4])
+        return SeqUpdate(table.view(n, m), l if lens is None else lens, copies.view(pairs, 2), info)
     _check_tensor("out.page_table", out.page_table, (n, m), torch.int32)
     _check_tensor("out.seq_lens", out.seq_lens, (n,), torch.int32)
     _check_tensor("out.copies", out.copies, (pairs, 2), torch.int32)
@@ -983,61 +1005,75 @@ def _seq_out(out: Optional[SeqUpdate], n: int, m: int, pairs: int, lens, dev) ->
     return out
 
 
-@_on_stream
 def omnimem_seq_update(page_table: torch.Tensor, seq_lens: torch.Tensor, num_pages: int, block_size: int,
                        parent: torch.Tensor, keep: Optional[torch.Tensor] = None, grow: Optional[torch.Tensor] = None, *,
                        chunk_tokens: int = 0, out: Optional[SeqUpdate] = None,
-                       workspace: Optional[torch.Tensor] = None) -> SeqUpdate:
+                       workspace: Optional[torch.Tensor] = None, stream=None) -> SeqUpdate:
     """The next step's sequences: new row i is the first keep[i] tokens (None: all) of row
     parent[i] (-1: an empty sequence) and room for grow[i] more (None: none); rows that no parent
     names are freed.  The copies that rows with a shared page need before they are
     appended to are result.copies, for omnimem_copy_pages(..., result.copies, result.info) on
     every layer.  Where info[2] (pages short) or info[3] (rows over capacity) is not 0, no row
-    grew.  Takes stream=."""
-    desc = _seq_table(page_table, seq_lens, int(num_pages), int(block_size), int(chunk_tokens))
+    grew."""
+    dev = page_table.get_device() if isinstance(page_table, torch.Tensor) else -1
+    if dev >= 0 and (stream is not None or dev != _current_device()):
+        with _elsewhere(page_table, stream):
+            return omnimem_seq_update(page_table, seq_lens, num_pages, block_size, parent, keep, grow,
+                                      chunk_tokens=chunk_tokens, out=out, workspace=workspace)
+    desc = ctypes.byref(_seq_table(page_table, seq_lens, num_pages, block_size, chunk_tokens))
     _need(isinstance(parent, torch.Tensor) and parent.dim() == 1, "parent must be a 1-D tensor")
     n = parent.shape[0]
-    for name, t in (("parent", parent), ("keep", keep), ("grow", grow)):
-        if t is not None:
-            _check_tensor(name, t, (n,), torch.int32)
-    dev = page_table.device
-    made = _seq_out(out, n, page_table.shape[1], n, None, dev)
-    _on_gpu(page_table, "page_table", seq_lens=seq_lens, parent=parent, keep=keep, grow=grow, out_table=made.page_table,
-            out_lens=made.seq_lens, copies=made.copies, info=made.info)
+    _check_tensor("parent", parent, (n,), torch.int32)
+    if keep is not None:
+        _check_tensor("keep", keep, (n,), torch.int32)
+    if grow is not None:
+        _check_tensor("grow", grow, (n,), torch.int32)
+    _on_gpu(page_table, "page_table", seq_lens=seq_lens, parent=parent, keep=keep, grow=grow)
+    made = _seq_out(out, n, page_table.shape[1], n, None, page_table.device)
+    if out is not None:
+        _on_gpu(page_table, "page_table", out_table=made.page_table, out_lens=made.seq_lens, copies=made.copies,
+                info=made.info)
     L = lib()
-    need = L.omnimem_seq_workspace_bytes(ctypes.byref(desc), n)
+    need = L.omnimem_seq_workspace_bytes(desc, n)
     if workspace is None:
-        workspace = workspace_tensor(need, dev)
+        workspace = torch.empty(need or 256, dtype=torch.uint8, device=page_table.device)
     else:
         _check_workspace(workspace, need, page_table)
-    st = L.omnimem_seq_update(ctypes.byref(desc), n, _ptr(parent), _ptr(keep), _ptr(grow), _ptr(made.page_table),
-                              _ptr(made.seq_lens), _ptr(made.copies), _ptr(made.info), workspace.data_ptr(),
-                              workspace.numel(), _current_raw_stream())
-    _check(st, "omnimem_seq_update")
+    st = L.omnimem_seq_update(desc, n, _ptr(parent), _ptr(keep), _ptr(grow), _ptr(made.page_table), _ptr(made.seq_lens),
+                              _ptr(made.copies), _ptr(made.info), workspace.data_ptr(), workspace.numel(),
+                              _current_raw_stream())
+    if st != 0:
+        _check(st, "omnimem_seq_update")
     return made
 
 
-@_on_stream
 def omnimem_seq_compact(page_table: torch.Tensor, seq_lens: torch.Tensor, num_pages: int, block_size: int, *,
                         chunk_tokens: int = 0, out: Optional[SeqUpdate] = None,
-                        workspace: Optional[torch.Tensor] = None) -> SeqUpdate:
+                        workspace: Optional[torch.Tensor] = None, stream=None) -> SeqUpdate:
     """The tables with all pages in use moved to the front of the pool; the moves to make are
     result.copies, for omnimem_copy_pages(..., result.copies, result.info) on every layer, and
-    result.info[1] pages are in use.  The lengths stay (result.seq_lens is seq_lens).  Takes stream=."""
-    desc = _seq_table(page_table, seq_lens, int(num_pages), int(block_size), int(chunk_tokens))
-    dev = page_table.device
+    result.info[1] pages are in use.  The lengths stay (result.seq_lens is seq_lens)."""
+    dev = page_table.get_device() if isinstance(page_table, torch.Tensor) else -1
+    if dev >= 0 and (stream is not None or dev != _current_device()):
+        with _elsewhere(page_table, stream):
+            return omnimem_seq_compact(page_table, seq_lens, num_pages, block_size, chunk_tokens=chunk_tokens, out=out,
+                                       workspace=workspace)
+    desc = ctypes.byref(_seq_table(page_table, seq_lens, num_pages, block_size, chunk_tokens))
+    _on_gpu(page_table, "page_table", seq_lens=seq_lens)
     n, m = page_table.shape
-    made = _seq_out(out, n, m, max(1, int(num_pages) // 2), seq_lens, dev)
-    _on_gpu(page_table, "page_table", seq_lens=seq_lens, out_table=made.page_table, moves=made.copies, info=made.info)
+    made = _seq_out(out, n, m, max(1, num_pages // 2), seq_lens, page_table.device)
+    if out is not None:
+        _on_gpu(page_table, "page_table", out_table=made.page_table, moves=made.copies, info=made.info)
     L = lib()
-    need = L.omnimem_seq_workspace_bytes(ctypes.byref(desc), 0)
+    need = L.omnimem_seq_workspace_bytes(desc, 0)
     if workspace is None:
-        workspace = workspace_tensor(need, dev)
+        workspace = torch.empty(need or 256, dtype=torch.uint8, device=page_table.device)
     else:
         _check_workspace(workspace, need, page_table)
-    st = L.omnimem_seq_compact(ctypes.byref(desc), _ptr(made.page_table), _ptr(made.copies), _ptr(made.info),
-                               workspace.data_ptr(), workspace.numel(), _current_raw_stream())
-    _check(st, "omnimem_seq_compact")
+    st = L.omnimem_seq_compact(desc, _ptr(made.page_table), _ptr(made.copies), _ptr(made.info), workspace.data_ptr(),
+                               workspace.numel(), _current_raw_stream())
+    if st != 0:
+        _check(st, "omnimem_seq_compact")
     return made
 
 
