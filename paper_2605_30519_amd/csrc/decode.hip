@@ -7,7 +7,7 @@
 // into MFMA operand registers, the next tile's loads issued as soon as the registers of the
 // present one are read.  Four rollouts of 47 to 94 thousand tokens, 12 heads of 128, bf16
 // (1.66 GB): 247 us, 6.7 TB/s, with plain instead of nontemporal loads 283; 48 sequences of 100
-// to 16,000 tokens, 40 query heads over 8 (617 MB): 110 us, 5.6 TB/s.
+// to 16,000 tokens, 40 query heads over 8 (617 MB): 106 us, 5.8 TB/s.
 //
 // Split.  An item is a (sequence, key/value head, tile of up to 32 query heads); its units of
 // 32 tokens (64 for bf16 heads of 64) follow one another on a line of all items' units, and
@@ -28,6 +28,10 @@ namespace omnimem {
 namespace {
 
 constexpr int kThreads = kDecodeWaves * kWave;
+// What an item costs beside its units (its waves meet, its result is written), in units: lengths
+// on the line count it, so that a share of short items holds fewer units.  12 sequences of 1 to
+// 11,664 tokens, 40 fp32 heads of 64: 82 us without, 66 with one unit, 58 with three, 59 with six.
+constexpr int kItemUnits = 3;
 constexpr int kMinUnits = 4;      // units of a share: one for each wave
 constexpr float kLowest = -FLT_MAX;  // below every score: a row without keys keeps sum 0
 constexpr int kNontemporal = 2;   // cache policy of a buffer load: read once
@@ -310,7 +314,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_decode(const DecodeArgs A) {
     for (int s = first_seq; s < last_seq; ++s) {
       len = A.g.lens[s];
       const int u = span_of<UT>(A, len).units;
-      mine += u;
+      mine += u > 0 ? u + kItemUnits : 0;
       empty |= u == 0;
     }
     const int upto = scan_lanes(mine);
@@ -345,19 +349,24 @@ __global__ __launch_bounds__(kThreads, 2) void k_decode(const DecodeArgs A) {
     } else {
       for (;; ++g.seq) {
         g.sp = span_of<UT>(A, __builtin_amdgcn_readfirstlane(A.g.lens[g.seq]));
-        if (x - before < g.sp.units) break;
-        before += g.sp.units;
+        if (g.sp.units == 0) continue;
+        if (x - before < g.sp.units + kItemUnits) break;
+        before += g.sp.units + kItemUnits;
       }
     }
     const int64_t in = pos - static_cast<int64_t>(before) * HH;
-    g.head = in <= 0x7fffffff ? static_cast<int>(static_cast<uint32_t>(in) / static_cast<uint32_t>(g.sp.units))
-                              : static_cast<int>(in / g.sp.units);
-    g.unit = static_cast<int>(in - static_cast<int64_t>(g.head) * g.sp.units);
+    const int length = g.sp.units + kItemUnits;
+    g.head = in <= 0x7fffffff ? static_cast<int>(static_cast<uint32_t>(in) / static_cast<uint32_t>(length))
+                              : static_cast<int>(in / length);
+    const int at_unit = static_cast<int>(in - static_cast<int64_t>(g.head) * length) - kItemUnits;
+    g.unit = max(at_unit, 0);
+    left += min(at_unit, 0);
     if (tid == 0) {
       DecodeStart st{};
       if (g.unit > 0) st = DecodeStart{pos - g.unit, g.sp.units, g.seq, g.head, share};
       A.starts[blockIdx.x] = st;
     }
+    if (left <= 0) return;  // the share ends in front of the item's first unit
   }
   g.stop = min(g.sp.units, g.unit + left);
   left -= g.stop - g.unit;
@@ -426,7 +435,8 @@ __global__ __launch_bounds__(kThreads, 2) void k_decode(const DecodeArgs A) {
   };
   // the stream's next segment; false behind the share's last one
   auto next_segment = [&]() -> bool {
-    if (DIRECT || left == 0) return false;
+    left -= kItemUnits;
+    if (DIRECT || left <= 0) return false;
     f.unit = 0;
     if (++f.head == HH) {
       f.head = 0;
@@ -598,7 +608,7 @@ __global__ __launch_bounds__(256) void k_decode_join(const DecodeArgs A) {
   const int r = blockIdx.y * ROWS + own, hq = h * A.G + tile * A.tile_rows + r;
   const bool real = r < min(A.tile_rows, A.G - tile * A.tile_rows);
   // the item's first share is its workgroup's first segment, or its last one
-  const int tail = static_cast<int64_t>(w0) * st.share < st.first ? 1 : 0;
+  const int tail = static_cast<int64_t>(w0) * st.share < st.first - kItemUnits ? 1 : 0;
   float m = kLowest, total = 0.f;
   f32x4 o{};
   if (real) {

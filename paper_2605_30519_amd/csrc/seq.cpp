@@ -64,9 +64,10 @@ bool good_stride(int64_t stride, int64_t row, int64_t eb) {
 constexpr int64_t kDecodeWgs = 256, kDecodeManyWgs = 512;
 
 // A workgroup to an item, and no join, while an item is short at its longest: one sequence of 500
-// tokens (18 units), 8 key heads, 7.7 us against 9.1, 64 of them 22.8 / 25.6, one of 1,000 tokens
-// 16.1 / 9.8.  With two items for each CU, up to twice as long: 64 x 1,000 tokens 42 / 45 us.
-constexpr int64_t kDirectUnits = 20, kDirectItems = 512;
+// tokens (18 units), 8 key heads, 7.7 us against 9.1, 64 of them 22.8 / 25.6; one of 1,000 tokens
+// 16.1 / 9.8.  (Many items of 1,000 tokens gain 6% so, and lose as much if they are ragged.)
+constexpr int64_t kDirectUnits = 20;
+constexpr int64_t kItemOverhead = 64;  // of an item's length on the line, no less than the kernel adds
 
 omnimem_status_t plan_decode(const omnimem_seq_cache_t* sc, const SeqGeom& g, int32_t num_q_heads, int32_t window,
                              DecodePlan& p) {
@@ -81,11 +82,11 @@ omnimem_status_t plan_decode(const omnimem_seq_cache_t* sc, const SeqGeom& g, in
   const int64_t unit = sc->dtype == OMNIMEM_BF16 && sc->head_dim == 64 ? 64 : 32;
   const int64_t units = blocks * (g.B / unit);
   // a sum of the sequences' units in 31 bits, positions on the line in 40
-  if (items > 0x7fffffff / 256 || static_cast<int64_t>(g.N) * g.M * (g.B / unit) > 0x7fffffff ||
+  if (items > 0x7fffffff / 256 || static_cast<int64_t>(g.N) * (static_cast<int64_t>(g.M) * (g.B / unit) + kItemOverhead) > 0x7fffffff ||
       (items > 0 && units > (int64_t{1} << 40) / items))
     return OMNIMEM_EINVAL;
-  p.direct = units <= kDirectUnits || (items >= kDirectItems && units <= 2 * kDirectUnits);
-  const int64_t most = items * units;
+  p.direct = units <= kDirectUnits;
+  const int64_t most = items * (units + kItemOverhead);
   const int64_t wgs = items > kDecodeWgs ? kDecodeManyWgs : kDecodeWgs;
   p.wgs = static_cast<int>(p.direct ? items : most < wgs ? most : wgs);
   p.join_rows = items * 16 <= p.wgs ? 1 : p.rows >= 4 ? 4 : p.rows >= 2 ? 2 : 1;
