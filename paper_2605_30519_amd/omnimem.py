@@ -782,6 +782,9 @@ except AttributeError:
     _current_device = torch.cuda.current_device
 
 
+_I32_MAX = 2 ** 31 - 1
+
+
 def _elsewhere(like: torch.Tensor, stream):
     """The context for work of a call on another GPU than the current one, or on `stream` (a torch
     stream or a raw handle): there that GPU is the current device and that stream its
@@ -797,16 +800,19 @@ def _elsewhere(like: torch.Tensor, stream):
 
 
 def _seq_table(page_table, seq_lens, num_pages: int, block_size: int, chunk_tokens: int) -> omnimem_seq_table_t:
+    i32 = torch.int32
+    shape = page_table.shape if isinstance(page_table, torch.Tensor) else ()
     # the common case, without building any message
-    if not (isinstance(page_table, torch.Tensor) and isinstance(seq_lens, torch.Tensor) and page_table.dim() == 2 and
-            page_table.dtype is torch.int32 and seq_lens.dtype is torch.int32 and page_table.is_contiguous() and
-            seq_lens.is_contiguous() and seq_lens.shape == page_table.shape[:1]):
-        _need(isinstance(page_table, torch.Tensor) and page_table.dim() == 2, "page_table must be an [N, max_blocks] tensor")
-        _check_tensor("page_table", page_table, page_table.shape, torch.int32)
-        _check_tensor("seq_lens", seq_lens, page_table.shape[:1], torch.int32)
-    n, m = page_table.shape
-    return omnimem_seq_table_t(n, m, block_size, chunk_tokens or block_size, num_pages, page_table.data_ptr(),
-                               seq_lens.data_ptr())
+    if not (len(shape) == 2 and isinstance(seq_lens, torch.Tensor) and seq_lens.shape == (shape[0],) and
+            page_table.dtype is i32 and seq_lens.dtype is i32 and page_table.is_contiguous() and seq_lens.is_contiguous()):
+        _need(len(shape) == 2, "page_table must be an [N, max_blocks] tensor")
+        _check_tensor("page_table", page_table, shape, i32)
+        _check_tensor("seq_lens", seq_lens, shape[:1], i32)
+    n, m = shape
+    if not (n * m <= _I32_MAX and 0 <= chunk_tokens <= _I32_MAX and 0 <= block_size <= _I32_MAX):
+        raise ValueError("page_table, block_size or chunk_tokens out of range")   # 32-bit fields
+    return omnimem_seq_table_t(n, m, int(block_size), int(chunk_tokens or block_size), int(num_pages),
+                               page_table.data_ptr(), seq_lens.data_ptr())
 
 
 @dataclass
@@ -901,6 +907,7 @@ def omnimem_decode_attn(cache: SeqKVCache, q: torch.Tensor, scale: Optional[floa
     H = kp.shape[1]
     _need(hq >= 1 and hq % H == 0, "q must have a multiple of the cache's heads")
     _need(n == cache.page_table.shape[0], "q must have one row per sequence")
+    _need(0 <= window <= _I32_MAX, "window must be 0 (all tokens) to 2^31 - 1")
     if out is not None or lse is not None:
         _check_outputs(q, out, lse)
     desc = ctypes.byref(cache.descriptor())
@@ -913,10 +920,10 @@ def omnimem_decode_attn(cache: SeqKVCache, q: torch.Tensor, scale: Optional[floa
     else:
         _check_workspace(workspace, need, q)
     if out is None:
-        out = torch.empty((n, hq, d), dtype=q.dtype, device=q.device)
+        out = torch.empty_like(q, memory_format=torch.contiguous_format)
     if lse is None and want_lse:
         lse = torch.empty((hq, n), dtype=torch.float32, device=q.device)
-    st = L.omnimem_decode_attn(desc, q.data_ptr(), stride, hq, window, d ** -0.5 if scale is None else scale,
+    st = L.omnimem_decode_attn(desc, q.data_ptr(), stride, hq, int(window), d ** -0.5 if scale is None else float(scale),
                                out.data_ptr(), _ptr(lse), workspace.data_ptr(), workspace.numel(), _current_raw_stream())
     if st != 0:
         _check(st, "omnimem_decode_attn")
@@ -972,6 +979,7 @@ def omnimem_copy_pages(k_pages: torch.Tensor, v_pages: Optional[torch.Tensor], p
     _need(isinstance(pairs, torch.Tensor) and pairs.dim() == 2, "pairs must be an [n, 2] tensor")
     n = pairs.shape[0]
     _check_tensor("pairs", pairs, (n, 2), torch.int32)
+    _need(n <= _I32_MAX, "pairs must hold fewer than 2^31 pairs")
     if count is not None:
         _need(isinstance(count, torch.Tensor) and count.dtype is torch.int32 and count.numel() >= 1 and
               count.is_contiguous(), "count must be an int32 tensor")
@@ -1023,6 +1031,7 @@ def omnimem_seq_update(page_table: torch.Tensor, seq_lens: torch.Tensor, num_pag
     desc = ctypes.byref(_seq_table(page_table, seq_lens, num_pages, block_size, chunk_tokens))
     _need(isinstance(parent, torch.Tensor) and parent.dim() == 1, "parent must be a 1-D tensor")
     n = parent.shape[0]
+    _need(n <= _I32_MAX, "parent must have fewer than 2^31 rows")
     _check_tensor("parent", parent, (n,), torch.int32)
     if keep is not None:
         _check_tensor("keep", keep, (n,), torch.int32)
@@ -1061,7 +1070,7 @@ def omnimem_seq_compact(page_table: torch.Tensor, seq_lens: torch.Tensor, num_pa
     desc = ctypes.byref(_seq_table(page_table, seq_lens, num_pages, block_size, chunk_tokens))
     _on_gpu(page_table, "page_table", seq_lens=seq_lens)
     n, m = page_table.shape
-    made = _seq_out(out, n, m, max(1, num_pages // 2), seq_lens, page_table.device)
+    made = _seq_out(out, n, m, max(1, int(num_pages) // 2), seq_lens, page_table.device)
     if out is not None:
         _on_gpu(page_table, "page_table", out_table=made.page_table, moves=made.copies, info=made.info)
     L = lib()

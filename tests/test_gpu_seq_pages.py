@@ -107,6 +107,15 @@ def test_append_to_more_sequences_than_threads(dev):
     append_case(dev, F32, 1, 64, 64, 64, lens, [(i * 7) % (t + 1) for i, t in enumerate(lens)], 7)
 
 
+def test_append_leaves_rows_behind_the_last_start(dev):
+    cache = SeqKVCache(torch.zeros((4, 2, 64, 64), device=dev), torch.zeros((4, 2, 64, 64), device=dev),
+                       i32([[0, 1], [2, 3]], dev), i32([70, 3], dev))
+    k = torch.ones((50, 2, 64), device=dev)
+    omnimem_append_kv(cache, k, k, i32([2, 10, 12], dev))
+    assert int(cache.k_pages[..., 0].sum()) == 2 * (8 + 2)
+    assert cache.k_pages[0, :, 62:].eq(1).all() and cache.k_pages[1, :, :6].eq(1).all() and cache.k_pages[2, :, 1:3].eq(1).all()
+
+
 def test_append_nothing(dev):
     append_case(dev, BF16, 2, 64, 64, 64, [10, 0], [0, 0], 8)
     append_case(dev, BF16, 2, 64, 64, 64, [], [], 9)
@@ -229,6 +238,16 @@ def test_update_beam_step(dev):
     # a shorter fork of a full block still begins a copy
     u = update_and_check(dev, [[3, 1, -1]], [128], 9, 64, 0, [0, 0], [128, 70], [1, 1])
     assert u.copies.tolist()[0] == [1, 2] and u.page_table.tolist() == [[3, 1, 0], [3, 2, -1]]
+
+
+def test_update_with_a_page_twice_in_a_row(dev):
+    u = update_and_check(dev, [[3, 3, 5]], [150], 8, 64, 0, [0], None, [1])
+    assert u.copies.tolist() == [[-1, -1]]
+    u = update_and_check(dev, [[3, 5, 3]], [150], 8, 64, 0, [0, 0], [150, 140], [1, 64])
+    assert u.info.tolist() == [0, 2, 0, 1]                          # 204 tokens in a row of 192
+    u = update_and_check(dev, [[3, 5, 3]], [150], 8, 64, 0, [0, 0], [150, 140], [1, 52])
+    assert u.info.tolist() == [2, 4, 0, 0]                          # page 3 is a full block too
+    compact_and_check(dev, [[7, 6, 7], [6, 6, 6]], [150, 129], 8, 64, 0)
 
 
 def test_update_frees_and_takes_the_lowest_pages(dev):

@@ -1,0 +1,257 @@
+"""The sequence cache's refusals, on the CPU: the C ABI's statuses for bad arguments (nothing is
+launched), its workspace sizes, and the binding's checks of tensors, each with a ValueError
+that names the argument.  CPU tensors of the right shape are refused last."""
+import ctypes
+
+import pytest
+import torch
+
+from paper_2605_30519_amd import omnimem as om
+
+FAKE = 0x10000  # aligned, never dereferenced
+OK, EINVAL, EUNSUP, EWS = 0, -1, -2, -3
+BIG = 2 ** 31 - 1
+
+
+def abi():
+    """The library the C cases run against; the sanitizer test swaps in a host-only build."""
+    return om.lib()
+
+
+def table(**kw):
+    d = dict(num_seqs=3, max_blocks=10, block_size=64, chunk_tokens=64, num_pages=30, page_table=FAKE, seq_lens=FAKE)
+    d.update(kw)
+    return om.omnimem_seq_table_t(**d)
+
+
+def cache(dtype=0, num_heads=2, head_dim=64, k_pages=FAKE, v_pages=FAKE, **kw):
+    return om.omnimem_seq_cache_t(table(**kw), dtype, num_heads, head_dim, k_pages, v_pages)
+
+
+TABLE_CASES = [
+    (dict(num_seqs=-1), EINVAL), (dict(max_blocks=0), EINVAL), (dict(chunk_tokens=0), EINVAL),
+    (dict(block_size=32), EUNSUP), (dict(block_size=96), EUNSUP), (dict(num_pages=-1), EINVAL),
+    (dict(num_pages=2 ** 31), EINVAL), (dict(page_table=0), EINVAL), (dict(seq_lens=0), EINVAL),
+    (dict(page_table=FAKE + 2), EINVAL), (dict(seq_lens=FAKE + 1), EINVAL),
+    (dict(max_blocks=2 ** 25), EINVAL),                                   # 2^31 tokens
+    (dict(max_blocks=2 ** 24, block_size=128, chunk_tokens=128), EINVAL),
+]
+CACHE_CASES = [
+    (dict(dtype=2), EUNSUP), (dict(head_dim=96), EUNSUP), (dict(num_heads=0), EINVAL), (dict(num_heads=2 ** 20 + 1), EINVAL),
+    (dict(k_pages=0), EINVAL), (dict(v_pages=0), EINVAL), (dict(k_pages=FAKE + 8), EINVAL), (dict(v_pages=FAKE + 4), EINVAL),
+    (dict(num_pages=BIG, num_heads=2 ** 20, head_dim=128), EINVAL),      # a pool past 2^40 elements
+]
+
+
+def test_cache_arguments():
+    L = abi()
+    for kw, want in TABLE_CASES + CACHE_CASES:
+        c = cache(**kw)
+        assert L.omnimem_decode_attn(ctypes.byref(c), FAKE, 128, 2, 0, 0.1, FAKE, None, FAKE, 1 << 30, None) == want, kw
+        assert L.omnimem_append_kv(ctypes.byref(c), FAKE, 128, FAKE, 128, 3, None, None) == want, kw
+    for kw, want in TABLE_CASES:
+        t = table(**kw)
+        assert L.omnimem_seq_update(ctypes.byref(t), 3, FAKE, FAKE, FAKE, FAKE + 64, FAKE + 64, FAKE, FAKE, FAKE, 1 << 30,
+                                    None) == want, kw
+        assert L.omnimem_seq_compact(ctypes.byref(t), FAKE + 64, FAKE, FAKE, FAKE, 1 << 30, None) == want, kw
+    assert L.omnimem_decode_attn(None, FAKE, 128, 2, 0, 0.1, FAKE, None, FAKE, 1 << 30, None) == EINVAL
+    assert L.omnimem_append_kv(None, FAKE, 128, FAKE, 128, 3, None, None) == EINVAL
+    assert L.omnimem_seq_update(None, 0, None, None, None, None, None, None, FAKE, FAKE, 256, None) == EINVAL
+    assert L.omnimem_seq_compact(None, FAKE, FAKE, FAKE, FAKE, 256, None) == EINVAL
+
+
+def test_decode_arguments():
+    L = abi()
+    c = cache(max_blocks=1000)
+    need = L.omnimem_decode_workspace_bytes(ctypes.byref(c), 4)
+    assert need > 256 and need % 256 == 0
+
+    def call(q=FAKE, stride=256, heads=4, window=0, scale=0.1, out=FAKE, lse=FAKE, ws=FAKE, n=need, c=c):
+        return L.omnimem_decode_attn(ctypes.byref(c), q, stride, heads, window, scale, out, lse, ws, n, None)
+
+    for kw in (dict(q=0), dict(q=FAKE + 8), dict(out=0), dict(out=FAKE + 4), dict(lse=FAKE + 2), dict(heads=3),
+               dict(heads=0), dict(heads=-2), dict(stride=255), dict(stride=260), dict(stride=-256), dict(stride=2 ** 41),
+               dict(window=-1), dict(scale=0.0), dict(scale=-1.0), dict(scale=float("nan")), dict(scale=float("inf")),
+               dict(ws=0), dict(ws=FAKE + 16)):
+        assert call(**kw) == EINVAL, kw
+    assert call(n=need - 1) == EWS
+    assert L.omnimem_decode_attn(ctypes.byref(cache(num_seqs=0, page_table=0, seq_lens=0)), None, 256, 4, 0, 0.1, None, None,
+                                 None, 0, None) == OK
+    # sizes without buffers
+    bare = cache(max_blocks=1000, page_table=0, seq_lens=0, k_pages=0, v_pages=0)
+    assert L.omnimem_decode_workspace_bytes(ctypes.byref(bare), 4) == need
+    assert L.omnimem_decode_workspace_bytes(ctypes.byref(bare), 3) == 0
+    assert L.omnimem_decode_workspace_bytes(None, 4) == 0
+    # more units than positions are counted in
+    assert L.omnimem_decode_workspace_bytes(ctypes.byref(cache(num_seqs=BIG, max_blocks=2 ** 20)), 4) == 0
+    assert L.omnimem_decode_workspace_bytes(ctypes.byref(cache(num_seqs=BIG, max_blocks=1)), 4) == 0
+
+
+def test_append_arguments():
+    L = abi()
+    c = cache()
+
+    def call(k=FAKE, ks=128, v=FAKE, vs=128, tokens=3, starts=FAKE, c=c):
+        return L.omnimem_append_kv(ctypes.byref(c), k, ks, v, vs, tokens, starts, None)
+
+    for kw in (dict(k=0), dict(v=0), dict(k=FAKE + 8), dict(v=FAKE + 2), dict(ks=127), dict(vs=132), dict(ks=-128),
+               dict(tokens=-1), dict(starts=FAKE + 1), dict(starts=None, tokens=2), dict(vs=2 ** 41)):
+        assert call(**kw) == EINVAL, kw
+    assert call(tokens=0, k=0, v=0) == OK
+    assert call(c=cache(num_seqs=0, page_table=0, seq_lens=0)) == OK
+
+
+def test_copy_arguments():
+    L = abi()
+
+    def call(k=FAKE, v=FAKE, pages=10, nbytes=1024, layers=2, step=10240, pairs=FAKE, count=FAKE, most=4):
+        return L.omnimem_copy_pages(k, v, pages, nbytes, layers, step, pairs, count, most, None)
+
+    for kw in (dict(k=0), dict(k=FAKE + 8), dict(v=FAKE + 8), dict(pages=-1), dict(pages=2 ** 31), dict(nbytes=0),
+               dict(nbytes=1000), dict(layers=-1), dict(step=10224), dict(step=10241), dict(step=-16), dict(pairs=0),
+               dict(pairs=FAKE + 2), dict(count=FAKE + 1), dict(most=-1), dict(nbytes=2 ** 45), dict(pages=BIG, nbytes=2 ** 20)):
+        assert call(**kw) == EINVAL, kw
+    for kw in (dict(pages=0, k=0, v=0), dict(layers=0), dict(most=0, pairs=0)):
+        assert call(**kw) == OK, kw
+
+
+def test_update_and_compact_arguments():
+    L = abi()
+    t = table()
+    need = L.omnimem_seq_workspace_bytes(ctypes.byref(t), 5)
+    none = L.omnimem_seq_workspace_bytes(ctypes.byref(t), 0)
+    assert need > none >= 256 and need % 256 == 0
+
+    def update(n=5, parent=FAKE, keep=FAKE, grow=FAKE, rows=FAKE + 64, lens=FAKE + 64, copies=FAKE, info=FAKE, ws=FAKE,
+               size=need, t=t):
+        return L.omnimem_seq_update(ctypes.byref(t), n, parent, keep, grow, rows, lens, copies, info, ws, size, None)
+
+    for kw in (dict(n=-1), dict(parent=0), dict(rows=0), dict(lens=0), dict(copies=0), dict(info=0), dict(parent=FAKE + 1),
+               dict(keep=FAKE + 2), dict(grow=FAKE + 3), dict(info=FAKE + 2), dict(rows=FAKE), dict(lens=FAKE), dict(ws=0),
+               dict(ws=FAKE + 64), dict(n=BIG)):
+        assert update(**kw) == EINVAL, kw
+    assert update(size=need - 1) == EWS
+
+    def compact(rows=FAKE + 64, moves=FAKE, info=FAKE, ws=FAKE, size=none):
+        return L.omnimem_seq_compact(ctypes.byref(t), rows, moves, info, ws, size, None)
+
+    for kw in (dict(rows=0), dict(rows=FAKE), dict(moves=0), dict(info=0), dict(moves=FAKE + 2), dict(ws=0), dict(ws=FAKE + 8)):
+        assert compact(**kw) == EINVAL, kw
+    assert compact(size=none - 1) == EWS
+    assert L.omnimem_seq_workspace_bytes(None, 1) == 0
+    assert L.omnimem_seq_workspace_bytes(ctypes.byref(table(page_table=0, seq_lens=0)), 5) == need
+    assert L.omnimem_seq_workspace_bytes(ctypes.byref(t), -1) == 0
+
+
+# ------------------------------------------------------------------------- the binding
+
+H, D, B, N, M, P = 2, 64, 64, 3, 4, 12
+I32, BF16 = torch.int32, torch.bfloat16
+
+
+def seq_cache(dtype=BF16):
+    pages = torch.zeros((P, H, B, D), dtype=dtype)
+    return om.SeqKVCache(pages, pages.clone(), torch.zeros((N, M), dtype=I32), torch.zeros(N, dtype=I32))
+
+
+def rows(n=N, h=H, d=D, dtype=BF16):
+    return torch.zeros((n, h, d), dtype=dtype)
+
+
+def refused(match, fn, *args, error=ValueError, **kw):
+    with pytest.raises(error, match=match):
+        fn(*args, **kw)
+
+
+def test_binding_decode():
+    c = seq_cache()
+    f = om.omnimem_decode_attn
+    refused(r"q must be a \[rows, H, d\] tensor", f, c, rows()[0])
+    refused("q must have shape", f, c, rows(d=32))
+    refused("q must be torch.bfloat16", f, c, rows(dtype=torch.float32))
+    refused("q must have a multiple", f, c, rows(h=3))
+    refused("q must have one row per sequence", f, c, rows(n=4))
+    refused("q must have contiguous", f, c, torch.zeros((N, D, H), dtype=BF16).transpose(1, 2))
+    refused("out must have shape", f, c, rows(), out=rows(n=4))
+    refused("lse must have shape", f, c, rows(), lse=torch.zeros((N, H)))
+    refused("lse must be torch.float32", f, c, rows(), lse=torch.zeros((H, N), dtype=BF16))
+    refused("window must be", f, c, rows(), window=-1)
+    refused("window must be", f, c, rows(), window=2 ** 32)
+    refused("the cache must live on a GPU", f, c, rows())
+    refused("unsupported page dtype", f, seq_cache(torch.float16), rows(dtype=torch.float16), error=TypeError)
+
+
+def test_binding_cache():
+    f = om.omnimem_decode_attn
+    c = seq_cache()
+    c.v_pages = c.v_pages[:-1]
+    refused("share one", f, c, rows())
+    c = seq_cache()
+    c.k_pages = c.k_pages.transpose(0, 1).contiguous().transpose(0, 1)
+    refused("cache tensors must be contiguous", f, c, rows())
+    c = seq_cache()
+    c.page_table = c.page_table.long()
+    refused("page_table must be torch.int32", f, c, rows())
+    c = seq_cache()
+    c.page_table = torch.zeros((M, N), dtype=I32).t()
+    refused("page_table must be contiguous", f, c, rows())
+    c = seq_cache()
+    c.seq_lens = torch.zeros(N + 1, dtype=I32)
+    refused("seq_lens must have shape", f, c, rows())
+    c = seq_cache()
+    c.page_table = torch.zeros((N, M, 1), dtype=I32)
+    refused(r"page_table must be an \[N, max_blocks\] tensor", f, c, rows())
+    c = seq_cache()
+    c.chunk_tokens = 2 ** 32 + 64
+    refused("out of range", f, c, rows())
+    c = seq_cache()
+    refused("num_chunks exceeds", c.chunks, 0, M + 1)
+    h = c.chunks(1, M)
+    assert h.page_table.shape == (M, 1) and h.num_chunks == M and h.blocks_per_chunk == 1
+    c.chunk_tokens = 100
+    assert c.chunks(2, 2).page_table.shape == (2, 2) and c.chunks(0, 0).num_chunks == 0
+
+
+def test_binding_append():
+    c = seq_cache()
+    f = om.omnimem_append_kv
+    refused("k must have shape", f, c, rows(h=3), rows())
+    refused("v must be torch.bfloat16", f, c, rows(), rows(dtype=torch.float32))
+    refused("k and v must have as many rows", f, c, rows(n=5), rows(n=4), torch.zeros(N + 1, dtype=I32))
+    refused("one row per sequence", f, c, rows(n=5), rows(n=5))
+    refused("starts must have shape", f, c, rows(n=5), rows(n=5), torch.zeros(N, dtype=I32))
+    refused("starts must be torch.int32", f, c, rows(n=5), rows(n=5), torch.zeros(N + 1, dtype=torch.int64))
+    refused("k must have contiguous", f, c, torch.zeros((N, D, H), dtype=BF16).transpose(1, 2), rows())
+    refused("the cache must live on a GPU", f, c, rows(), rows())
+
+
+def test_binding_copy():
+    c = seq_cache()
+    f, k, v = om.omnimem_copy_pages, c.k_pages, c.v_pages
+    pairs = torch.zeros((2, 2), dtype=I32)
+    refused("k_pages must be", f, k[0], v[0], pairs)
+    refused("v_pages must match", f, k, v[:-1], pairs)
+    refused("v_pages must match", f, k, v.float(), pairs)
+    refused("k_pages must be contiguous", f, k[:, :1], v[:, :1], pairs)
+    refused("distance between layers", f, k.view(2, 6, H, B, D), torch.zeros((2, 2, 6, H, B, D), dtype=BF16)[:, 0], pairs)
+    refused(r"pairs must be an \[n, 2\] tensor", f, k, v, pairs[0])
+    refused("pairs must have shape", f, k, v, torch.zeros((2, 3), dtype=I32))
+    refused("pairs must be torch.int32", f, k, v, pairs.long())
+    refused("count must be an int32 tensor", f, k, v, pairs, torch.zeros(1, dtype=torch.int64))
+    refused("k_pages must live on a GPU", f, k, v, pairs)
+
+
+def test_binding_tables():
+    t, l = torch.zeros((N, M), dtype=I32), torch.zeros(N, dtype=I32)
+    parent = torch.zeros(5, dtype=I32)
+    f = om.omnimem_seq_update
+    refused("page_table must be an", f, l, l, P, B, parent)
+    refused("seq_lens must be torch.int32", f, t, l.long(), P, B, parent)
+    refused("parent must be a 1-D tensor", f, t, l, P, B, parent[None])
+    refused("parent must be torch.int32", f, t, l, P, B, parent.long())
+    refused("keep must have shape", f, t, l, P, B, parent, l)
+    refused("grow must be torch.int32", f, t, l, P, B, parent, parent, parent.float())
+    refused("page_table must live on a GPU", f, t, l, P, B, parent)
+    refused("page_table must live on a GPU", om.omnimem_seq_compact, t, l, P, B)
+    refused("seq_lens must have shape", om.omnimem_seq_compact, t, l[:-1], P, B)
+    refused("page_table must be an", om.omnimem_seq_compact, None, l, P, B)
