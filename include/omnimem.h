@@ -454,9 +454,9 @@ typedef struct {
   void* v_pages;
 } omnimem_seq_cache_t;
 
-/* Bytes of device workspace omnimem_decode_attn needs (0 on invalid arguments); the
-   table, the lengths and the pages may be NULL here. */
-size_t omnimem_decode_workspace_bytes(const omnimem_seq_cache_t* sc, int32_t num_q_heads);
+/* Bytes of device workspace omnimem_decode_attn needs (0 on invalid arguments; 256: none, and
+   its workspace may be NULL); the table, the lengths and the pages may be NULL here. */
+size_t omnimem_decode_workspace_bytes(const omnimem_seq_cache_t* sc, int32_t num_q_heads, int32_t window);
 
 /*
  * Attention of one new token per sequence: for every sequence i and query head h,
@@ -468,7 +468,7 @@ size_t omnimem_decode_workspace_bytes(const omnimem_seq_cache_t* sc, int32_t num
  * of these tokens do not matter, NaN included.
  * q:   [N][num_q_heads][d] of sc->dtype, row i at q + i*q_stride elements (a multiple of
  *      16 bytes, >= num_q_heads*d); num_q_heads is a multiple of H.
- * out: [N][num_q_heads][d] of sc->dtype (out).  lse: [num_q_heads][N] float (out, may be NULL).
+ * out: [N][num_q_heads][d] of sc->dtype (out), apart from q.  lse: [num_q_heads][N] float (out, may be NULL).
  * workspace: device scratch of at least omnimem_decode_workspace_bytes(), 256-byte
  * aligned; calls that can overlap need one each.  Nothing in it outlives the call.
  * The work is split over the sequences' real lengths, so the order of the sums, and the

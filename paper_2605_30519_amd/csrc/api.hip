@@ -182,8 +182,9 @@ OMNIMEM_API omnimem_status_t omnimem_union_gather_attn(const omnimem_kv_cache_t*
   return hip_status(omnimem::launch_union_gather(g, up, a, union_blocks, workspace, as_stream(stream)));
 }
 
-OMNIMEM_API size_t omnimem_decode_workspace_bytes(const omnimem_seq_cache_t* sc, int32_t num_q_heads) {
-  return omnimem::decode_workspace_bytes(sc, num_q_heads);
+OMNIMEM_API size_t omnimem_decode_workspace_bytes(const omnimem_seq_cache_t* sc, int32_t num_q_heads,
+                                                  int32_t window) {
+  return omnimem::decode_workspace_bytes(sc, num_q_heads, window);
 }
 
 OMNIMEM_API omnimem_status_t omnimem_decode_attn(const omnimem_seq_cache_t* sc, const void* q, int64_t q_stride,

@@ -27,11 +27,11 @@
 namespace omnimem {
 namespace {
 
-constexpr int kThreads = kDecodeWaves * kWave;
 // What an item costs beside its units (its waves meet, its result is written), in units: lengths
 // on the line count it, so that a share of short items holds fewer units.  12 sequences of 1 to
 // 11,664 tokens, 40 fp32 heads of 64: 82 us without, 66 with one unit, 58 with three, 59 with six.
 constexpr int kItemUnits = 3;
+constexpr int kThreads = kDecodeWaves * kWave;
 constexpr int kMinUnits = 4;      // units of a share: one for each wave
 constexpr float kLowest = -FLT_MAX;  // below every score: a row without keys keeps sum 0
 constexpr int kNontemporal = 2;   // cache policy of a buffer load: read once
@@ -279,6 +279,7 @@ __device__ __forceinline__ void lds_sync() {
   __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
 }
 
+// DIRECT: the workgroup's share is item blockIdx.x.
 template <typename T, int D, int NT, bool DIRECT>
 __global__ __launch_bounds__(kThreads, 2) void k_decode(const DecodeArgs A) {
   using L = Tile<T, D>;

@@ -367,7 +367,7 @@ __device__ __forceinline__ void write_rows(const SeqGeom& g, const SeqUpdateLaun
       a.info[2] = max(all[1] - room, 0);
       a.info[3] = all[3];
     }
-    for (int r = copied + tid; r < a.num_new; r += NT) {
+    for (int64_t r = copied + tid; r < a.num_new; r += NT) {
       a.pairs[2 * r] = -1;
       a.pairs[2 * r + 1] = -1;
     }
@@ -379,8 +379,9 @@ __device__ __forceinline__ void write_rows(const SeqGeom& g, const SeqUpdateLaun
     const int fresh = b - p.kept;  // of the row's added blocks; -1: the block that is copied
     if (done && (fresh >= 0 ? fresh < p.added : copy && fresh == -1)) {
       if (fresh < 0) {
-        a.pairs[2 * nth] = page;
-        a.pairs[2 * nth + 1] = pool.template select<true>(at);
+        int32_t* pair = a.pairs + 2 * static_cast<int64_t>(nth);
+        pair[0] = page;
+        pair[1] = pool.template select<true>(at);
       }
       page = pool.template select<true>(at + copy + fresh);
     }

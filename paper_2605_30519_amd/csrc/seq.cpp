@@ -65,7 +65,8 @@ constexpr int64_t kDecodeWgs = 256, kDecodeManyWgs = 512;
 
 // A workgroup to an item, and no join, while an item is short at its longest: one sequence of 500
 // tokens (18 units), 8 key heads, 7.7 us against 9.1, 64 of them 22.8 / 25.6; one of 1,000 tokens
-// 16.1 / 9.8.  (Many items of 1,000 tokens gain 6% so, and lose as much if they are ragged.)
+// 16.1 / 9.8 (16.5 with eight waves: a CU takes in no more).  Many items of 1,000 tokens gain 6%
+// so, and lose as much if they are ragged.
 constexpr int64_t kDirectUnits = 20;
 constexpr int64_t kItemOverhead = 64;  // of an item's length on the line, no less than the kernel adds
 
@@ -119,10 +120,12 @@ omnimem_status_t plan_seq(const SeqGeom& g, int32_t num_new, SeqPlan& p) {
 
 }  // namespace
 
-size_t decode_workspace_bytes(const omnimem_seq_cache_t* sc, int32_t num_q_heads) {
+size_t decode_workspace_bytes(const omnimem_seq_cache_t* sc, int32_t num_q_heads, int32_t window) {
   SeqGeom g;
   DecodePlan p;
-  if (resolve_seq_cache(sc, g, true) != OMNIMEM_OK || plan_decode(sc, g, num_q_heads, 0, p) != OMNIMEM_OK) return 0;
+  if (window < 0 || resolve_seq_cache(sc, g, true) != OMNIMEM_OK ||
+      plan_decode(sc, g, num_q_heads, window, p) != OMNIMEM_OK)
+    return 0;
   return p.total;
 }
 
@@ -156,7 +159,7 @@ omnimem_status_t check_decode_attn(const omnimem_seq_cache_t* sc, const void* q,
   a.scale = scale;
   a.out = out;
   a.lse = lse;
-  return check_scratch(workspace, workspace_bytes, p.total);
+  return p.direct ? OMNIMEM_OK : check_scratch(workspace, workspace_bytes, p.total);
 }
 
 omnimem_status_t check_append_kv(const omnimem_seq_cache_t* sc, const void* k, int64_t k_stride, const void* v,

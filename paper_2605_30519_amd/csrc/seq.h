@@ -112,7 +112,7 @@ struct SeqUpdateLaunch {
   int32_t* info;
 };
 
-size_t decode_workspace_bytes(const omnimem_seq_cache_t* sc, int32_t num_q_heads);
+size_t decode_workspace_bytes(const omnimem_seq_cache_t* sc, int32_t num_q_heads, int32_t window);
 size_t seq_workspace_bytes(const omnimem_seq_table_t* st, int32_t num_new);
 
 omnimem_status_t check_decode_attn(const omnimem_seq_cache_t* sc, const void* q, int64_t q_stride, int32_t num_q_heads,

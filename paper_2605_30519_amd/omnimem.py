@@ -219,7 +219,7 @@ def _configure(L, required: bool = True):
     L.omnimem_numa_bind.restype = i32
     scp = ctypes.POINTER(omnimem_seq_cache_t)
     stp = ctypes.POINTER(omnimem_seq_table_t)
-    L.omnimem_decode_workspace_bytes.argtypes = [scp, i32]
+    L.omnimem_decode_workspace_bytes.argtypes = [scp, i32, i32]
     L.omnimem_decode_workspace_bytes.restype = sz
     L.omnimem_decode_attn.argtypes = [scp, vp, i64, i32, i32, f32, vp, vp, vp, sz, vp]
     L.omnimem_decode_attn.restype = i32
@@ -886,8 +886,8 @@ def _rows_stride(name: str, t, heads: Optional[int], like: torch.Tensor) -> int:
     return s0 if n > 1 else h * d
 
 
-def omnimem_decode_workspace_bytes(cache: SeqKVCache, num_q_heads: int) -> int:
-    return int(lib().omnimem_decode_workspace_bytes(ctypes.byref(cache.descriptor()), int(num_q_heads)))
+def omnimem_decode_workspace_bytes(cache: SeqKVCache, num_q_heads: int, window: int = 0) -> int:
+    return int(lib().omnimem_decode_workspace_bytes(ctypes.byref(cache.descriptor()), int(num_q_heads), int(window)))
 
 
 def omnimem_decode_attn(cache: SeqKVCache, q: torch.Tensor, scale: Optional[float] = None, *, window: int = 0,
@@ -914,17 +914,18 @@ def omnimem_decode_attn(cache: SeqKVCache, q: torch.Tensor, scale: Optional[floa
     if out is not None or lse is not None:
         _on_gpu(kp, out=out, lse=lse)
     L = lib()
-    need = L.omnimem_decode_workspace_bytes(desc, hq)
-    if workspace is None:
-        workspace = torch.empty(need or 256, dtype=torch.uint8, device=q.device)
-    else:
+    window = int(window)
+    need = L.omnimem_decode_workspace_bytes(desc, hq, window)
+    if workspace is not None:
         _check_workspace(workspace, need, q)
+    elif need > 256:   # 256: the call needs none
+        workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
     if out is None:
         out = torch.empty_like(q, memory_format=torch.contiguous_format)
     if lse is None and want_lse:
         lse = torch.empty((hq, n), dtype=torch.float32, device=q.device)
-    st = L.omnimem_decode_attn(desc, q.data_ptr(), stride, hq, int(window), d ** -0.5 if scale is None else float(scale),
-                               out.data_ptr(), _ptr(lse), workspace.data_ptr(), workspace.numel(), _current_raw_stream())
+    st = L.omnimem_decode_attn(desc, q.data_ptr(), stride, hq, window, d ** -0.5 if scale is None else float(scale),
+                               out.data_ptr(), _ptr(lse), _ptr(workspace), need, _current_raw_stream())
     if st != 0:
         _check(st, "omnimem_decode_attn")
     return out, lse

@@ -10,8 +10,8 @@ using namespace omnimem;
 
 extern "C" {
 
-size_t omnimem_decode_workspace_bytes(const omnimem_seq_cache_t* sc, int32_t heads) {
-  return decode_workspace_bytes(sc, heads);
+size_t omnimem_decode_workspace_bytes(const omnimem_seq_cache_t* sc, int32_t heads, int32_t window) {
+  return decode_workspace_bytes(sc, heads, window);
 }
 size_t omnimem_seq_workspace_bytes(const omnimem_seq_table_t* st, int32_t n) { return seq_workspace_bytes(st, n); }
 

@@ -227,7 +227,7 @@ def test_agrees_with_dense_attention_of_one_row(dev):
 
 
 def test_a_short_workspace_is_refused(dev):
-    cache, g = build(dev, BF16, 2, 64, 64, 64, [100], 17)
+    cache, g = build(dev, BF16, 2, 64, 64, 64, [2000], 17)
     q = queries(dev, BF16, 1, 2, 64, g)
     ws = workspace_tensor(omnimem_decode_workspace_bytes(cache, 2), dev)
     with pytest.raises(ValueError, match="workspace holds"):

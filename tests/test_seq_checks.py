@@ -63,7 +63,7 @@ def test_cache_arguments():
 def test_decode_arguments():
     L = abi()
     c = cache(max_blocks=1000)
-    need = L.omnimem_decode_workspace_bytes(ctypes.byref(c), 4)
+    need = L.omnimem_decode_workspace_bytes(ctypes.byref(c), 4, 0)
     assert need > 256 and need % 256 == 0
 
     def call(q=FAKE, stride=256, heads=4, window=0, scale=0.1, out=FAKE, lse=FAKE, ws=FAKE, n=need, c=c):
@@ -79,12 +79,17 @@ def test_decode_arguments():
                                  None, 0, None) == OK
     # sizes without buffers
     bare = cache(max_blocks=1000, page_table=0, seq_lens=0, k_pages=0, v_pages=0)
-    assert L.omnimem_decode_workspace_bytes(ctypes.byref(bare), 4) == need
-    assert L.omnimem_decode_workspace_bytes(ctypes.byref(bare), 3) == 0
-    assert L.omnimem_decode_workspace_bytes(None, 4) == 0
+    assert L.omnimem_decode_workspace_bytes(ctypes.byref(bare), 4, 0) == need
+    assert L.omnimem_decode_workspace_bytes(ctypes.byref(bare), 3, 0) == 0
+    assert L.omnimem_decode_workspace_bytes(None, 4, 0) == 0
+    # a window needs no more than the whole row, a short row or window nothing at all
+    assert 256 < L.omnimem_decode_workspace_bytes(ctypes.byref(bare), 4, 20000) <= need
+    assert L.omnimem_decode_workspace_bytes(ctypes.byref(bare), 4, 1) == 256
+    assert L.omnimem_decode_workspace_bytes(ctypes.byref(cache()), 4, 0) == 256
+    assert L.omnimem_decode_workspace_bytes(ctypes.byref(bare), 4, -1) == 0
     # more units than positions are counted in
-    assert L.omnimem_decode_workspace_bytes(ctypes.byref(cache(num_seqs=BIG, max_blocks=2 ** 20)), 4) == 0
-    assert L.omnimem_decode_workspace_bytes(ctypes.byref(cache(num_seqs=BIG, max_blocks=1)), 4) == 0
+    assert L.omnimem_decode_workspace_bytes(ctypes.byref(cache(num_seqs=BIG, max_blocks=2 ** 20)), 4, 0) == 0
+    assert L.omnimem_decode_workspace_bytes(ctypes.byref(cache(num_seqs=BIG, max_blocks=1)), 4, 0) == 0
 
 
 def test_append_arguments():
