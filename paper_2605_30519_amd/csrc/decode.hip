@@ -348,7 +348,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_decode(const DecodeArgs A) {
     if (per == 1) {
       g.sp = span_of<UT>(A, __builtin_amdgcn_readlane(len, at));
     } else {
-      for (;; ++g.seq) {
+      for (; g.seq < N; ++g.seq) {
         g.sp = span_of<UT>(A, __builtin_amdgcn_readfirstlane(A.g.lens[g.seq]));
         if (g.sp.units == 0) continue;
         if (x - before < g.sp.units + kItemUnits) break;
@@ -441,8 +441,10 @@ __global__ __launch_bounds__(kThreads, 2) void k_decode(const DecodeArgs A) {
     f.unit = 0;
     if (++f.head == HH) {
       f.head = 0;
-      do f.sp = span_of<UT>(A, __builtin_amdgcn_readfirstlane(A.g.lens[++f.seq]));
-      while (f.sp.units == 0);
+      do {
+        if (++f.seq >= N) return false;
+        f.sp = span_of<UT>(A, __builtin_amdgcn_readfirstlane(A.g.lens[f.seq]));
+      } while (f.sp.units == 0);
     }
     f.stop = min(f.sp.units, left);
     left -= f.stop;
