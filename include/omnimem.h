@@ -509,7 +509,8 @@ omnimem_status_t omnimem_copy_pages(void* k_pages, void* v_pages, int64_t num_pa
                                     int32_t max_pairs, void* stream);
 
 /* Bytes of device workspace omnimem_seq_update (for num_new rows) and omnimem_seq_compact
-   (num_new = 0) need (0 on invalid arguments); the table and the lengths may be NULL here. */
+   (num_new = 0) need (0 on invalid arguments; 256: none, and the workspace may be NULL); the
+   table and the lengths may be NULL here. */
 size_t omnimem_seq_workspace_bytes(const omnimem_seq_table_t* st, int32_t num_new);
 
 /*

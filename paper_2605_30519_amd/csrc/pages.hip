@@ -486,14 +486,8 @@ __global__ __launch_bounds__(kSeqThreads) void k_seq_compact(const SeqGeom g, co
   write_compacted<kSeqThreads, false>(g, a, pool, scan, max_moves, lanes, nullptr);
 }
 
-// Small tables in one workgroup and one launch, all state in LDS: a word per page, INT_MAX free,
-// -1 named by a row that does not write to it, else the lowest row that does.  One launch costs
-// the host 6 us less than three; on the GPU, 16 rows of 18 entries take 7.1 us against 10.6
-// (update; compaction 5.2 / 8.6), 16 of 252 9.2 / 11.9 (9.3 / 13.3), 8 of 939 11.6 / 12.0 (13.4 / 11.5),
-// 256 of 65 27 / 14 (29 / 13): one CU's instruction rate.
-constexpr int kOneThreads = 1024, kOnePages = 16384, kOneRows = 1024;
-constexpr int64_t kOneEntries = 8192;
-
+// Small tables (p.one) in one workgroup and one launch, all state in LDS: a word per page, INT_MAX
+// free, -1 named by a row that does not write to it, else the lowest row that does.
 __device__ __forceinline__ void bitmap_of(const int* state, uint32_t* used, int pages) {
   for (int p = threadIdx.x; p < (pages + kWave - 1) / kWave * kWave; p += kOneThreads) {
     const uint64_t bits = __ballot(p < pages && state[p] != INT_MAX);
@@ -607,8 +601,7 @@ hipError_t launch_copy_pages(const CopyLaunch& a, hipStream_t stream) {
 
 hipError_t launch_seq_update(const SeqGeom& g, const SeqPlan& p, const SeqUpdateLaunch& a, void* workspace,
                              hipStream_t stream) {
-  if (g.num_pages <= kOnePages && a.num_new <= kOneRows && static_cast<int64_t>(a.num_new) * g.M <= kOneEntries)
-    return launch_kernel(k_seq_update_one, dim3(1), dim3(kOneThreads), 0, stream, g, a);
+  if (p.one) return launch_kernel(k_seq_update_one, dim3(1), dim3(kOneThreads), 0, stream, g, a);
   const SeqScratch x = scratch_of(p, workspace);
   LaunchStatus st;
   mark_used(g, p, a, x, a.num_new, stream, st);
@@ -620,8 +613,7 @@ hipError_t launch_seq_update(const SeqGeom& g, const SeqPlan& p, const SeqUpdate
 hipError_t launch_seq_compact(const SeqGeom& g, const SeqPlan& p, const SeqUpdateLaunch& a, void* workspace,
                               hipStream_t stream) {
   const int max_moves = g.num_pages >= 2 ? static_cast<int>(g.num_pages / 2) : 1;
-  if (g.num_pages <= kOnePages && g.N <= kOneRows && static_cast<int64_t>(g.N) * g.M <= kOneEntries)
-    return launch_kernel(k_seq_compact_one, dim3(1), dim3(kOneThreads), 0, stream, g, a, max_moves);
+  if (p.one) return launch_kernel(k_seq_compact_one, dim3(1), dim3(kOneThreads), 0, stream, g, a, max_moves);
   const SeqScratch x = scratch_of(p, workspace);
   LaunchStatus st;
   mark_used(g, p, a, x, g.N, stream, st);

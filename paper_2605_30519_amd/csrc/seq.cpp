@@ -94,9 +94,9 @@ omnimem_status_t plan_decode(const omnimem_seq_cache_t* sc, const SeqGeom& g, in
   p.slot_floats = static_cast<size_t>(p.rows) * (sc->head_dim + 2);
   p.slot_floats = (p.slot_floats + 3) / 4 * 4;
   p.off_part = 0;
-  const size_t shares = p.direct ? 0 : p.wgs;
+  const size_t shares = p.direct ? 0 : p.wgs;  // a direct call needs no scratch: 256
   p.off_starts = align256(shares * 2 * p.slot_floats * sizeof(float));
-  p.total = p.off_starts + align256(shares * sizeof(DecodeStart)) + 256;
+  p.total = p.direct ? 256 : p.off_starts + align256(shares * sizeof(DecodeStart)) + 512;
   return OMNIMEM_OK;
 }
 
@@ -105,16 +105,19 @@ omnimem_status_t check_scratch(const void* workspace, size_t have, size_t need) 
   return have < need ? OMNIMEM_EWORKSPACE : OMNIMEM_OK;
 }
 
+// num_new: rows of an update, or 0 for a compaction of the table's rows.
 omnimem_status_t plan_seq(const SeqGeom& g, int32_t num_new, SeqPlan& p) {
   if (num_new < 0 || static_cast<int64_t>(num_new) * g.M > 0x7fffffff || static_cast<int64_t>(g.N) * g.M > 0x7fffffff)
     return OMNIMEM_EINVAL;  // entries, and the pages that rows ask for, are counted in 31 bits
+  const int rows = num_new > 0 ? num_new : g.N;
+  p.one = g.num_pages <= kOnePages && rows <= kOneRows && static_cast<int64_t>(rows) * g.M <= kOneEntries;
   p.words = (g.num_pages + 31) / 32;
   const size_t map = align256(static_cast<size_t>(p.words) * 4);
   p.off_held = 0;
   p.off_tail = map;
   p.off_first = p.off_tail + (num_new > 0 ? map : 0);
   p.off_rows = p.off_first + (num_new > 0 ? align256(static_cast<size_t>(g.num_pages) * 4) : 0);
-  p.total = p.off_rows + align256(static_cast<size_t>(num_new) * sizeof(RowPlan)) + 256;
+  p.total = p.one ? 256 : p.off_rows + align256(static_cast<size_t>(num_new) * sizeof(RowPlan)) + 512;
   return OMNIMEM_OK;
 }
 
@@ -223,7 +226,7 @@ omnimem_status_t check_seq_update(const omnimem_seq_table_t* st, int32_t num_new
     return OMNIMEM_EINVAL;
   if (g.N > 0 && (out_table == g.table || out_lens == g.lens)) return OMNIMEM_EINVAL;
   a = SeqUpdateLaunch{num_new, parent, keep, grow, out_table, out_lens, copies, info};
-  return check_scratch(workspace, workspace_bytes, p.total);
+  return p.one ? OMNIMEM_OK : check_scratch(workspace, workspace_bytes, p.total);
 }
 
 omnimem_status_t check_seq_compact(const omnimem_seq_table_t* st, int32_t* out_table, int32_t* moves, int32_t* info,
@@ -236,7 +239,7 @@ omnimem_status_t check_seq_compact(const omnimem_seq_table_t* st, int32_t* out_t
     return OMNIMEM_EINVAL;
   if (g.N > 0 && (out_table == nullptr || out_table == g.table)) return OMNIMEM_EINVAL;
   a = SeqUpdateLaunch{0, nullptr, nullptr, nullptr, out_table, nullptr, moves, info};
-  return check_scratch(workspace, workspace_bytes, p.total);
+  return p.one ? OMNIMEM_OK : check_scratch(workspace, workspace_bytes, p.total);
 }
 
 }  // namespace omnimem

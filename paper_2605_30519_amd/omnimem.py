@@ -1038,20 +1038,21 @@ def omnimem_seq_update(page_table: torch.Tensor, seq_lens: torch.Tensor, num_pag
         _check_tensor("keep", keep, (n,), torch.int32)
     if grow is not None:
         _check_tensor("grow", grow, (n,), torch.int32)
-    _on_gpu(page_table, "page_table", seq_lens=seq_lens, parent=parent, keep=keep, grow=grow)
+    if dev < 0 or not (seq_lens.get_device() == dev == parent.get_device() and (keep is None or keep.get_device() == dev)
+                       and (grow is None or grow.get_device() == dev)):
+        _on_gpu(page_table, "page_table", seq_lens=seq_lens, parent=parent, keep=keep, grow=grow)
     made = _seq_out(out, n, page_table.shape[1], n, None, page_table.device)
     if out is not None:
         _on_gpu(page_table, "page_table", out_table=made.page_table, out_lens=made.seq_lens, copies=made.copies,
                 info=made.info)
     L = lib()
     need = L.omnimem_seq_workspace_bytes(desc, n)
-    if workspace is None:
-        workspace = torch.empty(need or 256, dtype=torch.uint8, device=page_table.device)
-    else:
+    if workspace is not None:
         _check_workspace(workspace, need, page_table)
+    elif need > 256:   # 256: the call needs none
+        workspace = torch.empty(need, dtype=torch.uint8, device=page_table.device)
     st = L.omnimem_seq_update(desc, n, _ptr(parent), _ptr(keep), _ptr(grow), _ptr(made.page_table), _ptr(made.seq_lens),
-                              _ptr(made.copies), _ptr(made.info), workspace.data_ptr(), workspace.numel(),
-                              _current_raw_stream())
+                              _ptr(made.copies), _ptr(made.info), _ptr(workspace), need, _current_raw_stream())
     if st != 0:
         _check(st, "omnimem_seq_update")
     return made
@@ -1076,12 +1077,12 @@ def omnimem_seq_compact(page_table: torch.Tensor, seq_lens: torch.Tensor, num_pa
         _on_gpu(page_table, "page_table", out_table=made.page_table, moves=made.copies, info=made.info)
     L = lib()
     need = L.omnimem_seq_workspace_bytes(desc, 0)
-    if workspace is None:
-        workspace = torch.empty(need or 256, dtype=torch.uint8, device=page_table.device)
-    else:
+    if workspace is not None:
         _check_workspace(workspace, need, page_table)
-    st = L.omnimem_seq_compact(desc, _ptr(made.page_table), _ptr(made.copies), _ptr(made.info), workspace.data_ptr(),
-                               workspace.numel(), _current_raw_stream())
+    elif need > 256:   # 256: the call needs none
+        workspace = torch.empty(need, dtype=torch.uint8, device=page_table.device)
+    st = L.omnimem_seq_compact(desc, _ptr(made.page_table), _ptr(made.copies), _ptr(made.info), _ptr(workspace), need,
+                               _current_raw_stream())
     if st != 0:
         _check(st, "omnimem_seq_compact")
     return made

@@ -327,6 +327,24 @@ def test_compact_edges(dev):
     assert u.info.tolist()[0] > 1000
 
 
+def test_a_dirty_workspace(dev):
+    """Tables past one workgroup's, with scratch that another use has left full."""
+    rng = random.Random(6)
+    table, lens = random_tables(rng, 300, 17000, 64, 64, 1500)
+    M = max(len(r) for r in table) + 1
+    table = [r + [-1] * (M - len(r)) for r in table]
+    t, l = i32(table, dev), i32(lens, dev)
+    need = omnimem_seq_workspace_bytes(t, l, 17000, 64, 300)
+    assert need > 256
+    for fill in (255, 0, 127):
+        ws = workspace_tensor(need, dev).fill_(fill)
+        update_and_check(dev, table, lens, 17000, 64, 0, list(range(300)), None, [1] * 300, workspace=ws)
+        ws.fill_(fill)
+        c = omnimem_seq_compact(t, l, 17000, 64, workspace=ws)
+        rows, _, info = seq_oracle.compact(table, lens, 17000, 64, 64)
+        assert c.info.tolist() == info and c.page_table.tolist() == rows
+
+
 def test_given_buffers_and_workspace(dev):
     t, l = i32([[3, 1], [0, 4]], dev), i32([100, 70], dev)
     ws = workspace_tensor(omnimem_seq_workspace_bytes(t, l, 8, 64, 2), dev)

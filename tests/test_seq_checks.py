@@ -122,10 +122,12 @@ def test_copy_arguments():
 
 def test_update_and_compact_arguments():
     L = abi()
-    t = table()
+    t = table(num_pages=20000)
     need = L.omnimem_seq_workspace_bytes(ctypes.byref(t), 5)
     none = L.omnimem_seq_workspace_bytes(ctypes.byref(t), 0)
-    assert need > none >= 256 and need % 256 == 0
+    assert need > none > 256 and need % 256 == 0
+    small = table()                                          # small tables need no scratch
+    assert L.omnimem_seq_workspace_bytes(ctypes.byref(small), 5) == 256 == L.omnimem_seq_workspace_bytes(ctypes.byref(small), 0)
 
     def update(n=5, parent=FAKE, keep=FAKE, grow=FAKE, rows=FAKE + 64, lens=FAKE + 64, copies=FAKE, info=FAKE, ws=FAKE,
                size=need, t=t):
@@ -144,7 +146,7 @@ def test_update_and_compact_arguments():
         assert compact(**kw) == EINVAL, kw
     assert compact(size=none - 1) == EWS
     assert L.omnimem_seq_workspace_bytes(None, 1) == 0
-    assert L.omnimem_seq_workspace_bytes(ctypes.byref(table(page_table=0, seq_lens=0)), 5) == need
+    assert L.omnimem_seq_workspace_bytes(ctypes.byref(table(page_table=0, seq_lens=0, num_pages=20000)), 5) == need
     assert L.omnimem_seq_workspace_bytes(ctypes.byref(t), -1) == 0
 
 
