@@ -18,6 +18,9 @@
  * it is appended (omnimem_compress_chunk); omnimem_select_compressed then scores
  * from the pooled keys instead of streaming all of K, and omnimem_cmp_attn is the
  * compression branch of Eq. 1 over the pooled keys and values.
+ * The sequence cache (omnimem_seq_update, omnimem_copy_pages, omnimem_append_kv,
+ * omnimem_decode_attn, omnimem_seq_compact) serves generation token by token, or chunk
+ * by chunk, of many sequences over one page pool.
  *
  * Conventions shared by every entry point
  *  - Every buffer pointer is a DEVICE pointer unless marked (host).  The caller

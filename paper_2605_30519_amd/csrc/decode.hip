@@ -279,11 +279,12 @@ __device__ __forceinline__ void lds_sync() {
   __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
 }
 
-// DIRECT: the workgroup's share is item blockIdx.x.
-template <typename T, int D, int NT, bool DIRECT>
+template <typename T, int D, int NT, DecodeSplit SPLIT>
 __global__ __launch_bounds__(kThreads, 2) void k_decode(const DecodeArgs A) {
   using L = Tile<T, D>;
   constexpr int RT = L::RT, VW = L::VW, QS = L::QS, UT = L::UNIT;
+  constexpr bool LINE = SPLIT == DecodeSplit::kLine, BY_WAVE = SPLIT == DecodeSplit::kWave;
+  constexpr int TEAM = BY_WAVE ? 1 : kDecodeWaves;  // waves that share a segment
   __shared__ __align__(16) float s_o[kDecodeWaves][NT * 16][D];
   __shared__ float s_top[kDecodeWaves][NT * 16], s_sum[kDecodeWaves][NT * 16];
   const int tid = threadIdx.x, lane = tid % kWave;
@@ -294,15 +295,17 @@ __global__ __launch_bounds__(kThreads, 2) void k_decode(const DecodeArgs A) {
 
   Segment g{};
   int left = 0;  // units of the share from g.unit on
-  if constexpr (DIRECT) {
-    g.seq = blockIdx.x / HH;
-    g.head = blockIdx.x % HH;
+  if constexpr (!LINE) {
+    const int item = BY_WAVE ? blockIdx.x * kDecodeWaves + wave : blockIdx.x;
+    g.seq = item / HH;
+    g.head = item - g.seq * HH;
+    if (g.seq >= N) return;  // behind the last item, where every wave has its own
     g.sp = span_of<UT>(A, __builtin_amdgcn_readfirstlane(A.g.lens[g.seq]));
     left = g.sp.units;
     if (left == 0) {
       const int h = g.head / A.head_tiles, tile = g.head % A.head_tiles;
       const int rows = min(A.tile_rows, A.G - tile * A.tile_rows);
-      for (int e = tid; e < rows * (D / 4); e += kThreads)
+      for (int e = BY_WAVE ? lane : tid; e < rows * (D / 4); e += TEAM * kWave)
         finish<T>(A, g.seq, h * A.G + tile * A.tile_rows + e / (D / 4), e % (D / 4) * 4, f32x4{}, 0.f, 0.f);
       return;
     }
@@ -377,7 +380,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_decode(const DecodeArgs A) {
   // most one in front of g; its units are looked up 64 at a time, lane l the l-th one's page,
   // first token row, and rows in use.
   Segment f = g;
-  int next = f.unit + wave;
+  int next = f.unit + (BY_WAVE ? 0 : wave);
   uint64_t mask = 0;
   int l_page = 0, l_row = 0, l_lo = 0, l_hi = 0;
   int lo = 0, hi = 0, sub = 0;  // the tile's unit: rows in use, rows before the tile
@@ -392,7 +395,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_decode(const DecodeArgs A) {
         lo = hi = sub = 0;  // a tile of no rows
         return false;
       }
-      const int u = next + lane * kDecodeWaves;
+      const int u = next + lane * TEAM;
       bool ok = u < f.stop;
       if (ok) {
         const int in_block = block_shift(A.g) - (UT == 64 ? 6 : 5);  // log2 of a block's units
@@ -407,7 +410,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_decode(const DecodeArgs A) {
         ok = l_page >= 0 && l_page < A.g.num_pages && l_lo < l_hi;
       }
       mask = __ballot(ok);
-      next += kWave * kDecodeWaves;
+      next += kWave * TEAM;
     }
     const int at = __builtin_ctzll(mask);
     mask &= mask - 1;
@@ -437,7 +440,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_decode(const DecodeArgs A) {
   // the stream's next segment; false behind the share's last one
   auto next_segment = [&]() -> bool {
     left -= kItemUnits;
-    if (DIRECT || left <= 0) return false;
+    if (!LINE || left <= 0) return false;
     f.unit = 0;
     if (++f.head == HH) {
       f.head = 0;
@@ -538,6 +541,23 @@ __global__ __launch_bounds__(kThreads, 2) void k_decode(const DecodeArgs A) {
     // the waves' results meet
     const int tile = g.head % A.head_tiles, hq0 = g.head / A.head_tiles * A.G + tile * A.tile_rows;
     const int rows = min(A.tile_rows, A.G - tile * A.tile_rows);
+    if constexpr (BY_WAVE) {
+#pragma unroll
+      for (int n = 0; n < NT; ++n) {
+        const float total = sum_over_groups(sum[n]);
+        if (n * 16 + i >= rows) continue;
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+#pragma unroll
+          for (int x = 0; x < VW / 4; ++x) {
+            f32x4 w;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) w[e] = o[n][4 * x + e][r];
+            finish<T>(A, g.seq, hq0 + n * 16 + i, L::dim(4 * j + r, x), w, top[n], total);
+          }
+      }
+      return;
+    }
     if (!first) lds_sync();  // the last segment's results have been read
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
@@ -560,7 +580,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_decode(const DecodeArgs A) {
       }
     }
     lds_sync();
-    const bool complete = DIRECT || (g.unit == 0 && g.stop == g.sp.units);
+    const bool complete = !LINE || (g.unit == 0 && g.stop == g.sp.units);
     float* slot = A.part + (static_cast<int64_t>(blockIdx.x) * 2 + (first ? 0 : 1)) * A.slot_floats;
     for (int e = tid; e < rows * (D / 4); e += kThreads) {
       const int r = e / (D / 4), d = e % (D / 4) * 4;
@@ -653,13 +673,12 @@ __global__ __launch_bounds__(256) void k_decode_join(const DecodeArgs A) {
 
 template <typename T, int D, int NT>
 hipError_t launch_rows(const DecodeArgs& A, const DecodePlan& p, hipStream_t stream) {
+  const auto kernel = p.split == DecodeSplit::kLine   ? k_decode<T, D, NT, DecodeSplit::kLine>
+                      : p.split == DecodeSplit::kItem ? k_decode<T, D, NT, DecodeSplit::kItem>
+                                                      : k_decode<T, D, NT, DecodeSplit::kWave>;
   LaunchStatus st;
-  if (p.direct) {
-    st(k_decode<T, D, NT, true>, dim3(p.wgs), dim3(kThreads), 0, stream, A);
-    return st.err;
-  }
-  st(k_decode<T, D, NT, false>, dim3(p.wgs), dim3(kThreads), 0, stream, A);
-  if (p.wgs > 1) {
+  st(kernel, dim3(p.wgs), dim3(kThreads), 0, stream, A);
+  if (p.split == DecodeSplit::kLine && p.wgs > 1) {
     const auto join = p.join_rows == 1 ? k_decode_join<T, D, 1> : p.join_rows == 2 ? k_decode_join<T, D, 2> : k_decode_join<T, D, 4>;
     st(join, dim3(p.wgs, (p.rows + p.join_rows - 1) / p.join_rows), dim3(256), 0, stream, A);
   }

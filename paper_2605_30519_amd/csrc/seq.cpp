@@ -67,7 +67,10 @@ constexpr int64_t kDecodeWgs = 256, kDecodeManyWgs = 512;
 // tokens (18 units), 8 key heads, 7.7 us against 9.1, 64 of them 22.8 / 25.6; one of 1,000 tokens
 // 16.1 / 9.8 (16.5 with eight waves: a CU takes in no more).  Many items of 1,000 tokens gain 6%
 // so, and lose as much if they are ragged.
-constexpr int64_t kDirectUnits = 20;
+// Where there are four of them and more for each CU, a wave to an item up to 8 units: 1,024 items of
+// 60 tokens, 24 query heads, 17.2 -> 11.8 us (4 query heads 10.6 -> 8.2, one fp32 17.4 -> 13.8); 512
+// items 9.0 / 8.9 (5.9 / 6.8, 9.5 / 10.8), 64 items of 120 tokens 4.9 -> 9.0.
+constexpr int64_t kItemUnitsMost = 20, kWaveUnitsMost = 8, kWaveItems = 1024;
 constexpr int64_t kItemOverhead = 64;  // of an item's length on the line, no less than the kernel adds
 
 omnimem_status_t plan_decode(const omnimem_seq_cache_t* sc, const SeqGeom& g, int32_t num_q_heads, int32_t window,
@@ -78,25 +81,34 @@ omnimem_status_t plan_decode(const omnimem_seq_cache_t* sc, const SeqGeom& g, in
   p.head_tiles = (p.G + p.tile_rows - 1) / p.tile_rows;
   p.rows = p.G < p.tile_rows ? p.G : p.tile_rows;
   const int64_t items = static_cast<int64_t>(g.N) * sc->num_heads * p.head_tiles;
-  // blocks and units of an item, at most
-  const int64_t blocks = window > 0 && window / g.B + 2 < g.M && g.Bpc == 1 ? window / g.B + 2 : g.M;
+  // Blocks and units of an item, at most.  A window reaches into window / S + 2 chunks, and
+  // tokens of one run lie in no more than a B-th of them, and two, blocks.
+  int64_t blocks = g.M;
+  if (window > 0) {
+    const int64_t runs = g.Bpc == 1 && g.S == g.B ? 1 : window / g.S + 2;
+    blocks = window / g.B + 2 * runs < blocks ? window / g.B + 2 * runs : blocks;
+  }
   const int64_t unit = sc->dtype == OMNIMEM_BF16 && sc->head_dim == 64 ? 64 : 32;
   const int64_t units = blocks * (g.B / unit);
   // a sum of the sequences' units in 31 bits, positions on the line in 40
   if (items > 0x7fffffff / 256 || static_cast<int64_t>(g.N) * (static_cast<int64_t>(g.M) * (g.B / unit) + kItemOverhead) > 0x7fffffff ||
       (items > 0 && units > (int64_t{1} << 40) / items))
     return OMNIMEM_EINVAL;
-  p.direct = units <= kDirectUnits;
+  p.split = units <= kWaveUnitsMost && items >= kWaveItems ? DecodeSplit::kWave
+            : units <= kItemUnitsMost                         ? DecodeSplit::kItem
+                                                              : DecodeSplit::kLine;
   const int64_t most = items * (units + kItemOverhead);
   const int64_t wgs = items > kDecodeWgs ? kDecodeManyWgs : kDecodeWgs;
-  p.wgs = static_cast<int>(p.direct ? items : most < wgs ? most : wgs);
+  p.wgs = static_cast<int>(p.split == DecodeSplit::kLine   ? (most < wgs ? most : wgs)
+                           : p.split == DecodeSplit::kItem ? items
+                                                           : (items + kDecodeWaves - 1) / kDecodeWaves);
   p.join_rows = items * 16 <= p.wgs ? 1 : p.rows >= 4 ? 4 : p.rows >= 2 ? 2 : 1;
   p.slot_floats = static_cast<size_t>(p.rows) * (sc->head_dim + 2);
   p.slot_floats = (p.slot_floats + 3) / 4 * 4;
   p.off_part = 0;
-  const size_t shares = p.direct ? 0 : p.wgs;  // a direct call needs no scratch: 256
+  const size_t shares = p.split == DecodeSplit::kLine ? p.wgs : 0;
   p.off_starts = align256(shares * 2 * p.slot_floats * sizeof(float));
-  p.total = p.direct ? 256 : p.off_starts + align256(shares * sizeof(DecodeStart)) + 512;
+  p.total = shares == 0 ? 256 : p.off_starts + align256(shares * sizeof(DecodeStart)) + 512;
   return OMNIMEM_OK;
 }
 
@@ -162,7 +174,7 @@ omnimem_status_t check_decode_attn(const omnimem_seq_cache_t* sc, const void* q,
   a.scale = scale;
   a.out = out;
   a.lse = lse;
-  return p.direct ? OMNIMEM_OK : check_scratch(workspace, workspace_bytes, p.total);
+  return p.split != DecodeSplit::kLine ? OMNIMEM_OK : check_scratch(workspace, workspace_bytes, p.total);
 }
 
 omnimem_status_t check_append_kv(const omnimem_seq_cache_t* sc, const void* k, int64_t k_stride, const void* v,

@@ -23,7 +23,8 @@ struct SeqGeom {
 // ---------------------------------------------------------------- decode
 // The (sequence, key/value head, tile of query heads) items of a call, each of them its
 // sequence's units of 32 tokens (64 for bf16 heads of 64) in turn, form one line, which `wgs`
-// workgroups share evenly; or, where sequences are short, an item is a workgroup's (direct).
+// workgroups share evenly; or, where sequences are short, an item is a workgroup's, or a wave's.
+enum class DecodeSplit { kLine, kItem, kWave };
 constexpr int kDecodeWaves = 4;
 constexpr int kDecodeHeadRows = 16;  // query heads of an MFMA tile
 
@@ -33,7 +34,7 @@ struct DecodePlan {
   int tile_rows;     // query heads of a tile: 16 or 32
   int rows;          // of them in use, min(G, tile_rows)
   int wgs;           // workgroups
-  bool direct;
+  DecodeSplit split;
   int join_rows;     // query heads of a workgroup that joins shares
   size_t off_part, off_starts, total;
   size_t slot_floats;  // one workgroup's partial result of one item: O [rows][d], max [rows], sum [rows]

@@ -166,6 +166,19 @@ def test_many_sequences(dev):
     check(cache, queries(dev, F32, 700, 2, 64, g))
 
 
+@pytest.mark.parametrize("dtype,d,H,G,window", [(BF16, 128, 4, 3, 0), (F32, 64, 8, 20, 0), (BF16, 64, 3, 1, 5), (F32, 128, 4, 17, 90)])
+def test_many_short_items(dev, dtype, d, H, G, window):
+    """Over a thousand (sequence, head) items of up to two blocks, or of a short window; the last
+    workgroup is not full."""
+    N = 345 if H == 3 else 260 if H == 4 else 131
+    lens = [(i * 29) % 129 for i in range(N)]
+    if window:
+        lens[7], lens[100] = 400, 129
+    say(f"decode short {dtype} d={d} H={H} G={G} window={window}")
+    cache, g = build(dev, dtype, H, d, 64, 64, lens, 18, extra_blocks=0)
+    check(cache, queries(dev, dtype, N, H * G, d, g), window)
+
+
 def test_strided_queries_and_given_buffers(dev):
     cache, g = build(dev, BF16, 2, 128, 64, 64, [100, 300, 5], 12)
     qkv = queries(dev, BF16, 3, 4 * 3, 128, g).view(3, 3, 4, 128)
