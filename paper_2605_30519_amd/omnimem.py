@@ -1004,9 +1004,14 @@ def _seq_out(out: Optional[SeqUpdate], n: int, m: int, pairs: int, lens, dev) ->
     """The caller's buffers, checked, or new ones, cut from one allocation (lens: given)."""
     if out is None:
         own = n if lens is None else 0
-        table, l, copies, info = torch.empty(n * m + own + 2 * pairs + 4, dtype=torch.int32, device=dev).split(
-            [n * m, own, 2 * pairs, 4])
-        return SeqUpdate(table.view(n, m), l if lens is None else lens, copies.view(pairs, 2), info)
+        flat = torch.empty(n * m + own + 2 * pairs + 4, dtype=torch.int32, device=dev)
+        if own:
+            lens = flat.as_strided((n,), (1,), n * m)
+        elif lens is None:
+            lens = flat[:0]
+        at = n * m + own
+        return SeqUpdate(flat.as_strided((n, m), (m, 1), 0), lens, flat.as_strided((pairs, 2), (2, 1), at),
+                         flat.as_strided((4,), (1,), at + 2 * pairs))
     _check_tensor("out.page_table", out.page_table, (n, m), torch.int32)
     _check_tensor("out.seq_lens", out.seq_lens, (n,), torch.int32)
     _check_tensor("out.copies", out.copies, (pairs, 2), torch.int32)
