@@ -332,10 +332,13 @@ __global__ __launch_bounds__(kThreads, 2) void k_decode(const DecodeArgs A) {
     const int64_t pos = static_cast<int64_t>(blockIdx.x) * share;
     // sequences without tokens get their zeros
     if (__ballot(empty) != 0) {
-      for (int s = blockIdx.x; s < N; s += gridDim.x) {
-        if (span_of<UT>(A, A.g.lens[s]).units != 0) continue;
-        for (int e = tid; e < A.a.Hq * (D / 4); e += kThreads)
-          finish<T>(A, s, e / (D / 4), e % (D / 4) * 4, f32x4{}, 0.f, 0.f);
+      const int each = (N + gridDim.x - 1) / gridDim.x;
+      const int end = min(static_cast<int64_t>(N), (static_cast<int64_t>(blockIdx.x) + 1) * each);
+      for (int64_t s0 = static_cast<int64_t>(blockIdx.x) * each; s0 < end; s0 += kWave) {
+        uint64_t none = __ballot(s0 + lane < end && span_of<UT>(A, A.g.lens[min(s0 + lane, int64_t{N} - 1)]).units == 0);
+        for (; none != 0; none &= none - 1)
+          for (int e = tid; e < A.a.Hq * (D / 4); e += kThreads)
+            finish<T>(A, static_cast<int>(s0) + __builtin_ctzll(none), e / (D / 4), e % (D / 4) * 4, f32x4{}, 0.f, 0.f);
       }
     }
     if (pos >= line) {

@@ -179,6 +179,20 @@ def test_many_short_items(dev, dtype, d, H, G, window):
     check(cache, queries(dev, dtype, N, H * G, d, g), window)
 
 
+def test_thousands_of_sequences_most_of_them_empty(dev):
+    """More sequences than one look at them by a workgroup's lanes, some long, so that shares are joined."""
+    lens = [900 if i % 5000 == 17 else 40 if i % 700 == 3 else 0 for i in range(20000)]
+    cache, g = build(dev, F32, 1, 64, 64, 64, lens, 19)
+    q = queries(dev, F32, len(lens), 1, 64, g)
+    out, lse = omnimem_decode_attn(cache, q)
+    some = [i for i, t in enumerate(lens) if t] + [0, 1, 19999]
+    O, L, ob, lb = seq_oracle.decode(q[some], cache.k_pages, cache.v_pages, cache.page_table[some], cache.seq_lens[some], 64,
+                                     64, 0, 0.125)
+    assert ((out[some].double().cpu() - O).abs() <= ob).all()
+    full = torch.tensor(lens) > 0
+    assert (out.cpu()[~full] == 0).all() and (lse.cpu()[:, ~full] == -math.inf).all() and torch.isfinite(lse.cpu()[:, full]).all()
+
+
 def test_strided_queries_and_given_buffers(dev):
     cache, g = build(dev, BF16, 2, 128, 64, 64, [100, 300, 5], 12)
     qkv = queries(dev, BF16, 3, 4 * 3, 128, g).view(3, 3, 4, 128)

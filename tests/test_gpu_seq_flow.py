@@ -214,6 +214,37 @@ def test_steps_in_a_graph(dev):
             assert torch.equal(x, y)
 
 
+def test_two_graphs_that_share_a_workspace(dev):
+    """Nothing in a workspace outlives its call: two graphs over one workspace, replayed in turn."""
+    g = torch.Generator(device=dev).manual_seed(21)
+    runs = []
+    for N, t, H in ((2, 4000, 4), (9, 1500, 2)):
+        n = -(-t // 64)
+        cache = SeqKVCache(torch.randn((N * n, H, 64, 128), generator=g, device=dev).to(BF16),
+                           torch.randn((N * n, H, 64, 128), generator=g, device=dev).to(BF16),
+                           torch.randperm(N * n, generator=g, device=dev).int().view(N, n),
+                           torch.full((N,), t, dtype=torch.int32, device=dev))
+        q = torch.randn((N, 2 * H, 128), generator=g, device=dev).to(BF16)
+        runs.append((cache, q, torch.empty_like(q), torch.empty((2 * H, N), device=dev)))
+    ws = workspace_tensor(max(omnimem_decode_workspace_bytes(r[0], r[1].shape[1]) for r in runs), dev)
+    want = [omnimem_decode_attn(c, q) for c, q, _, _ in runs]
+    torch.cuda.synchronize()
+    graphs = []
+    for cache, q, out, lse in runs:
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1]):
+            omnimem_decode_attn(cache, q, out=out, lse=lse, workspace=ws)
+    for _ in range(3):
+        for graph, r in zip(graphs, runs):
+            r[2].fill_(-3)
+            graph.replay()
+        torch.cuda.synchronize()
+        for (o, l), r in zip(want, runs):
+            assert torch.equal(r[2], o) and torch.equal(r[3], l)
+        for graph in reversed(graphs):
+            graph.replay()
+
+
 def test_two_streams_at_once(dev):
     """Calls on two streams, each with buffers of its own, do not disturb one another."""
     g = torch.Generator(device=dev).manual_seed(11)
