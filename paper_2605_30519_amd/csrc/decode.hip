@@ -34,6 +34,7 @@ constexpr int kItemUnits = 3;
 constexpr int kThreads = kDecodeWaves * kWave;
 constexpr int kMinUnits = 4;      // units of a share: one for each wave
 constexpr float kLowest = -FLT_MAX;  // below every score: a row without keys keeps sum 0
+constexpr int kAskUnits = 64;     // units of a share from which it is asked whether pages are shared
 constexpr int kNontemporal = 2;   // cache policy of a buffer load: read once
 
 struct DecodeArgs {
@@ -120,6 +121,7 @@ struct Tile<uint16_t, D> {
 
   __device__ __forceinline__ static int key(int t, int r, int j) { return 32 * (t / 2) + 8 * j + 4 * (t % 2) + r; }
 
+  template <int POLICY>
   __device__ __forceinline__ void load_k(__amdgpu_buffer_rsrc_t rs, int i, int j) {
     const int at = (8 * (i / 4) + i % 4) * ROW + j * 16;
 #pragma unroll
@@ -128,8 +130,9 @@ struct Tile<uint16_t, D> {
       for (int a = 0; a < 2; ++a)
 #pragma unroll
         for (int s = 0; s < QS; ++s)
-          k[b][a][s] = __builtin_amdgcn_raw_buffer_load_b128(rs, at + (32 * b + 4 * a) * ROW + s * 64, 0, kNontemporal);
+          k[b][a][s] = __builtin_amdgcn_raw_buffer_load_b128(rs, at + (32 * b + 4 * a) * ROW + s * 64, 0, POLICY);
   }
+  template <int POLICY>
   __device__ __forceinline__ void load_v(__amdgpu_buffer_rsrc_t rs, int i, int j) {
     const int at = 8 * j * ROW + i * VW * 2;
 #pragma unroll
@@ -137,8 +140,8 @@ struct Tile<uint16_t, D> {
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
         const int from = at + (32 * b + e) * ROW;
-        if constexpr (VW == 8) v[b][e] = __builtin_amdgcn_raw_buffer_load_b128(rs, from, 0, kNontemporal);
-        else v[b][e] = __builtin_amdgcn_raw_buffer_load_b64(rs, from, 0, kNontemporal);
+        if constexpr (VW == 8) v[b][e] = __builtin_amdgcn_raw_buffer_load_b128(rs, from, 0, POLICY);
+        else v[b][e] = __builtin_amdgcn_raw_buffer_load_b64(rs, from, 0, POLICY);
       }
   }
   __device__ __forceinline__ void clear_v_below(int lo, int j) {
@@ -193,14 +196,16 @@ struct Tile<float, D> {
 
   __device__ __forceinline__ static int key(int t, int r, int j) { return 16 * t + 4 * j + r; }
 
+  template <int POLICY>
   __device__ __forceinline__ void load_k(__amdgpu_buffer_rsrc_t rs, int i, int j) {
     const int at = i * ROW + j * 16;
 #pragma unroll
     for (int t = 0; t < RT; ++t)
 #pragma unroll
       for (int s = 0; s < QS; ++s)
-        k[t][s] = __builtin_amdgcn_raw_buffer_load_b128(rs, at + 16 * t * ROW + s * 64, 0, kNontemporal);
+        k[t][s] = __builtin_amdgcn_raw_buffer_load_b128(rs, at + 16 * t * ROW + s * 64, 0, POLICY);
   }
+  template <int POLICY>
   __device__ __forceinline__ void load_v(__amdgpu_buffer_rsrc_t rs, int i, int j) {
     const int at = 4 * j * ROW + i * 16;
 #pragma unroll
@@ -209,7 +214,7 @@ struct Tile<float, D> {
       for (int r = 0; r < 4; ++r)
 #pragma unroll
         for (int x = 0; x < VW / 4; ++x)
-          v[t][r][x] = __builtin_amdgcn_raw_buffer_load_b128(rs, at + (16 * t + r) * ROW + x * 256, 0, kNontemporal);
+          v[t][r][x] = __builtin_amdgcn_raw_buffer_load_b128(rs, at + (16 * t + r) * ROW + x * 256, 0, POLICY);
   }
   __device__ __forceinline__ void clear_v_below(int lo, int j) {
 #pragma unroll
@@ -295,6 +300,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_decode(const DecodeArgs A) {
 
   Segment g{};
   int left = 0;  // units of the share from g.unit on
+  bool long_share = false;
   if constexpr (!LINE) {
     const int item = BY_WAVE ? blockIdx.x * kDecodeWaves + wave : blockIdx.x;
     g.seq = item / HH;
@@ -329,6 +335,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_decode(const DecodeArgs A) {
     const int even = small ? static_cast<int>((static_cast<uint32_t>(line) + gridDim.x - 1) / gridDim.x)
                            : static_cast<int>((line + gridDim.x - 1) / gridDim.x);
     const int share = max(kMinUnits, even);
+    long_share = share >= kAskUnits;
     const int64_t pos = static_cast<int64_t>(blockIdx.x) * share;
     // sequences without tokens get their zeros
     if (__ballot(empty) != 0) {
@@ -388,32 +395,35 @@ __global__ __launch_bounds__(kThreads, 2) void k_decode(const DecodeArgs A) {
   int l_page = 0, l_row = 0, l_lo = 0, l_hi = 0;
   int lo = 0, hi = 0, sub = 0;  // the tile's unit: rows in use, rows before the tile
   int64_t row = 0;              // the unit's first row in the pools
+  auto look_up = [&]() {
+    const int u = next + lane * TEAM;
+    bool ok = u < f.stop;
+    if (ok) {
+      const int in_block = block_shift(A.g) - (UT == 64 ? 6 : 5);  // log2 of a block's units
+      const int b = f.sp.block + (u >> in_block);
+      l_row = (u & ((1 << in_block) - 1)) * UT;
+      const int c = A.g.Bpc == 1 ? b : b / A.g.Bpc;
+      const int in = (b - c * A.g.Bpc) * A.g.B + l_row;
+      const int tok = c * A.g.S + in;
+      l_page = A.g.table[static_cast<int64_t>(f.seq) * A.g.M + b];
+      l_hi = min(UT, min(A.g.S - in, f.sp.end - tok));
+      l_lo = max(0, f.sp.begin - tok);
+      ok = l_page >= 0 && l_page < A.g.num_pages && l_lo < l_hi;
+    }
+    mask = __ballot(ok);
+    next += kWave * TEAM;
+  };
   auto advance = [&]() -> bool {
     if (sub + L::KEYS < hi) {
       sub += L::KEYS;
       return true;
     }
     while (mask == 0) {
-      if (next >= f.stop) {
+      if (!LINE || next >= f.stop) {  // an item of a workgroup's own or a wave's is one look-up
         lo = hi = sub = 0;  // a tile of no rows
         return false;
       }
-      const int u = next + lane * TEAM;
-      bool ok = u < f.stop;
-      if (ok) {
-        const int in_block = block_shift(A.g) - (UT == 64 ? 6 : 5);  // log2 of a block's units
-        const int b = f.sp.block + (u >> in_block);
-        l_row = (u & ((1 << in_block) - 1)) * UT;
-        const int c = A.g.Bpc == 1 ? b : b / A.g.Bpc;
-        const int in = (b - c * A.g.Bpc) * A.g.B + l_row;
-        const int tok = c * A.g.S + in;
-        l_page = A.g.table[static_cast<int64_t>(f.seq) * A.g.M + b];
-        l_hi = min(UT, min(A.g.S - in, f.sp.end - tok));
-        l_lo = max(0, f.sp.begin - tok);
-        ok = l_page >= 0 && l_page < A.g.num_pages && l_lo < l_hi;
-      }
-      mask = __ballot(ok);
-      next += kWave * TEAM;
+      look_up();
     }
     const int at = __builtin_ctzll(mask);
     mask &= mask - 1;
@@ -461,159 +471,187 @@ __global__ __launch_bounds__(kThreads, 2) void k_decode(const DecodeArgs A) {
 
   L t;
   load_q();
-  bool have = advance();
-  t.load_k(rsrc(A.a.k_pages), i, j);
-  __builtin_amdgcn_sched_barrier(0);  // K in front of V here as in the loop, whose waits count on it
-  t.load_v(rsrc(A.a.v_pages), i, j);
-  for (bool first = true;; first = false) {
-    f32x4 o[NT][VW] = {};
-    float top[NT], sum[NT];
-#pragma unroll
-    for (int n = 0; n < NT; ++n) {
-      top[n] = kLowest;
-      sum[n] = 0.f;
+  // A page of one sequence is read once, and marked so it comes a tenth faster; one that forked
+  // sequences share is read by each, and serves them from the caches when it is not.  16 sequences
+  // of 30,000 tokens, 8 key heads, on one prompt's pages: 241 us marked, 147 not; 8,000 tokens: 69
+  // / 50.  On pages of their own, four of 47 to 94 thousand tokens, 12 key heads: 248 / 272.  So a
+  // workgroup with a long share looks whether the row in front of or behind its first segment's has
+  // the same pages.  A short share gains nothing (64 of 2,000: 45 both) and would wait 0.5 us for
+  // the answer, and with more than 16 query heads to a key head a second loop costs registers that
+  // there are not.
+  bool shared = false;
+  if constexpr (LINE && NT == 1) {
+    const int u = f.unit + lane;
+    bool same = false;
+    if (long_share && u < f.stop && N > 1) {
+      const int b = f.sp.block + (u >> (block_shift(A.g) - (UT == 64 ? 6 : 5)));
+      const int32_t* at = A.g.table + static_cast<int64_t>(f.seq) * A.g.M + b;
+      const int32_t before = f.seq > 0 ? at[-A.g.M] : -1, behind = f.seq + 1 < N ? at[A.g.M] : -1;
+      same = before == *at || behind == *at;
     }
-    bool ahead = false;  // f is the segment behind g
-    bool follows = false;
-    while (have) {
-      const int clo = lo - sub, chi = hi - sub;  // rows of the tile in use
-      f32x4 s[NT][RT];
-#pragma unroll
-      for (int n = 0; n < NT; ++n)
-#pragma unroll
-        for (int r = 0; r < RT; ++r) s[n][r] = t.qk(q[n], r);
-      have = advance();
-      if (!have) {
-        ahead = true;
-        follows = next_segment();
-        if (follows) advance();
-      }
-      t.load_k(rsrc(A.a.k_pages), i, j);
-      const bool whole = clo <= 0 && chi >= L::KEYS;
+    shared = 2 * __popcll(__ballot(same)) > min(kWave, f.stop - f.unit);
+  }
+  if constexpr (!LINE) look_up();
+  bool have = advance();
+  auto stream = [&](auto policy) __attribute__((always_inline)) {
+    constexpr int POLICY = decltype(policy)::value;
+    t.template load_k<POLICY>(rsrc(A.a.k_pages), i, j);
+    __builtin_amdgcn_sched_barrier(0);  // K in front of V here as in the loop, whose waits count on it
+    t.template load_v<POLICY>(rsrc(A.a.v_pages), i, j);
+    for (bool first = true;; first = false) {
+      f32x4 o[NT][VW] = {};
+      float top[NT], sum[NT];
 #pragma unroll
       for (int n = 0; n < NT; ++n) {
-        float m = kLowest;
+        top[n] = kLowest;
+        sum[n] = 0.f;
+      }
+      bool ahead = false;  // f is the segment behind g
+      bool follows = false;
+      while (have) {
+        const int clo = lo - sub, chi = hi - sub;  // rows of the tile in use
+        f32x4 s[NT][RT];
 #pragma unroll
-        for (int r = 0; r < RT; ++r)
+        for (int n = 0; n < NT; ++n)
 #pragma unroll
-          for (int e = 0; e < 4; ++e) s[n][r][e] *= A.scale2;
-        if (!whole) {
+          for (int r = 0; r < RT; ++r) s[n][r] = t.qk(q[n], r);
+        have = advance();
+        if (!have) {
+          ahead = true;
+          follows = next_segment();
+          if (follows) advance();
+        }
+        t.template load_k<POLICY>(rsrc(A.a.k_pages), i, j);
+        const bool whole = clo <= 0 && chi >= L::KEYS;
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+          float m = kLowest;
+#pragma unroll
+          for (int r = 0; r < RT; ++r)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) s[n][r][e] *= A.scale2;
+          if (!whole) {
+#pragma unroll
+            for (int r = 0; r < RT; ++r)
+#pragma unroll
+              for (int e = 0; e < 4; ++e) {
+                const int key = L::key(r, e, j);
+                s[n][r][e] = key >= clo && key < chi ? s[n][r][e] : -INFINITY;
+              }
+          }
+#pragma unroll
+          for (int r = 0; r < RT; ++r)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) m = fmaxf(m, s[n][r][e]);
+          m = fmaxf(max_over_groups(m), top[n]);
+          const float keep = exp2f(top[n] - m);
+          top[n] = m;
+          float add = 0.f;
 #pragma unroll
           for (int r = 0; r < RT; ++r)
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-              const int key = L::key(r, e, j);
-              s[n][r][e] = key >= clo && key < chi ? s[n][r][e] : -INFINITY;
+              s[n][r][e] = __builtin_amdgcn_exp2f(s[n][r][e] - m);
+              add += s[n][r][e];
+            }
+          sum[n] = sum[n] * keep + add;
+          if (__any(keep != 1.f)) {
+#pragma unroll
+            for (int x = 0; x < VW; ++x)
+#pragma unroll
+              for (int e = 0; e < 4; ++e) o[n][x][e] *= keep;
+          }
+        }
+        if (clo > 0) t.clear_v_below(clo, j);
+        t.template pv<NT>(s, o);
+        t.template load_v<POLICY>(rsrc(A.a.v_pages), i, j);
+      }
+      if (!ahead) {  // the wave had no tile of this segment
+        follows = next_segment();
+        if (follows) advance();
+        t.template load_k<POLICY>(rsrc(A.a.k_pages), i, j);
+        __builtin_amdgcn_sched_barrier(0);
+        t.template load_v<POLICY>(rsrc(A.a.v_pages), i, j);
+      }
+
+      // the waves' results meet
+      const int tile = g.head % A.head_tiles, hq0 = g.head / A.head_tiles * A.G + tile * A.tile_rows;
+      const int rows = min(A.tile_rows, A.G - tile * A.tile_rows);
+      if constexpr (BY_WAVE) {
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+          const float total = sum_over_groups(sum[n]);
+          if (n * 16 + i >= rows) continue;
+#pragma unroll
+          for (int r = 0; r < 4; ++r)
+#pragma unroll
+            for (int x = 0; x < VW / 4; ++x) {
+              f32x4 w;
+#pragma unroll
+              for (int e = 0; e < 4; ++e) w[e] = o[n][4 * x + e][r];
+              finish<T>(A, g.seq, hq0 + n * 16 + i, L::dim(4 * j + r, x), w, top[n], total);
             }
         }
-#pragma unroll
-        for (int r = 0; r < RT; ++r)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) m = fmaxf(m, s[n][r][e]);
-        m = fmaxf(max_over_groups(m), top[n]);
-        const float keep = exp2f(top[n] - m);
-        top[n] = m;
-        float add = 0.f;
-#pragma unroll
-        for (int r = 0; r < RT; ++r)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            s[n][r][e] = __builtin_amdgcn_exp2f(s[n][r][e] - m);
-            add += s[n][r][e];
-          }
-        sum[n] = sum[n] * keep + add;
-        if (__any(keep != 1.f)) {
-#pragma unroll
-          for (int x = 0; x < VW; ++x)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) o[n][x][e] *= keep;
-        }
+        return;
       }
-      if (clo > 0) t.clear_v_below(clo, j);
-      t.template pv<NT>(s, o);
-      t.load_v(rsrc(A.a.v_pages), i, j);
-    }
-    if (!ahead) {  // the wave had no tile of this segment
-      follows = next_segment();
-      if (follows) advance();
-      t.load_k(rsrc(A.a.k_pages), i, j);
-      __builtin_amdgcn_sched_barrier(0);
-      t.load_v(rsrc(A.a.v_pages), i, j);
-    }
-
-    // the waves' results meet
-    const int tile = g.head % A.head_tiles, hq0 = g.head / A.head_tiles * A.G + tile * A.tile_rows;
-    const int rows = min(A.tile_rows, A.G - tile * A.tile_rows);
-    if constexpr (BY_WAVE) {
+      if (!first) lds_sync();  // the last segment's results have been read
 #pragma unroll
       for (int n = 0; n < NT; ++n) {
         const float total = sum_over_groups(sum[n]);
-        if (n * 16 + i >= rows) continue;
-#pragma unroll
-        for (int r = 0; r < 4; ++r)
-#pragma unroll
-          for (int x = 0; x < VW / 4; ++x) {
-            f32x4 w;
-#pragma unroll
-            for (int e = 0; e < 4; ++e) w[e] = o[n][4 * x + e][r];
-            finish<T>(A, g.seq, hq0 + n * 16 + i, L::dim(4 * j + r, x), w, top[n], total);
+        if (n * 16 + i < rows) {
+          if (j == 0) {
+            s_top[wave][n * 16 + i] = top[n];
+            s_sum[wave][n * 16 + i] = total;
           }
-      }
-      return;
-    }
-    if (!first) lds_sync();  // the last segment's results have been read
+          float* to = s_o[wave][n * 16 + i];
 #pragma unroll
-    for (int n = 0; n < NT; ++n) {
-      const float total = sum_over_groups(sum[n]);
-      if (n * 16 + i < rows) {
-        if (j == 0) {
-          s_top[wave][n * 16 + i] = top[n];
-          s_sum[wave][n * 16 + i] = total;
-        }
-        float* to = s_o[wave][n * 16 + i];
+          for (int r = 0; r < 4; ++r)
 #pragma unroll
-        for (int r = 0; r < 4; ++r)
+            for (int x = 0; x < VW / 4; ++x) {
+              f32x4 w;
 #pragma unroll
-          for (int x = 0; x < VW / 4; ++x) {
-            f32x4 w;
-#pragma unroll
-            for (int e = 0; e < 4; ++e) w[e] = o[n][4 * x + e][r];
-            *reinterpret_cast<f32x4*>(to + L::dim(4 * j + r, x)) = w;
-          }
-      }
-    }
-    lds_sync();
-    const bool complete = !LINE || (g.unit == 0 && g.stop == g.sp.units);
-    float* slot = A.part + (static_cast<int64_t>(blockIdx.x) * 2 + (first ? 0 : 1)) * A.slot_floats;
-    for (int e = tid; e < rows * (D / 4); e += kThreads) {
-      const int r = e / (D / 4), d = e % (D / 4) * 4;
-      float m = s_top[0][r];
-#pragma unroll
-      for (int w = 1; w < kDecodeWaves; ++w) m = fmaxf(m, s_top[w][r]);
-      float total = 0.f;
-      f32x4 x{};
-#pragma unroll
-      for (int w = 0; w < kDecodeWaves; ++w) {
-        const float c = exp2f(s_top[w][r] - m);
-        total += c * s_sum[w][r];
-        const f32x4 y = *reinterpret_cast<const f32x4*>(&s_o[w][r][d]);
-#pragma unroll
-        for (int v = 0; v < 4; ++v) x[v] += c * y[v];
-      }
-      if (complete) {
-        finish<T>(A, g.seq, hq0 + r, d, x, m, total);
-      } else {
-        *reinterpret_cast<f32x4*>(slot + r * D + d) = x;
-        if (d == 0) {
-          slot[A.rows * D + r] = m;
-          slot[A.rows * (D + 1) + r] = total;
+              for (int e = 0; e < 4; ++e) w[e] = o[n][4 * x + e][r];
+              *reinterpret_cast<f32x4*>(to + L::dim(4 * j + r, x)) = w;
+            }
         }
       }
+      lds_sync();
+      const bool complete = !LINE || (g.unit == 0 && g.stop == g.sp.units);
+      float* slot = A.part + (static_cast<int64_t>(blockIdx.x) * 2 + (first ? 0 : 1)) * A.slot_floats;
+      for (int e = tid; e < rows * (D / 4); e += kThreads) {
+        const int r = e / (D / 4), d = e % (D / 4) * 4;
+        float m = s_top[0][r];
+#pragma unroll
+        for (int w = 1; w < kDecodeWaves; ++w) m = fmaxf(m, s_top[w][r]);
+        float total = 0.f;
+        f32x4 x{};
+#pragma unroll
+        for (int w = 0; w < kDecodeWaves; ++w) {
+          const float c = exp2f(s_top[w][r] - m);
+          total += c * s_sum[w][r];
+          const f32x4 y = *reinterpret_cast<const f32x4*>(&s_o[w][r][d]);
+#pragma unroll
+          for (int v = 0; v < 4; ++v) x[v] += c * y[v];
+        }
+        if (complete) {
+          finish<T>(A, g.seq, hq0 + r, d, x, m, total);
+        } else {
+          *reinterpret_cast<f32x4*>(slot + r * D + d) = x;
+          if (d == 0) {
+            slot[A.rows * D + r] = m;
+            slot[A.rows * (D + 1) + r] = total;
+          }
+        }
+      }
+      if (!follows) return;
+      g = f;
+      have = hi > sub;
     }
-    if (!follows) return;
-    g = f;
-    have = hi > sub;
+  };
+  if constexpr (LINE && NT == 1) {
+    if (shared) return stream(std::integral_constant<int, 0>{});
   }
+  stream(std::integral_constant<int, kNontemporal>{});
 }
 
 // The shares of an item that several workgroups took, joined in the order of the line by the

@@ -193,6 +193,31 @@ def test_thousands_of_sequences_most_of_them_empty(dev):
     assert (out.cpu()[~full] == 0).all() and (lse.cpu()[:, ~full] == -math.inf).all() and torch.isfinite(lse.cpu()[:, full]).all()
 
 
+@pytest.mark.parametrize("dtype,d,G,t", [(BF16, 128, 4, 3300), (BF16, 64, 1, 6500), (F32, 128, 3, 3300), (F32, 64, 16, 3300),
+                                         (BF16, 128, 20, 3300)])
+def test_long_sequences_that_share_most_pages(dev, dtype, d, G, t):
+    """Rows that one prompt's pages serve, beside one with its own and two prompts in turn: each
+    workgroup's share is long and its pages are shared, or not.  The same pages held once for each
+    row give the same bits."""
+    say(f"decode shared {dtype} d={d} G={G}")
+    base, g = build(dev, dtype, 4, d, 64, 64, [t, t - 900, t - 70], 20)
+    src = [0] * 29 + [1] + [2] * 20 + [0, 2] * 7
+    table = base.page_table[src].contiguous()
+    lens = base.seq_lens[src] - torch.arange(64, dtype=torch.int32, device=dev)
+    cache = SeqKVCache(base.k_pages, base.v_pages, table, lens, 64)
+    q = queries(dev, dtype, 64, 4 * G, d, g)
+    out, lse = omnimem_decode_attn(cache, q)
+    own = table.long().clamp(min=0).flatten()
+    apart = SeqKVCache(base.k_pages[own], base.v_pages[own],
+                       torch.arange(own.numel(), dtype=torch.int32, device=dev).view_as(table), lens, 64)
+    out2, lse2 = omnimem_decode_attn(apart, q)
+    assert torch.equal(out, out2) and torch.equal(lse, lse2)
+    some = [0, 28, 29, 49, 50, 63]
+    O, L, ob, lb = seq_oracle.decode(q[some], cache.k_pages, cache.v_pages, table[some], lens[some], 64, 64, 0, d ** -0.5)
+    assert ((out[some].double().cpu() - O).abs() <= ob).all()
+    assert ((lse[:, some].double().cpu() - L).abs() <= lb).all()
+
+
 def test_strided_queries_and_given_buffers(dev):
     cache, g = build(dev, BF16, 2, 128, 64, 64, [100, 300, 5], 12)
     qkv = queries(dev, BF16, 3, 4 * 3, 128, g).view(3, 3, 4, 128)
