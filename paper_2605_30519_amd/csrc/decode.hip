@@ -6,7 +6,7 @@
 // and no barrier between loads and products, tiles of 8 KB of K and 8 KB of V a wave straight
 // into MFMA operand registers, the next tile's loads issued as soon as the registers of the
 // present one are read.  Four rollouts of 47 to 94 thousand tokens, 12 heads of 128, bf16
-// (1.66 GB): 247 us, 6.7 TB/s, with plain instead of nontemporal loads 283; 48 sequences of 100
+// (1.66 GB): 248 us, 6.7 TB/s, with plain instead of nontemporal loads 272; 48 sequences of 100
 // to 16,000 tokens, 40 query heads over 8 (617 MB): 106 us, 5.8 TB/s.
 //
 // Split.  An item is a (sequence, key/value head, tile of up to 32 query heads); its units of
