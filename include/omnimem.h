@@ -477,8 +477,8 @@ size_t omnimem_decode_workspace_bytes(const omnimem_seq_cache_t* sc, int32_t num
  * The work is split over the sequences' real lengths, so the order of the sums, and the
  * last bits of O, depend on all lengths of the batch; whether pages are shared changes
  * the time alone (long sequences that share pages are read faster in rows next to each
- * other).  bf16: as omnimem_sparse_attn (P is rounded to bf16 before PV); f32: fp32
- * arithmetic throughout.
+ * other).  bf16: P enters PV in two bf16 pieces, 2^-14 off, and sums are fp32, so that O is
+ * off by little more than its rounding; f32: fp32 arithmetic throughout.
  */
 omnimem_status_t omnimem_decode_attn(const omnimem_seq_cache_t* sc, const void* q, int64_t q_stride,
                                      int32_t num_q_heads, int32_t window, float scale, void* out, float* lse,

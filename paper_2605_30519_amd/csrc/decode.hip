@@ -36,6 +36,7 @@ constexpr int kMinUnits = 4;      // units of a share: one for each wave
 constexpr float kLowest = -FLT_MAX;  // below every score: a row without keys keeps sum 0
 constexpr int kAskUnits = 64;     // units of a share from which it is asked whether pages are shared
 constexpr int kNontemporal = 2;   // cache policy of a buffer load: read once
+constexpr float kBelow = 1.f - 1.f / 256;  // of a probability: what its first bf16 piece is cut from
 
 struct DecodeArgs {
   SeqGeom g;
@@ -161,17 +162,28 @@ struct Tile<uint16_t, D> {
     return c;
   }
   // O^T row tiles m: dims VW * (row of the tile) + m.  A word of the A operand holds dim m of two
-  // keys, picked out of the keys' rows.  P is rounded to bf16, as in the library's other kernels:
-  // 1.6e-3 off fp64 in norm, which is the output's own rounding; the sums stay fp32.
+  // keys, picked out of the keys' rows.  P goes in two bf16 pieces: the first is a truncation of
+  // somewhat less than P, between P (1 - 3 * 2^-8) and P, so that the second is not 0 and an
+  // infinite value stays infinite in the sum; the second, rounded by 2^-8 of itself, leaves P
+  // 3 * 2^-16 off, and the output's rounding is what O is off by.
   template <int NT>
   __device__ __forceinline__ void pv(const f32x4 (&p)[NT][RT], f32x4 (&o)[NT][VW]) const {
 #pragma unroll
     for (int b = 0; b < KB; ++b) {
-      bf16x8 pb[NT];
+      bf16x8 high[NT], low[NT];
 #pragma unroll
-      for (int n = 0; n < NT; ++n)
+      for (int n = 0; n < NT; ++n) {
+        u32x4 w;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) pb[n][e] = static_cast<__bf16>(p[n][2 * b + e / 4][e % 4]);
+        for (int e = 0; e < 8; e += 2) {
+          const f32x4 x = p[n][2 * b + e / 4];
+          const uint32_t a0 = __float_as_uint(x[e % 4] * kBelow), a1 = __float_as_uint(x[e % 4 + 1] * kBelow);
+          w[e / 2] = __builtin_amdgcn_perm(a1, a0, 0x07060302u);
+          low[n][e] = static_cast<__bf16>(x[e % 4] - __uint_as_float(a0 & 0xffff0000u));
+          low[n][e + 1] = static_cast<__bf16>(x[e % 4 + 1] - __uint_as_float(a1 & 0xffff0000u));
+        }
+        high[n] = __builtin_bit_cast(bf16x8, w);
+      }
 #pragma unroll
       for (int m = 0; m < VW; ++m) {
         u32x4 w;
@@ -179,8 +191,10 @@ struct Tile<uint16_t, D> {
         for (int e = 0; e < 4; ++e)
           w[e] = __builtin_amdgcn_perm(v[b][2 * e + 1][m / 2], v[b][2 * e][m / 2], m % 2 ? 0x07060302u : 0x05040100u);
 #pragma unroll
-        for (int n = 0; n < NT; ++n)
-          o[n][m] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, w), pb[n], o[n][m], 0, 0, 0);
+        for (int n = 0; n < NT; ++n) {
+          o[n][m] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, w), high[n], o[n][m], 0, 0, 0);
+          o[n][m] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, w), low[n], o[n][m], 0, 0, 0);
+        }
       }
     }
   }
@@ -387,12 +401,13 @@ __global__ __launch_bounds__(kThreads, 2) void k_decode(const DecodeArgs A) {
 
   // The wave's tiles form one stream over the segments: while a segment's last tile is worked
   // on, the first one of the next segment is on its way.  The stream's own segment is f, at
-  // most one in front of g; its units are looked up 64 at a time, lane l the l-th one's page,
-  // first token row, and rows in use.
+  // most one in front of g; its units are looked up 64 at a time, lane l the l-th one's page and,
+  // in one register, its first token row and its rows in use.
   Segment f = g;
   int next = f.unit + (BY_WAVE ? 0 : wave);
   uint64_t mask = 0;
-  int l_page = 0, l_row = 0, l_lo = 0, l_hi = 0;
+  int l_page = 0;
+  uint32_t l_rows = 0;
   int lo = 0, hi = 0, sub = 0;  // the tile's unit: rows in use, rows before the tile
   int64_t row = 0;              // the unit's first row in the pools
   auto look_up = [&]() {
@@ -401,14 +416,15 @@ __global__ __launch_bounds__(kThreads, 2) void k_decode(const DecodeArgs A) {
     if (ok) {
       const int in_block = block_shift(A.g) - (UT == 64 ? 6 : 5);  // log2 of a block's units
       const int b = f.sp.block + (u >> in_block);
-      l_row = (u & ((1 << in_block) - 1)) * UT;
+      const int l_row = (u & ((1 << in_block) - 1)) * UT;
       const int c = A.g.Bpc == 1 ? b : b / A.g.Bpc;
       const int in = (b - c * A.g.Bpc) * A.g.B + l_row;
       const int tok = c * A.g.S + in;
       l_page = A.g.table[static_cast<int64_t>(f.seq) * A.g.M + b];
-      l_hi = min(UT, min(A.g.S - in, f.sp.end - tok));
-      l_lo = max(0, f.sp.begin - tok);
+      const int l_hi = min(UT, min(A.g.S - in, f.sp.end - tok));
+      const int l_lo = max(0, f.sp.begin - tok);
       ok = l_page >= 0 && l_page < A.g.num_pages && l_lo < l_hi;
+      l_rows = static_cast<uint32_t>(l_row << 16 | l_hi) | static_cast<uint32_t>(l_lo) << 8;  // where ok: <= 96, 64, 63
     }
     mask = __ballot(ok);
     next += kWave * TEAM;
@@ -427,10 +443,11 @@ __global__ __launch_bounds__(kThreads, 2) void k_decode(const DecodeArgs A) {
     }
     const int at = __builtin_ctzll(mask);
     mask &= mask - 1;
-    lo = __builtin_amdgcn_readlane(l_lo, at);
-    hi = __builtin_amdgcn_readlane(l_hi, at);
+    const int rows = __builtin_amdgcn_readlane(l_rows, at);
+    lo = rows >> 8 & 0xff;
+    hi = rows & 0xff;
     row = (static_cast<int64_t>(__builtin_amdgcn_readlane(l_page, at)) * A.a.H + f.head / A.head_tiles) * A.g.B +
-          __builtin_amdgcn_readlane(l_row, at);
+          (rows >> 16);
     sub = lo / L::KEYS * L::KEYS;
     return true;
   };
