@@ -164,7 +164,7 @@ constexpr int kSeqThreads = 512;
 
 struct SeqScratch {
   uint32_t* held;  // pages that a row names without writing to them next
-  uint32_t* tail;  // pages that a row will write to (update)
+  uint32_t* tail;  // pages that a row will write to; null, as the next two, without new rows
   int* first;      // the lowest such row of a page of `tail`
   RowPlan* rows;
   int64_t words;
@@ -295,7 +295,7 @@ __global__ __launch_bounds__(256) void k_seq_clear(const SeqGeom g, const SeqUpd
   const int64_t id = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x, n = static_cast<int64_t>(gridDim.x) * 256;
   for (int64_t w = id; w < x.words; w += n) {
     x.held[w] = 0;
-    if (a.num_new > 0) x.tail[w] = 0;
+    if (x.tail != nullptr) x.tail[w] = 0;
   }
   for (int64_t r = id; r < a.num_new; r += n) {
     const RowPlan p = plan_row(g, a, static_cast<int>(r));
@@ -556,8 +556,10 @@ __global__ __launch_bounds__(kOneThreads) void k_seq_compact_one(const SeqGeom g
 
 SeqScratch scratch_of(const SeqPlan& p, void* workspace) {
   char* ws = static_cast<char*>(workspace);
-  return SeqScratch{reinterpret_cast<uint32_t*>(ws + p.off_held), reinterpret_cast<uint32_t*>(ws + p.off_tail),
-                    reinterpret_cast<int*>(ws + p.off_first), reinterpret_cast<RowPlan*>(ws + p.off_rows), p.words};
+  uint32_t* held = reinterpret_cast<uint32_t*>(ws + p.off_held);
+  if (!p.growing) return SeqScratch{held, nullptr, nullptr, nullptr, p.words};
+  return SeqScratch{held, reinterpret_cast<uint32_t*>(ws + p.off_tail), reinterpret_cast<int*>(ws + p.off_first),
+                    reinterpret_cast<RowPlan*>(ws + p.off_rows), p.words};
 }
 
 constexpr int kSeqMaxWgs = 256;

@@ -123,12 +123,13 @@ omnimem_status_t plan_seq(const SeqGeom& g, int32_t num_new, SeqPlan& p) {
     return OMNIMEM_EINVAL;  // entries, and the pages that rows ask for, are counted in 31 bits
   const int rows = num_new > 0 ? num_new : g.N;
   p.one = g.num_pages <= kOnePages && rows <= kOneRows && static_cast<int64_t>(rows) * g.M <= kOneEntries;
+  p.growing = num_new > 0;
   p.words = (g.num_pages + 31) / 32;
   const size_t map = align256(static_cast<size_t>(p.words) * 4);
   p.off_held = 0;
   p.off_tail = map;
-  p.off_first = p.off_tail + (num_new > 0 ? map : 0);
-  p.off_rows = p.off_first + (num_new > 0 ? align256(static_cast<size_t>(g.num_pages) * 4) : 0);
+  p.off_first = p.off_tail + (p.growing ? map : 0);
+  p.off_rows = p.off_first + (p.growing ? align256(static_cast<size_t>(g.num_pages) * 4) : 0);
   p.total = p.one ? 256 : p.off_rows + align256(static_cast<size_t>(num_new) * sizeof(RowPlan)) + 512;
   return OMNIMEM_OK;
 }

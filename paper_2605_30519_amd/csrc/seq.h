@@ -85,8 +85,8 @@ struct CopyLaunch {
   int max_pairs;
 };
 
-// Scratch of the table updates: two bitmaps of the pool's pages, one word per page (the
-// lowest growing row of a page) and the new rows' records.
+// Scratch of the table updates: a bitmap of the pool's pages, and where there are new rows a
+// second one, one word per page (the lowest growing row of a page) and the rows' records.
 // A workgroup with its state in LDS does small tables instead.  One launch costs the host 6 us
 // less than three; on the GPU, 16 rows of 18 entries take 7.1 us against 10.6 (update; compaction
 // 5.2 / 8.6), 16 of 252 9.2 / 11.9 (9.3 / 13.3), 8 of 939 11.6 / 12.0 (13.4 / 11.5), 256 of 65 27 / 14
@@ -96,6 +96,7 @@ constexpr int64_t kOneEntries = 8192;
 
 struct SeqPlan {
   bool one;
+  bool growing;   // new rows may write to pages: a second bitmap, `first` and `rows` have their place
   int64_t words;  // 32-page words of a bitmap
   size_t off_held, off_tail, off_first, off_rows, total;
 };

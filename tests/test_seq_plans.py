@@ -1,0 +1,45 @@
+"""The sequence cache's work plans on the CPU, from a host-only build: what a call uses of its
+workspace lies inside the size that it asks for."""
+import ctypes
+import os
+import subprocess
+
+import pytest
+
+from conftest import ROOT
+from paper_2605_30519_amd import omnimem as om
+
+FAKE = 0x10000  # aligned, never dereferenced
+
+
+@pytest.fixture(scope="module")
+def shim(tmp_path_factory):
+    so = str(tmp_path_factory.mktemp("plans") / "seq_plan_shim.so")
+    subprocess.run(["g++", "-O1", "-std=c++17", "-shared", "-fPIC", os.path.join(ROOT, "tests", "seq_plan_shim.cpp"),
+                    os.path.join(ROOT, "paper_2605_30519_amd", "csrc", "seq.cpp"), "-o", so], check=True)
+    return ctypes.CDLL(so)
+
+
+def table(n, m, pages):
+    return om.omnimem_seq_table_t(n, m, 64, 64, pages, FAKE, FAKE)
+
+
+@pytest.mark.parametrize("new", [0, 1, 5, 1300])
+@pytest.mark.parametrize("n,m,pages", [(3, 10, 30), (256, 65, 4000), (2000, 2, 100), (3, 10, 16385), (7, 70, 1 << 20),
+                                       (0, 5, 20000), (5000, 9, 0)])
+def test_update_stays_inside_its_workspace(shim, n, m, pages, new):
+    """The bitmaps, a word per page and the rows' records lie one behind the other; without new rows
+    only the first bitmap has a place, and nothing else may be used."""
+    out = (ctypes.c_int64 * 9)()
+    assert shim.shim_update_plan(ctypes.byref(table(n, m, pages)), new, out) == 0
+    one, growing, words, held, tail, first, rows, total, record = out
+    rows_here = new or n
+    assert one == (pages <= 16384 and rows_here <= 1024 and rows_here * m <= 8192)
+    assert growing == (new > 0) and words == -(-pages // 32)
+    if one:
+        return                                                   # all in one workgroup's LDS
+    ends = [(held, 4 * words)]
+    if growing:
+        ends += [(tail, 4 * words), (first, 4 * pages), (rows, record * new)]
+    for (at, size), behind in zip(ends, [a for a, _ in ends[1:]] + [total]):
+        assert at % 256 == 0 and at + size <= behind
