@@ -85,7 +85,7 @@ omnimem_status_t plan_decode(const omnimem_seq_cache_t* sc, const SeqGeom& g, in
   // tokens of one run lie in no more than a B-th of them, and two, blocks.
   int64_t blocks = g.M;
   if (window > 0) {
-    const int64_t runs = g.Bpc == 1 && g.S == g.B ? 1 : window / g.S + 2;
+    const int64_t runs = g.Bpc == 1 && g.S == g.B ? 1 : int64_t{window} / g.S + 2;
     blocks = window / g.B + 2 * runs < blocks ? window / g.B + 2 * runs : blocks;
   }
   const int64_t unit = sc->dtype == OMNIMEM_BF16 && sc->head_dim == 64 ? 64 : 32;

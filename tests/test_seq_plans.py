@@ -3,6 +3,7 @@ workspace lies inside the size that it asks for."""
 import ctypes
 import os
 import subprocess
+import sys
 
 import pytest
 
@@ -43,3 +44,34 @@ def test_update_stays_inside_its_workspace(shim, n, m, pages, new):
         ends += [(tail, 4 * words), (first, 4 * pages), (rows, record * new)]
     for (at, size), behind in zip(ends, [a for a, _ in ends[1:]] + [total]):
         assert at % 256 == 0 and at + size <= behind
+
+
+LARGE_WINDOWS = r'''
+import ctypes, sys
+sys.path[:0] = [{repo!r}]
+from paper_2605_30519_amd import omnimem as om
+
+f = om._configure(ctypes.CDLL({so!r}), required=False).omnimem_decode_workspace_bytes
+big = 2 ** 31 - 1
+for n, m in ((2, 5000), (4, 100000), (700, 3)):
+    for dtype, d in ((0, 64), (0, 128), (1, 64), (1, 128)):
+        for B in (64, 128):
+            for S in (1, 2, 3, 63, 64, 65, 100, 4680, big):
+                cache = om.omnimem_seq_cache_t(om.omnimem_seq_table_t(n, m, B, S, 30, None, None), dtype, 2, d, None, None)
+                whole = f(ctypes.byref(cache), 4, 0)
+                for window in (big, big - 1, big - 2, big - 3, 2 ** 30):
+                    assert f(ctypes.byref(cache), 4, window) == whole, (n, m, dtype, d, B, S, window)
+print("windows ok")
+'''
+
+
+def test_a_window_past_every_row_is_no_window(tmp_path):
+    """The largest windows with chunks of a token and more take what the whole rows take, with no
+    signed overflow on the way (UndefinedBehaviorSanitizer, in a child interpreter)."""
+    so = str(tmp_path / "seq_shim.so")
+    subprocess.run(["g++", "-O1", "-std=c++17", "-shared", "-fPIC", "-fsanitize=undefined", "-static-libubsan",
+                    "-fno-sanitize-recover=undefined", os.path.join(ROOT, "tests", "seq_shim.cpp"),
+                    os.path.join(ROOT, "paper_2605_30519_amd", "csrc", "seq.cpp"), "-o", so], check=True)
+    r = subprocess.run([sys.executable, "-c", LARGE_WINDOWS.format(repo=ROOT, so=so)], capture_output=True, text=True,
+                       timeout=300)
+    assert r.returncode == 0 and "windows ok" in r.stdout, (r.stdout[-2000:], r.stderr[-4000:])
