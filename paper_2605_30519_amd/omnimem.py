@@ -1001,7 +1001,8 @@ def omnimem_seq_workspace_bytes(page_table: torch.Tensor, seq_lens: torch.Tensor
 
 
 def _seq_out(out: Optional[SeqUpdate], n: int, m: int, pairs: int, lens, dev) -> SeqUpdate:
-    """The caller's buffers, checked, or new ones, cut from one allocation (lens: given)."""
+    """The caller's buffers, checked, or new ones, cut from one allocation.  lens: the lengths of a
+    call that writes none, which are the result's whatever `out` holds in their place."""
     if out is None:
         own = n if lens is None else 0
         flat = torch.empty(n * m + own + 2 * pairs + 4, dtype=torch.int32, device=dev)
@@ -1013,9 +1014,11 @@ def _seq_out(out: Optional[SeqUpdate], n: int, m: int, pairs: int, lens, dev) ->
         return SeqUpdate(flat.as_strided((n, m), (m, 1), 0), lens, flat.as_strided((pairs, 2), (2, 1), at),
                          flat.as_strided((4,), (1,), at + 2 * pairs))
     _check_tensor("out.page_table", out.page_table, (n, m), torch.int32)
-    _check_tensor("out.seq_lens", out.seq_lens, (n,), torch.int32)
     _check_tensor("out.copies", out.copies, (pairs, 2), torch.int32)
     _check_tensor("out.info", out.info, (4,), torch.int32)
+    if lens is not None:
+        return SeqUpdate(out.page_table, lens, out.copies, out.info)
+    _check_tensor("out.seq_lens", out.seq_lens, (n,), torch.int32)
     return out
 
 
@@ -1068,7 +1071,8 @@ def omnimem_seq_compact(page_table: torch.Tensor, seq_lens: torch.Tensor, num_pa
                         workspace: Optional[torch.Tensor] = None, stream=None) -> SeqUpdate:
     """The tables with all pages in use moved to the front of the pool; the moves to make are
     result.copies, for omnimem_copy_pages(..., result.copies, result.info) on every layer, and
-    result.info[1] pages are in use.  The lengths stay (result.seq_lens is seq_lens)."""
+    result.info[1] pages are in use.  The lengths stay: result.seq_lens is seq_lens, also with buffers
+    of the caller's (out), whose seq_lens is neither read nor written."""
     dev = page_table.get_device() if isinstance(page_table, torch.Tensor) else -1
     if dev >= 0 and (stream is not None or dev != _current_device()):
         with _elsewhere(page_table, stream):
