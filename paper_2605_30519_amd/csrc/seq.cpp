@@ -99,6 +99,7 @@ omnimem_status_t plan_decode(const omnimem_seq_cache_t* sc, const SeqGeom& g, in
                                                               : DecodeSplit::kLine;
   const int64_t most = items * (units + kItemOverhead);
   const int64_t wgs = items > kDecodeWgs ? kDecodeManyWgs : kDecodeWgs;
+  if (most > wgs * 0x7fffffff) return OMNIMEM_EINVAL;  // a workgroup's share of the line in 31 bits
   p.wgs = static_cast<int>(p.split == DecodeSplit::kLine   ? (most < wgs ? most : wgs)
                            : p.split == DecodeSplit::kItem ? items
                                                            : (items + kDecodeWaves - 1) / kDecodeWaves);

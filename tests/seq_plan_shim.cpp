@@ -23,3 +23,21 @@ extern "C" omnimem_status_t shim_update_plan(const omnimem_seq_table_t* st, int3
   for (int i = 0; i < 9; ++i) out[i] = all[i];
   return s;
 }
+
+// {split (0: line), wgs, items, most units of an item} of a decode call; the units are the table's or
+// the window's.
+extern "C" omnimem_status_t shim_decode_plan(const omnimem_seq_cache_t* sc, int32_t heads, int32_t window, int64_t* out) {
+  SeqGeom g;
+  DecodePlan p;
+  DecodeLaunch a;
+  void* const fake = reinterpret_cast<void*>(0x10000);
+  const omnimem_status_t s = check_decode_attn(sc, fake, static_cast<int64_t>(heads) * sc->head_dim, heads, window, 0.1f,
+                                               fake, nullptr, fake, static_cast<size_t>(1) << 62, g, p, a);
+  if (s != OMNIMEM_OK) return s;
+  const int unit = sc->dtype == OMNIMEM_BF16 && sc->head_dim == 64 ? 64 : 32;
+  out[0] = static_cast<int64_t>(p.split);
+  out[1] = p.wgs;
+  out[2] = static_cast<int64_t>(g.N) * sc->num_heads * p.head_tiles;
+  out[3] = static_cast<int64_t>(g.M) * (g.B / unit);
+  return s;
+}

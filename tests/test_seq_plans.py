@@ -75,3 +75,24 @@ def test_a_window_past_every_row_is_no_window(tmp_path):
     r = subprocess.run([sys.executable, "-c", LARGE_WINDOWS.format(repo=ROOT, so=so)], capture_output=True, text=True,
                        timeout=300)
     assert r.returncode == 0 and "windows ok" in r.stdout, (r.stdout[-2000:], r.stderr[-4000:])
+
+
+def test_a_share_of_the_line_is_counted_in_31_bits(shim):
+    """Whatever the checks accept leaves every workgroup of a decode call a share below 2^31 units: an
+    item counts its units and three more."""
+    out = (ctypes.c_int64 * 4)()
+    taken = refused = 0
+    for heads in (1, 256, 257, 511, 512, 513, 1024, 4096, 1 << 17, 1 << 18, 1 << 19, 1 << 20):
+        for m in (1, 11, 1000, 1 << 15, 1 << 20, 1 << 21, 1 << 22, (1 << 25) - 100, 1 << 29, (1 << 30) - 32):
+            for S in (1, 64):
+                for dtype, d in ((0, 64), (1, 64)):
+                    for n in (1, 3):
+                        cache = om.omnimem_seq_cache_t(om.omnimem_seq_table_t(n, m, 64, S, 1, FAKE, FAKE), dtype, heads, d,
+                                                       FAKE, FAKE)
+                        if shim.shim_decode_plan(ctypes.byref(cache), heads, 0, out) != 0:
+                            refused += 1
+                            continue
+                        taken += 1
+                        split, wgs, items, units = out
+                        assert split != 0 or -(-items * (units + 3) // wgs) < 2 ** 31, (heads, m, S, dtype, n)
+    assert taken > 200 and refused > 50
