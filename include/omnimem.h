@@ -436,7 +436,8 @@ int32_t omnimem_lru_slot_of(const omnimem_lru_t* lru, int32_t head, int32_t chun
  *
  * All calls below read the table and the lengths on the device: a length below 0
  * counts as 0, one beyond the row's capacity as the capacity, M div Bpc chunks and
- * the M mod Bpc blocks after them; a page id < 0 or >= num_pages is not resident.
+ * the M mod Bpc blocks after them (but omnimem_append_kv places its rows by the length
+ * as it stands); a page id < 0 or >= num_pages is not resident.
  */
 typedef struct {
   int32_t num_seqs;     /* N >= 0 */
@@ -488,7 +489,8 @@ omnimem_status_t omnimem_decode_attn(const omnimem_seq_cache_t* sc, const void* 
  * Writes new tokens' keys and values into the pages of their sequences.  The rows
  * starts[i] to starts[i+1] of k and v are the last starts[i+1] - starts[i] tokens of
  * sequence i: seq_lens already counts them, and their blocks have pages of their own
- * (omnimem_seq_update sees to both).  Rows in front of a sequence's first token,
+ * (omnimem_seq_update sees to both).  The last row is token seq_lens[i] - 1 also where the
+ * length is beyond the row's capacity.  Rows in front of a sequence's first token,
  * behind its capacity or in a block that is not resident are dropped, and nothing
  * else of the pool is written.  Two tokens in one slot (a page listed twice): either.
  * k, v:   `tokens` rows [H][d] of sc->dtype, row t at k + t*k_stride elements (v: v_stride;
