@@ -1,13 +1,13 @@
 // decode.hip -- attention of one new token per sequence over a paged cache, for gfx950:
 //   O[i][h] = sum_t softmax_t(scale <q_i, k_t>) v_t over the tokens of sequence i.
 //
-// A key and a value serve the G query heads of their head alone, 2 G flops a byte of bf16, so
+// A key and a value serve the G query heads of their head alone, G flops a byte of bf16, so
 // the kernel is bound by the stream of K and V from memory and built to keep it full: no LDS
 // and no barrier between loads and products, tiles of 8 KB of K and 8 KB of V a wave straight
 // into MFMA operand registers, the next tile's loads issued as soon as the registers of the
 // present one are read.  Four rollouts of 47 to 94 thousand tokens, 12 heads of 128, bf16
-// (1.66 GB): 248 us, 6.7 TB/s, with plain instead of nontemporal loads 272; 48 sequences of 100
-// to 16,000 tokens, 40 query heads over 8 (617 MB): 106 us, 5.8 TB/s.
+// (1.66 GB): 247 us with the join, 6.7 TB/s, with plain instead of nontemporal loads 272; 48
+// sequences of 100 to 16,000 tokens, 40 query heads over 8 (617 MB): 101 us with the join, 6.1 TB/s.
 //
 // Split.  An item is a (sequence, key/value head, tile of up to 32 query heads); its units of
 // 32 tokens (64 for bf16 heads of 64) follow one another on a line of all items' units, and
@@ -15,9 +15,9 @@
 // mix of lengths loads every workgroup alike and lengths stay on the device (a captured graph
 // replays with others).  The four waves take a segment's units in turn and meet in LDS; an
 // item that several workgroups share leaves (O, max, sum) a share in the workspace, which
-// k_decode_join adds up in the order of the line, in a launch of its own (4 us): workgroups
+// k_decode_join adds up in the order of the line, in a launch of its own (4 to 5 us): workgroups
 // that hand results on within a launch pay more for the caches between the dies.  With 64
-// instead of 32 tokens a unit the waves' loads differ more (115 us for the 48 sequences).
+// instead of 32 tokens a unit the waves' loads differ more (5% for the 48 sequences).
 #include <float.h>
 
 #include "device_common.h"
@@ -490,8 +490,8 @@ __global__ __launch_bounds__(kThreads, 2) void k_decode(const DecodeArgs A) {
   load_q();
   // A page of one sequence is read once, and marked so it comes a tenth faster; one that forked
   // sequences share is read by each, and serves them from the caches when it is not.  16 sequences
-  // of 30,000 tokens, 8 key heads, on one prompt's pages: 241 us marked, 147 not; 8,000 tokens: 69
-  // / 50.  On pages of their own, four of 47 to 94 thousand tokens, 12 key heads: 248 / 272.  So a
+  // of 30,000 tokens, 8 key heads, on one prompt's pages: 241 us marked, 150 not; 8,000 tokens: 69
+  // / 51.  On pages of their own, four of 47 to 94 thousand tokens, 12 key heads: 248 / 272.  So a
   // workgroup with a long share looks whether the row in front of or behind its first segment's has
   // the same pages.  A short share gains nothing (64 of 2,000: 45 both) and would wait 0.5 us for
   // the answer, and with more than 16 query heads to a key head a second loop costs registers that

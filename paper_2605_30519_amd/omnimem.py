@@ -861,6 +861,9 @@ class SeqKVCache:
 
 @dataclass
 class SeqUpdate:
+    """The tables of a next step.  Without buffers of the caller's (out) the tensors that a call makes
+    are views of one allocation, which lives as long as any of them: clone info or copies to
+    keep them without the table."""
     page_table: torch.Tensor  # [num_new, max_blocks] int32
     seq_lens: torch.Tensor    # [num_new] int32
     copies: torch.Tensor      # [.., 2] int32 (from, to), -1 behind the last one
