@@ -1,0 +1,471 @@
+"""The operators of the 8-bit sequence cache, as they are measured: new tokens' keys and values
+quantised into their pages, attention of one new token per sequence over such pages, rows of
+them read back, and pages copied with their scales.
+
+A case names one operator and its sizes.  `listed` holds the fixed ones, `draw` makes more of
+the same ranges, `prepare` builds what a program that generates many sequences has in hand
+before the call, `run` makes one pass (the plain form in elementary torch operations, or the
+library's entry points where `own` is true), and `exact` computes the same outputs in 64 bits.
+
+A page holds one block of B tokens for every key/value head: e4m3 codes [num_pages][H][B][d] of K
+and of V, and scales [num_pages][H][2], K's and V's; a value is code * scale.  Sequence i has a row
+of the page table [N][M] and a length.  Its tokens come in chunks of S: token t lies in block
+(t div S) * ceil(S / B) + (t mod S) div B, slot (t mod S) mod B, so that S = B is a contiguous
+sequence and S = 4,680 a history of video chunks.
+
+A scale is a power of two, the smallest 2^e (e >= -110) with |x| <= 448 * 2^e for the block's
+values x; where new tokens need a larger one than the tokens in front of them in the block
+have, those tokens' codes are rounded again to the larger one.  Codes are returned as float8
+tensors, that is as their values, beside the scales.
+"""
+import math
+
+import torch
+
+own = False
+DTYPES = {"bf16": torch.bfloat16, "fp32": torch.float32}
+E4M3 = torch.float8_e4m3fn
+LOWEST = -110   # of a scale's exponent
+DEV = "cuda"
+
+# op: decode = one query token per sequence; append = new tokens' K and V into the pages; read =
+# tokens' K and V out of them; copy = pages by a list of (source, target).
+# dtype = of queries and outputs, of new tokens, of tokens read back; N = sequences, Hq / H =
+# query heads / key-value heads, d = head size, B = tokens of a page, S = tokens of a chunk, lo..hi
+# = the shortest and longest sequence, window = only the last so many tokens (0: all), n = tokens
+# of a sequence that are appended or read (0 = ragged), first = read from somewhere inside the
+# sequence instead of its last tokens, layers and pairs = of a copy, extra = pool pages to a page
+# in use.
+
+
+def _case(name, op, dtype="bf16", N=1, Hq=12, H=12, d=128, B=64, S=64, lo=64, hi=64, window=0, n=1, first=False, layers=1,
+          pairs=0, extra=1.1):
+    c = {"op": op, "dtype": dtype, "N": N, "Hq": Hq, "H": H, "d": d, "B": B, "S": S, "lo": lo, "hi": hi, "window": window,
+         "n": n, "first": first, "layers": layers, "pairs": pairs, "extra": extra}
+    return {"name": name, **c} if name else c
+
+
+def listed():
+    return [
+        # the smallest call: one short sequence of a two-head layer, all launch latency
+        _case("decode_q8_tiny", "decode", "fp32", N=1, Hq=2, H=2, d=64, lo=300, hi=300),
+        # four rollouts of a 1.3B-shaped layer, 10 to 20 cached chunks each: the largest stream
+        _case("decode_q8_chunks", "decode", N=4, S=4680, lo=46800, hi=93600),
+        # a serving batch: 40 query heads over 8 key-value heads, lengths over two decades
+        _case("decode_q8_gqa_ragged", "decode", N=48, Hq=40, H=8, lo=100, hi=16000),
+        # a model with small heads of their own keys each, long contexts
+        _case("decode_q8_heads64", "decode", N=12, Hq=16, H=16, d=64, lo=4000, hi=30000),
+        # fp32 queries, small heads, eight query heads a key head, the last frame only
+        _case("decode_q8_fp32_window", "decode", "fp32", N=16, Hq=16, H=2, d=64, B=128, S=128, lo=1000, hi=6000, window=1560),
+        # one new token for each sequence of a batch, between two decoding steps
+        _case("append_q8_token", "append", N=64, lo=100, hi=16000, n=1),
+        # the chunk just generated, for eight rollouts of a 1.3B-shaped layer
+        _case("append_q8_chunk", "append", N=8, S=4680, lo=4680, hi=46800, n=4680),
+        # newly admitted prompts in fp32, some of them behind a prefix that is there
+        _case("append_q8_prompts", "append", "fp32", N=24, H=8, d=64, B=128, S=128, lo=30, hi=9000, n=0),
+        # the last chunk of four rollouts, for a step that attends over full precision
+        _case("read_q8_chunk", "read", N=4, S=4680, lo=46800, hi=93600, n=4680),
+        # some tokens from inside each sequence, in fp32
+        _case("read_q8_ragged", "read", "fp32", N=32, H=3, d=64, lo=50, hi=5000, n=0, first=True),
+        # the private copies that sixteen forked sequences need before they append
+        _case("copy_q8_fork", "copy", N=16, pairs=16, extra=4.0),
+        # the moves of a compaction, six layers of a 1.3B-shaped model at once
+        _case("copy_q8_moves", "copy", layers=6, pairs=300, extra=2.0),
+    ]
+
+
+def draw(rng):
+    def log(lo, hi):
+        return int(round(math.exp(rng.uniform(math.log(lo), math.log(hi)))))
+
+    while True:
+        op = rng.choice(["decode", "decode", "decode", "append", "append", "append", "read", "read", "copy"])
+        H = rng.choice([1, 2, 3, 4, 8, 8, 12, 12, 16, 40])
+        B = rng.choice([64, 64, 128])
+        S = rng.choice([B, B, B, 4680, 1560, log(B, 5000)])
+        hi = log(30, 100000)
+        lo = min(hi, log(1, hi))
+        dtype = rng.choice(["bf16", "bf16", "fp32"])
+        d = rng.choice([64, 128, 128])
+        if op == "decode":
+            c = _case(None, op, dtype, N=log(1, 128), Hq=H * rng.choice([1, 1, 2, 4, 5, 7, 8, 16, 24]), H=H, d=d, B=B, S=S, lo=lo,
+                      hi=hi, window=rng.choice([0, 0, 0, log(1, hi)]))
+        elif op in ("append", "read"):
+            c = _case(None, op, dtype, N=log(1, 128), H=H, d=d, B=B, S=S, lo=lo, hi=hi, n=rng.choice([1, 0, 0, log(1, hi)]),
+                      first=op == "read" and rng.random() < 0.5)
+        else:
+            c = _case(None, op, H=H, d=d, B=B, layers=rng.choice([1, 1, 2, 5]), pairs=log(1, 1000),
+                      extra=rng.choice([2.0, 3.0, 4.0]))
+        pool = 2 * _pool_pages(c) * c["layers"] * H * B * d
+        if pool > 2e9 or work(c)["bytes"] > 7e8 or (op == "decode" and c["N"] * _max_blocks(c) * H * B * d > 5.8e8):
+            continue
+        return c
+
+
+# ------------------------------------------------------------------------- sizes
+
+
+def _bpc(case):
+    return -(-case["S"] // case["B"])
+
+
+def _blocks(case, t):
+    """Blocks of a sequence of t tokens (a number or a tensor)."""
+    S, B = case["S"], case["B"]
+    return t // S * _bpc(case) + (t % S + B - 1) // B
+
+
+def _lens(case):
+    """The N lengths in ascending order, evenly spaced on a logarithmic scale."""
+    lo, hi, N = case["lo"], case["hi"], case["N"]
+    return [int(round(lo * (hi / lo) ** ((i + 0.5) / N))) for i in range(N)]
+
+
+def _max_blocks(case):
+    return _blocks(case, case["hi"]) + 1
+
+
+def _pool_pages(case):
+    if case["op"] == "copy":
+        return max(2, int(case["pairs"] * case["extra"]))
+    return max(2, int(sum(_blocks(case, t) for t in _lens(case)) * case["extra"]))
+
+
+def _news(case):
+    """Tokens of each sequence that are appended or read, of the lengths in ascending order."""
+    return [min(case["n"], t) if case["n"] else 1 + 7919 * (i + 1) % t for i, t in enumerate(_lens(case))]
+
+
+def work(case):
+    eb = 2 if case["dtype"] == "bf16" else 4
+    N, H, d, Hq = case["N"], case["H"], case["d"], case["Hq"]
+    if case["op"] == "decode":
+        read = [min(t, case["window"] or t) for t in _lens(case)]
+        pages = sum(_blocks(case, t) for t in read)
+        return {"bytes": 2 * sum(read) * H * d + 2 * N * Hq * d * eb + 4 * N * Hq + (4 + 8 * H) * pages,
+                "flops": 4 * sum(read) * Hq * d}
+    if case["op"] == "copy":
+        return {"bytes": 2 * case["layers"] * case["pairs"] * H * (2 * case["B"] * d + 8), "flops": 0}
+    new = _news(case)
+    pages = sum(_blocks(case, t) for t in new)
+    return {"bytes": 2 * sum(new) * H * d * (eb + 1) + (4 + 8 * H) * pages, "flops": 0}
+
+
+# ------------------------------------------------------------------------- inputs
+
+
+class _State:
+    pass
+
+
+def _pool(shape, g):
+    """Codes of random blocks [..., H, B, d], whose magnitudes differ from head to head and block to
+    block, and their scales [..., H]."""
+    x = torch.randn(shape, generator=g, device=DEV, dtype=torch.bfloat16).float()
+    x *= torch.exp(0.7 * torch.randn(shape[:-2] + (1, 1), generator=g, device=DEV))
+    e = _exponent(x.abs().amax((-1, -2)))
+    return (x * _power(-e)[..., None, None]).to(E4M3), _power(e)
+
+
+def prepare(case, seed):
+    g = torch.Generator(device=DEV)
+    g.manual_seed(int(seed))
+    st = _State()
+    st.case = case
+    N, H, d, B, M, P = case["N"], case["H"], case["d"], case["B"], _max_blocks(case), _pool_pages(case)
+    dt = DTYPES[case["dtype"]]
+    layers = (case["layers"],) if case["op"] == "copy" else ()
+    st.k, ks = _pool(layers + (P, H, B, d), g)
+    st.v, vs = _pool(layers + (P, H, B, d), g)
+    st.scales = torch.stack([ks, vs], -1).contiguous()
+
+    if case["op"] == "copy":
+        ids = torch.randperm(P, generator=g, device=DEV)
+        n = case["pairs"]
+        targets, sources = ids[:n], ids[n:]
+        # forked sequences share a source now and then; a target is written once
+        at = torch.randint(0, max(1, sources.numel()), (n,), generator=g, device=DEV)
+        st.pairs = torch.stack([sources[at], targets], 1).int().contiguous()
+        st.count = torch.full((4,), n, dtype=torch.int32, device=DEV)
+        return st
+
+    order = torch.randperm(N, generator=g, device=DEV)
+    lens = torch.tensor(_lens(case), device=DEV)[order]
+    nb = _blocks(case, lens)
+    here = torch.arange(M, device=DEV)[None] < nb[:, None]
+    ids = torch.randperm(P, generator=g, device=DEV)
+    at = torch.cumsum(here.flatten().int(), 0).view(N, M) - 1
+    st.table = torch.where(here, ids[at.clamp(0, P - 1)], -1).int().contiguous()
+    st.lens = lens.int()
+    if case["op"] in ("append", "read"):
+        new = torch.tensor(_news(case), device=DEV)[order]
+        st.T = sum(_news(case))
+        st.starts = torch.cat([new.new_zeros(1), torch.cumsum(new, 0)]).int()
+        if case["n"] == 1:
+            st.starts = None
+    if case["op"] == "read":
+        st.first = None
+        if case["first"]:
+            st.first = (torch.rand(N, generator=g, device=DEV) * (lens - new + 1)).int()
+        return st
+    if case["op"] == "append":
+        # K and V as a fused projection leaves them: rows of [3, H, d], Q first; tokens differ in size
+        qkv = torch.randn((st.T, 3, H, d), generator=g, device=DEV)
+        qkv = (qkv * torch.exp(0.7 * torch.randn((st.T, 1, H, 1), generator=g, device=DEV))).to(dt)
+        st.new_k, st.new_v = qkv[:, 1], qkv[:, 2]
+        return st
+    # a query looks for one of its sequence's tokens, which its score then lifts over the others
+    G = case["Hq"] // H
+    t = (torch.rand(N, generator=g, device=DEV) * lens).long()
+    S = case["S"]
+    page = st.table[torch.arange(N, device=DEV), t // S * _bpc(case) + t % S // B].long()
+    seek = st.k.view(torch.uint8)[page, :, t % S % B].view(E4M3).float() * ks[page][..., None]
+    seek = seek / seek.square().mean(-1, keepdim=True).sqrt().clamp(min=1e-3)
+    st.q = (torch.randn((N, case["Hq"], d), generator=g, device=DEV) + 0.6 * seek.repeat_interleave(G, 1)).to(dt)
+    return st
+
+
+# ------------------------------------------------------------------------- one pass
+
+
+def run(st):
+    if own:
+        return _own(st)
+    return {"decode": _plain_decode, "append": _plain_append, "read": _plain_read, "copy": _plain_copy}[st.case["op"]](st)
+
+
+def _own(st):
+    from paper_2605_30519_amd import (SeqKVCacheQ8, omnimem_append_kv_q8, omnimem_copy_pages_q8, omnimem_decode_attn_q8,
+                                      omnimem_read_kv_q8)
+    case = st.case
+    if case["op"] == "copy":
+        omnimem_copy_pages_q8(st.k, st.v, st.scales, st.pairs, st.count)
+        return st.k, st.v, st.scales
+    cache = SeqKVCacheQ8(st.k, st.v, st.scales, st.table, st.lens, case["S"])
+    if case["op"] == "append":
+        omnimem_append_kv_q8(cache, st.new_k, st.new_v, st.starts)
+        return st.k, st.v, st.scales
+    if case["op"] == "read":
+        return omnimem_read_kv_q8(cache, st.T, st.starts, first=st.first, dtype=DTYPES[case["dtype"]])
+    return omnimem_decode_attn_q8(cache, st.q, window=case["window"])
+
+
+def _power(e):
+    """2^e in fp32, by its bits."""
+    return ((e.int() + 127) << 23).view(torch.float32)
+
+
+def _exponent(most):
+    """The smallest e >= LOWEST with most <= 448 * 2^e."""
+    m, e = torch.frexp(most)
+    return torch.where(m <= 0.875, e - 9, e - 8).clamp(min=LOWEST)
+
+
+def _tokens(case, M):
+    """Token number of every slot of a row's M blocks [M * B], and whether the slot is one."""
+    S, B = case["S"], case["B"]
+    at = torch.arange(M * B, device=DEV)
+    block, slot = at // B, at % B
+    inside = block % _bpc(case) * B + slot
+    return block // _bpc(case) * S + inside, inside < S
+
+
+def _values(codes, pages, scale):
+    """Blocks of the pool in fp32."""
+    return codes.view(torch.uint8)[pages].view(E4M3).float() * scale[pages][..., None, None]
+
+
+def _plain_decode(st):
+    case = st.case
+    N, Hq, d = st.q.shape
+    P, H, B, _ = st.k.shape
+    M = st.table.shape[1]
+    tok, real = _tokens(case, M)
+    last = st.lens.long()[:, None]
+    ok = real & (tok < last)
+    if case["window"]:
+        ok = ok & (tok >= last - case["window"])
+    ok = ok & ((st.table >= 0) & (st.table < P)).repeat_interleave(B, 1)
+    pages = st.table.long().clamp(0, P - 1)
+    ok4 = ok[:, None, :, None]
+    k = _values(st.k, pages, st.scales[..., 0]).transpose(1, 2).reshape(N, H, M * B, d)
+    v = _values(st.v, pages, st.scales[..., 1]).transpose(1, 2).reshape(N, H, M * B, d).masked_fill(~ok4, 0.0)
+    q = st.q.float().view(N, H, Hq // H, d)
+    s = torch.matmul(k, q.transpose(2, 3).contiguous()) * (1.0 / math.sqrt(d))
+    s = s.masked_fill(~ok4, -math.inf)
+    top = s.amax(2, keepdim=True)
+    p = torch.exp(s - top.clamp(min=-3e38))
+    total = p.sum(2, keepdim=True)
+    o = torch.matmul(p.transpose(2, 3).contiguous(), v) / total.transpose(2, 3).clamp(min=1e-30)
+    lse = (top + torch.log(total)).view(N, Hq)
+    return o.view(N, Hq, d).to(st.q.dtype), lse.t().contiguous()
+
+
+def _places(st, T, first=None):
+    """Page and slot of each of T rows, and whether the row has a place."""
+    case = st.case
+    N, M = st.table.shape
+    P, _, B, _ = st.k.shape
+    S = case["S"]
+    starts = torch.arange(N + 1, device=DEV) if st.starts is None else st.starts.long()
+    row = torch.arange(T, device=DEV)
+    seq = torch.searchsorted(starts, row, right=True) - 1
+    t = st.lens.long()[seq] - starts[seq + 1] + row if first is None else first.long()[seq] + row - starts[seq]
+    t0 = t.clamp(min=0)
+    block = t0 // S * _bpc(case) + t0 % S // B
+    page = st.table[seq, block.clamp(max=M - 1)].long()
+    put = (t >= 0) & (t < st.lens.long()[seq]) & (block < M) & (page >= 0) & (page < P)
+    return page, t0 % S % B, put
+
+
+def _plain_append(st):
+    P, H, B, d = st.k.shape
+    page, slot, put = _places(st, st.T)
+    page, slot = page[put], slot[put]
+    begin = torch.full((P,), B, device=DEV).scatter_reduce_(0, page, slot, "amin")   # a page's first new slot
+    touched = begin < B
+    for which, (codes, new) in enumerate(((st.k, st.new_k), (st.v, st.new_v))):
+        new = new[put].float()
+        most = new.abs().amax(-1)
+        most = torch.zeros((P, H), device=DEV).scatter_reduce_(0, page[:, None].expand(-1, H), most, "amax")
+        need = _power(_exponent(most))
+        was = st.scales[..., which]
+        now = torch.where(begin[:, None] > 0, torch.maximum(was, need), need)
+        again = (touched & (begin > 0)).nonzero()[:, 0]   # blocks whose tokens may need rounding again
+        old = codes.view(torch.uint8)[again].view(E4M3).float() * (was[again] / now[again])[..., None, None]
+        stays = torch.arange(B, device=DEV)[None] >= begin[again][:, None]
+        old = torch.where(stays[:, None, :, None], codes.view(torch.uint8)[again], old.to(E4M3).view(torch.uint8))
+        codes.view(torch.uint8)[again] = old
+        codes.view(torch.uint8)[page, :, slot] = (new / now[page][..., None]).to(E4M3).view(torch.uint8)
+        st.scales[..., which] = torch.where(touched[:, None], now, was)
+    return st.k, st.v, st.scales
+
+
+def _plain_read(st):
+    dt = DTYPES[st.case["dtype"]]
+    P = st.k.shape[0]
+    page, slot, put = _places(st, st.T, st.first)
+    page = page.clamp(0, P - 1)
+    k = st.k.view(torch.uint8)[page, :, slot].view(E4M3).float() * st.scales[page][..., :1]
+    v = st.v.view(torch.uint8)[page, :, slot].view(E4M3).float() * st.scales[page][..., 1:]
+    return torch.where(put[:, None, None], k, 0.0).to(dt), torch.where(put[:, None, None], v, 0.0).to(dt)
+
+
+def _plain_copy(st):
+    P = st.k.shape[1]
+    src, dst = st.pairs.long().unbind(1)
+    take = (torch.arange(src.numel(), device=DEV) < st.count[0]) & (src >= 0) & (src < P) & (dst >= 0) & (dst < P)
+    src, dst = src[take], dst[take]
+    for t in (st.k.view(torch.uint8), st.v.view(torch.uint8), st.scales):
+        t[:, dst] = t[:, src]
+    return st.k, st.v, st.scales
+
+
+# ------------------------------------------------------------------------- in 64 bits
+
+
+def exact(case, seed):
+    st = prepare(case, seed)
+    if case["op"] == "decode":
+        return _exact_decode(st)
+    if case["op"] == "append":
+        return _exact_append(st)
+    if case["op"] == "read":
+        return _exact_read(st)
+    n, P = int(st.count[0]), st.k.shape[1]
+    pools = [st.k.double(), st.v.double(), st.scales.double()]
+    for s, t in st.pairs[:n].tolist():
+        if 0 <= s < P and 0 <= t < P:
+            for x in pools:
+                x[:, t] = x[:, s]
+    return tuple(pools)
+
+
+def _runs(case, t, n):
+    """Tokens t .. t + n - 1 of a sequence as (block, first slot, tokens), block by block."""
+    while n > 0:
+        c, inside = divmod(t, case["S"])
+        slot = inside % case["B"]
+        m = min(case["B"] - slot, case["S"] - inside, n)
+        yield c * _bpc(case) + inside // case["B"], slot, m
+        t, n = t + m, n - m
+
+
+def _exact_decode(st):
+    """Sequence by sequence: its tokens' rows gathered one block after another, a two-pass softmax."""
+    case = st.case
+    N, Hq, d = st.q.shape
+    H = st.k.shape[1]
+    out = torch.zeros((N, Hq, d), dtype=torch.float64, device=DEV)
+    lse = torch.full((Hq, N), -math.inf, dtype=torch.float64, device=DEV)
+    table = st.table.tolist()
+    for i, t in enumerate(st.lens.tolist()):
+        begin = max(0, t - case["window"]) if case["window"] else 0
+        at = [(table[i][b], slot, m) for b, slot, m in _runs(case, begin, t - begin)]
+        if not at:
+            continue
+        pages = torch.tensor([p for p, _, _ in at for _ in range(case["B"])], device=DEV)
+        slots = torch.arange(case["B"], device=DEV).repeat(len(at))
+        inside = torch.tensor([[a, a + m] for _, a, m in at], device=DEV).repeat_interleave(case["B"], 0)
+        use = (slots >= inside[:, 0]) & (slots < inside[:, 1])
+        pages, slots = pages[use], slots[use]
+        for h in range(H):
+            heads = slice(h * (Hq // H), (h + 1) * (Hq // H))
+            k = st.k.view(torch.uint8)[pages, h, slots].view(E4M3).double() * st.scales[pages, h, :1].double()
+            v = st.v.view(torch.uint8)[pages, h, slots].view(E4M3).double() * st.scales[pages, h, 1:].double()
+            s = k @ st.q[i, heads].double().t().contiguous() / math.sqrt(d)
+            lse[heads, i] = torch.logsumexp(s, 0)
+            out[i, heads] = torch.softmax(s, 0).t().contiguous() @ v
+    return out, lse
+
+
+def _round_e4m3(y):
+    """Nearest e4m3 value to y, |y| <= 448, ties to the even one: three bits behind the leading one,
+    which is worth 2^-6 or more."""
+    step = torch.exp2(torch.floor(torch.log2(y.abs().clamp(min=2.0 ** -6))) - 3)
+    return torch.round(y / step) * step
+
+
+def _spans(st):
+    """(sequence, first row, its token, rows) of every sequence's rows of an append or read."""
+    starts = list(range(st.case["N"] + 1)) if st.starts is None else st.starts.tolist()
+    first = None if getattr(st, "first", None) is None else st.first.tolist()
+    for i, t in enumerate(st.lens.tolist()):
+        n = starts[i + 1] - starts[i]
+        yield i, starts[i], t - n if first is None else first[i], n
+
+
+def _exact_append(st):
+    pools = [st.k.double(), st.v.double()]
+    scales = st.scales.double()
+    table = st.table.tolist()
+    for i, row, t, n in _spans(st):
+        for b, slot, m in _runs(st.case, t, n):
+            page = table[i][b]
+            for which, new in enumerate((st.new_k, st.new_v)):
+                x = new[row:row + m].double().transpose(0, 1)   # [H, m, d]
+                most = x.abs().amax((1, 2))
+                scale = torch.exp2(torch.ceil(torch.log2(most / 448)).clamp(min=LOWEST))
+                if slot > 0:
+                    was = scales[page, :, which]
+                    scale = torch.maximum(scale, was)
+                    old = pools[which][page, :, :slot]
+                    pools[which][page, :, :slot] = _round_e4m3(old * (was / scale)[:, None, None])
+                pools[which][page, :, slot:slot + m] = _round_e4m3(x / scale[:, None, None])
+                scales[page, :, which] = scale
+            row += m
+    return pools[0], pools[1], scales
+
+
+def _exact_read(st):
+    _, H, _, d = st.k.shape
+    out = [torch.zeros((st.T, H, d), dtype=torch.float64, device=DEV) for _ in range(2)]
+    table = st.table.tolist()
+    for i, row, t, n in _spans(st):
+        for b, slot, m in _runs(st.case, t, n):
+            page = table[i][b]
+            for which, codes in enumerate((st.k, st.v)):
+                x = codes[page, :, slot:slot + m].double() * st.scales[page, :, which].double()[:, None, None]
+                out[which][row:row + m] = x.transpose(0, 1)
+            row += m
+    return tuple(out)
