@@ -48,29 +48,29 @@ def _case(name, op, dtype="bf16", N=1, Hq=12, H=12, d=128, B=64, S=64, lo=64, hi
 def listed():
     return [
         # the smallest call: one short sequence of a two-head layer, all launch latency
-        _case("decode_q8_tiny", "decode", "fp32", N=1, Hq=2, H=2, d=64, lo=300, hi=300),
+        _case("decode_quant_tiny", "decode", "fp32", N=1, Hq=2, H=2, d=64, lo=300, hi=300),
         # four rollouts of a 1.3B-shaped layer, 10 to 20 cached chunks each: the largest stream
-        _case("decode_q8_chunks", "decode", N=4, S=4680, lo=46800, hi=93600),
+        _case("decode_quant_chunks", "decode", N=4, S=4680, lo=46800, hi=93600),
         # a serving batch: 40 query heads over 8 key-value heads, lengths over two decades
-        _case("decode_q8_gqa_ragged", "decode", N=48, Hq=40, H=8, lo=100, hi=16000),
+        _case("decode_quant_gqa_ragged", "decode", N=48, Hq=40, H=8, lo=100, hi=16000),
         # a model with small heads of their own keys each, long contexts
-        _case("decode_q8_heads64", "decode", N=12, Hq=16, H=16, d=64, lo=4000, hi=30000),
+        _case("decode_quant_heads64", "decode", N=12, Hq=16, H=16, d=64, lo=4000, hi=30000),
         # fp32 queries, small heads, eight query heads a key head, the last frame only
-        _case("decode_q8_fp32_window", "decode", "fp32", N=16, Hq=16, H=2, d=64, B=128, S=128, lo=1000, hi=6000, window=1560),
+        _case("decode_quant_fp32_window", "decode", "fp32", N=16, Hq=16, H=2, d=64, B=128, S=128, lo=1000, hi=6000, window=1560),
         # one new token for each sequence of a batch, between two decoding steps
-        _case("append_q8_token", "append", N=64, lo=100, hi=16000, n=1),
+        _case("append_quant_token", "append", N=64, lo=100, hi=16000, n=1),
         # the chunk just generated, for eight rollouts of a 1.3B-shaped layer
-        _case("append_q8_chunk", "append", N=8, S=4680, lo=4680, hi=46800, n=4680),
+        _case("append_quant_chunk", "append", N=8, S=4680, lo=4680, hi=46800, n=4680),
         # newly admitted prompts in fp32, some of them behind a prefix that is there
-        _case("append_q8_prompts", "append", "fp32", N=24, H=8, d=64, B=128, S=128, lo=30, hi=9000, n=0),
+        _case("append_quant_prompts", "append", "fp32", N=24, H=8, d=64, B=128, S=128, lo=30, hi=9000, n=0),
         # the last chunk of four rollouts, for a step that attends over full precision
-        _case("read_q8_chunk", "read", N=4, S=4680, lo=46800, hi=93600, n=4680),
+        _case("read_quant_chunk", "read", N=4, S=4680, lo=46800, hi=93600, n=4680),
         # some tokens from inside each sequence, in fp32
-        _case("read_q8_ragged", "read", "fp32", N=32, H=3, d=64, lo=50, hi=5000, n=0, first=True),
+        _case("read_quant_ragged", "read", "fp32", N=32, H=3, d=64, lo=50, hi=5000, n=0, first=True),
         # the private copies that sixteen forked sequences need before they append
-        _case("copy_q8_fork", "copy", N=16, pairs=16, extra=4.0),
+        _case("copy_quant_fork", "copy", N=16, pairs=16, extra=4.0),
         # the moves of a compaction, six layers of a 1.3B-shaped model at once
-        _case("copy_q8_moves", "copy", layers=6, pairs=300, extra=2.0),
+        _case("copy_quant_moves", "copy", layers=6, pairs=300, extra=2.0),
     ]
 
 
@@ -235,19 +235,19 @@ def run(st):
 
 
 def _own(st):
-    from paper_2605_30519_amd import (SeqKVCacheQ8, omnimem_append_kv_q8, omnimem_copy_pages_q8, omnimem_decode_attn_q8,
-                                      omnimem_read_kv_q8)
+    from paper_2605_30519_amd import (SeqKVCacheQuant, omnimem_append_kv_quant, omnimem_copy_pages_quant, omnimem_decode_attn_quant,
+                                      omnimem_read_kv_quant)
     case = st.case
     if case["op"] == "copy":
-        omnimem_copy_pages_q8(st.k, st.v, st.scales, st.pairs, st.count)
+        omnimem_copy_pages_quant(st.k, st.v, st.scales, st.pairs, st.count)
         return st.k, st.v, st.scales
-    cache = SeqKVCacheQ8(st.k, st.v, st.scales, st.table, st.lens, case["S"])
+    cache = SeqKVCacheQuant(st.k, st.v, st.scales, st.table, st.lens, case["S"])
     if case["op"] == "append":
-        omnimem_append_kv_q8(cache, st.new_k, st.new_v, st.starts)
+        omnimem_append_kv_quant(cache, st.new_k, st.new_v, st.starts)
         return st.k, st.v, st.scales
     if case["op"] == "read":
-        return omnimem_read_kv_q8(cache, st.T, st.starts, first=st.first, dtype=DTYPES[case["dtype"]])
-    return omnimem_decode_attn_q8(cache, st.q, window=case["window"])
+        return omnimem_read_kv_quant(cache, st.T, st.starts, first=st.first, dtype=DTYPES[case["dtype"]])
+    return omnimem_decode_attn_quant(cache, st.q, window=case["window"])
 
 
 def _power(e):
