@@ -247,4 +247,55 @@ OMNIMEM_API omnimem_status_t omnimem_seq_compact(const omnimem_seq_table_t* st, 
   return hip_status(omnimem::launch_seq_compact(g, p, a, workspace, as_stream(stream)));
 }
 
+OMNIMEM_API size_t omnimem_decode_quant_workspace_bytes(const omnimem_seq_cache_quant_t* sc, int32_t num_q_heads,
+                                                     int32_t window) {
+  return omnimem::decode_quant_workspace_bytes(sc, num_q_heads, window);
+}
+
+OMNIMEM_API omnimem_status_t omnimem_decode_attn_quant(const omnimem_seq_cache_quant_t* sc, int32_t dtype, const void* q,
+                                                    int64_t q_stride, int32_t num_q_heads, int32_t window, float scale,
+                                                    void* out, float* lse, void* workspace, size_t workspace_bytes,
+                                                    void* stream) {
+  omnimem::SeqGeom g;
+  omnimem::DecodePlan p;
+  omnimem::DecodeLaunch a;
+  const omnimem_status_t st = omnimem::check_decode_attn_quant(sc, dtype, q, q_stride, num_q_heads, window, scale, out, lse,
+                                                            workspace, workspace_bytes, g, p, a);
+  if (st != OMNIMEM_OK || g.N == 0) return st;
+  return hip_status(omnimem::launch_decode_quant(g, p, a, workspace, as_stream(stream)));
+}
+
+OMNIMEM_API omnimem_status_t omnimem_append_kv_quant(const omnimem_seq_cache_quant_t* sc, int32_t dtype, const void* k,
+                                                  int64_t k_stride, const void* v, int64_t v_stride, int32_t tokens,
+                                                  const int32_t* starts, void* stream) {
+  omnimem::SeqGeom g;
+  omnimem::AppendQuantLaunch a;
+  const omnimem_status_t st = omnimem::check_append_kv_quant(sc, dtype, k, k_stride, v, v_stride, tokens, starts, g, a);
+  if (st != OMNIMEM_OK || tokens == 0 || g.N == 0) return st;
+  return hip_status(omnimem::launch_append_kv_quant(g, a, as_stream(stream)));
+}
+
+OMNIMEM_API omnimem_status_t omnimem_read_kv_quant(const omnimem_seq_cache_quant_t* sc, int32_t dtype, int32_t tokens,
+                                                const int32_t* starts, const int32_t* first, void* out_k, void* out_v,
+                                                void* stream) {
+  omnimem::SeqGeom g;
+  omnimem::ReadQuantLaunch a;
+  const omnimem_status_t st = omnimem::check_read_kv_quant(sc, dtype, tokens, starts, first, out_k, out_v, g, a);
+  if (st != OMNIMEM_OK || tokens == 0 || g.N == 0) return st;
+  return hip_status(omnimem::launch_read_kv_quant(g, a, as_stream(stream)));
+}
+
+OMNIMEM_API omnimem_status_t omnimem_copy_pages_quant(void* k_pages, void* v_pages, float* scales, int64_t num_pages,
+                                                   int32_t num_heads, int32_t block_size, int32_t head_dim,
+                                                   int32_t layers, int64_t layer_stride, int64_t scale_stride,
+                                                   const int32_t* pairs, const int32_t* count, int32_t max_pairs,
+                                                   void* stream) {
+  omnimem::CopyLaunch a;
+  const omnimem_status_t st = omnimem::check_copy_pages_quant(k_pages, v_pages, scales, num_pages, num_heads, block_size,
+                                                           head_dim, layers, layer_stride, scale_stride, pairs, count,
+                                                           max_pairs, a);
+  if (st != OMNIMEM_OK || num_pages == 0 || layers == 0 || max_pairs == 0) return st;
+  return hip_status(omnimem::launch_copy_pages(a, as_stream(stream)));
+}
+
 OMNIMEM_API const char* omnimem_status_string(int32_t status) { return omnimem::status_string(status); }

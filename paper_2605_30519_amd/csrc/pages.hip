@@ -141,6 +141,11 @@ __device__ __forceinline__ void copy_pieces(const CopyLaunch& a, int pieces, int
       const int64_t c = at + u * kCopyThreads + threadIdx.x;
       if (c < a.page_chunks) store16<PAST>(x[u], to + c);
     }
+    if (a.scales != nullptr && pool == 0 && at == 0) {  // once for a page
+      float2* scales = reinterpret_cast<float2*>(a.scales) + layer * a.layer_scales;
+      for (int64_t h = threadIdx.x; h < a.page_scales; h += kCopyThreads)
+        scales[dst * a.page_scales + h] = scales[src * a.page_scales + h];
+    }
   }
 }
 

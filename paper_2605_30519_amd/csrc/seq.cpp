@@ -36,19 +36,33 @@ omnimem_status_t resolve_table(const omnimem_seq_table_t* st, SeqGeom& g, bool s
   return OMNIMEM_OK;
 }
 
-omnimem_status_t resolve_seq_cache(const omnimem_seq_cache_t* sc, SeqGeom& g, bool sizes_only) {
-  if (sc == nullptr) return OMNIMEM_EINVAL;
-  if (sc->dtype != OMNIMEM_BF16 && sc->dtype != OMNIMEM_F32) return OMNIMEM_EUNSUPPORTED;
-  if (sc->head_dim != 64 && sc->head_dim != 128) return OMNIMEM_EUNSUPPORTED;
-  if (sc->num_heads < 1 || sc->num_heads > (1 << 20)) return OMNIMEM_EINVAL;
-  const omnimem_status_t st = resolve_table(&sc->seqs, g, sizes_only);
+bool known_dtype(int32_t dtype) { return dtype == OMNIMEM_BF16 || dtype == OMNIMEM_F32; }
+
+omnimem_status_t resolve_pools(const omnimem_seq_table_t& seqs, int32_t num_heads, int32_t head_dim, const void* k_pages,
+                               const void* v_pages, SeqGeom& g, bool sizes_only) {
+  if (head_dim != 64 && head_dim != 128) return OMNIMEM_EUNSUPPORTED;
+  if (num_heads < 1 || num_heads > (1 << 20)) return OMNIMEM_EINVAL;
+  const omnimem_status_t st = resolve_table(&seqs, g, sizes_only);
   if (st != OMNIMEM_OK) return st;
   // the pool's elements stay inside int64 index arithmetic
-  if (g.num_pages > (int64_t{1} << 40) / (static_cast<int64_t>(sc->num_heads) * g.B * sc->head_dim))
-    return OMNIMEM_EINVAL;
-  if (!sizes_only && g.num_pages > 0 && (sc->k_pages == nullptr || sc->v_pages == nullptr)) return OMNIMEM_EINVAL;
-  if (!aligned(sc->k_pages, 16) || !aligned(sc->v_pages, 16)) return OMNIMEM_EINVAL;
+  if (g.num_pages > (int64_t{1} << 40) / (static_cast<int64_t>(num_heads) * g.B * head_dim)) return OMNIMEM_EINVAL;
+  if (!sizes_only && g.num_pages > 0 && (k_pages == nullptr || v_pages == nullptr)) return OMNIMEM_EINVAL;
+  if (!aligned(k_pages, 16) || !aligned(v_pages, 16)) return OMNIMEM_EINVAL;
   return OMNIMEM_OK;
+}
+
+omnimem_status_t resolve_seq_cache(const omnimem_seq_cache_t* sc, SeqGeom& g, bool sizes_only) {
+  if (sc == nullptr) return OMNIMEM_EINVAL;
+  if (!known_dtype(sc->dtype)) return OMNIMEM_EUNSUPPORTED;
+  return resolve_pools(sc->seqs, sc->num_heads, sc->head_dim, sc->k_pages, sc->v_pages, g, sizes_only);
+}
+
+omnimem_status_t resolve_quant_cache(const omnimem_seq_cache_quant_t* sc, SeqGeom& g, bool sizes_only) {
+  if (sc == nullptr) return OMNIMEM_EINVAL;
+  const omnimem_status_t st = resolve_pools(sc->seqs, sc->num_heads, sc->head_dim, sc->k_pages, sc->v_pages, g, sizes_only);
+  if (st != OMNIMEM_OK) return st;
+  if (!sizes_only && g.num_pages > 0 && sc->scales == nullptr) return OMNIMEM_EINVAL;
+  return aligned(sc->scales, 8) ? OMNIMEM_OK : OMNIMEM_EINVAL;
 }
 
 // A row stride in elements of `row` elements: covers the row, whole 16-byte chunks.
@@ -73,14 +87,15 @@ constexpr int64_t kDecodeWgs = 256, kDecodeManyWgs = 512;
 constexpr int64_t kItemUnitsMost = 20, kWaveUnitsMost = 8, kWaveItems = 1024;
 constexpr int64_t kItemOverhead = 64;  // of an item's length on the line, no less than the kernel adds
 
-omnimem_status_t plan_decode(const omnimem_seq_cache_t* sc, const SeqGeom& g, int32_t num_q_heads, int32_t window,
-                             DecodePlan& p) {
-  if (num_q_heads < 1 || num_q_heads % sc->num_heads != 0) return OMNIMEM_EINVAL;
-  p.G = num_q_heads / sc->num_heads;
+// unit: tokens of a unit
+omnimem_status_t plan_decode(int32_t num_heads, int32_t head_dim, int64_t unit, const SeqGeom& g, int32_t num_q_heads,
+                             int32_t window, DecodePlan& p) {
+  if (num_q_heads < 1 || num_q_heads % num_heads != 0) return OMNIMEM_EINVAL;
+  p.G = num_q_heads / num_heads;
   p.tile_rows = p.G <= kDecodeHeadRows ? kDecodeHeadRows : 2 * kDecodeHeadRows;
   p.head_tiles = (p.G + p.tile_rows - 1) / p.tile_rows;
   p.rows = p.G < p.tile_rows ? p.G : p.tile_rows;
-  const int64_t items = static_cast<int64_t>(g.N) * sc->num_heads * p.head_tiles;
+  const int64_t items = static_cast<int64_t>(g.N) * num_heads * p.head_tiles;
   // Blocks and units of an item, at most.  A window reaches into window / S + 2 chunks, and
   // tokens of one run lie in no more than a B-th of them, and two, blocks.
   int64_t blocks = g.M;
@@ -88,7 +103,6 @@ omnimem_status_t plan_decode(const omnimem_seq_cache_t* sc, const SeqGeom& g, in
     const int64_t runs = g.Bpc == 1 && g.S == g.B ? 1 : int64_t{window} / g.S + 2;
     blocks = window / g.B + 2 * runs < blocks ? window / g.B + 2 * runs : blocks;
   }
-  const int64_t unit = sc->dtype == OMNIMEM_BF16 && sc->head_dim == 64 ? 64 : 32;
   const int64_t units = blocks * (g.B / unit);
   // a sum of the sequences' units in 31 bits, positions on the line in 40
   if (items > 0x7fffffff / 256 || static_cast<int64_t>(g.N) * (static_cast<int64_t>(g.M) * (g.B / unit) + kItemOverhead) > 0x7fffffff ||
@@ -104,13 +118,24 @@ omnimem_status_t plan_decode(const omnimem_seq_cache_t* sc, const SeqGeom& g, in
                            : p.split == DecodeSplit::kItem ? items
                                                            : (items + kDecodeWaves - 1) / kDecodeWaves);
   p.join_rows = items * 16 <= p.wgs ? 1 : p.rows >= 4 ? 4 : p.rows >= 2 ? 2 : 1;
-  p.slot_floats = static_cast<size_t>(p.rows) * (sc->head_dim + 2);
+  p.slot_floats = static_cast<size_t>(p.rows) * (head_dim + 2);
   p.slot_floats = (p.slot_floats + 3) / 4 * 4;
   p.off_part = 0;
   const size_t shares = p.split == DecodeSplit::kLine ? p.wgs : 0;
   p.off_starts = align256(shares * 2 * p.slot_floats * sizeof(float));
   p.total = shares == 0 ? 256 : p.off_starts + align256(shares * sizeof(DecodeStart)) + 512;
   return OMNIMEM_OK;
+}
+
+omnimem_status_t plan_decode(const omnimem_seq_cache_t* sc, const SeqGeom& g, int32_t num_q_heads, int32_t window,
+                             DecodePlan& p) {
+  const int64_t unit = sc->dtype == OMNIMEM_BF16 && sc->head_dim == 64 ? 64 : 32;
+  return plan_decode(sc->num_heads, sc->head_dim, unit, g, num_q_heads, window, p);
+}
+
+omnimem_status_t plan_decode(const omnimem_seq_cache_quant_t* sc, const SeqGeom& g, int32_t num_q_heads, int32_t window,
+                             DecodePlan& p) {
+  return plan_decode(sc->num_heads, sc->head_dim, 64, g, num_q_heads, window, p);
 }
 
 omnimem_status_t check_scratch(const void* workspace, size_t have, size_t need) {
@@ -146,6 +171,15 @@ size_t decode_workspace_bytes(const omnimem_seq_cache_t* sc, int32_t num_q_heads
   return p.total;
 }
 
+size_t decode_quant_workspace_bytes(const omnimem_seq_cache_quant_t* sc, int32_t num_q_heads, int32_t window) {
+  SeqGeom g;
+  DecodePlan p;
+  if (window < 0 || resolve_quant_cache(sc, g, true) != OMNIMEM_OK ||
+      plan_decode(sc, g, num_q_heads, window, p) != OMNIMEM_OK)
+    return 0;
+  return p.total;
+}
+
 size_t seq_workspace_bytes(const omnimem_seq_table_t* st, int32_t num_new) {
   SeqGeom g;
   SeqPlan p;
@@ -153,30 +187,43 @@ size_t seq_workspace_bytes(const omnimem_seq_table_t* st, int32_t num_new) {
   return p.total;
 }
 
+namespace {
+
+// Of a decode call behind its cache and plan.
+omnimem_status_t check_decode(const SeqGeom& g, const DecodePlan& p, const DecodeLaunch& a, const void* workspace,
+                              size_t workspace_bytes) {
+  if (a.window < 0 || !isfinite(a.scale) || !(a.scale > 0.f)) return OMNIMEM_EINVAL;
+  if (!good_stride(a.q_stride, static_cast<int64_t>(a.Hq) * a.D, elem_bytes(a.dtype))) return OMNIMEM_EINVAL;
+  if (g.N == 0) return OMNIMEM_OK;
+  if (a.q == nullptr || a.out == nullptr || !aligned(a.q, 16) || !aligned(a.out, 16) || !aligned(a.lse, 4))
+    return OMNIMEM_EINVAL;
+  return p.split != DecodeSplit::kLine ? OMNIMEM_OK : check_scratch(workspace, workspace_bytes, p.total);
+}
+
+}  // namespace
+
 omnimem_status_t check_decode_attn(const omnimem_seq_cache_t* sc, const void* q, int64_t q_stride, int32_t num_q_heads,
                                    int32_t window, float scale, void* out, float* lse, const void* workspace,
                                    size_t workspace_bytes, SeqGeom& g, DecodePlan& p, DecodeLaunch& a) {
   omnimem_status_t st = resolve_seq_cache(sc, g, false);
   if (st == OMNIMEM_OK) st = plan_decode(sc, g, num_q_heads, window, p);
   if (st != OMNIMEM_OK) return st;
-  if (window < 0 || !isfinite(scale) || !(scale > 0.f)) return OMNIMEM_EINVAL;
-  if (!good_stride(q_stride, static_cast<int64_t>(num_q_heads) * sc->head_dim, elem_bytes(sc->dtype)))
-    return OMNIMEM_EINVAL;
-  if (g.N == 0) return OMNIMEM_OK;
-  if (q == nullptr || out == nullptr || !aligned(q, 16) || !aligned(out, 16) || !aligned(lse, 4)) return OMNIMEM_EINVAL;
-  a.dtype = sc->dtype;
-  a.H = sc->num_heads;
-  a.D = sc->head_dim;
-  a.k_pages = sc->k_pages;
-  a.v_pages = sc->v_pages;
-  a.q = q;
-  a.q_stride = q_stride;
-  a.Hq = num_q_heads;
-  a.window = window;
-  a.scale = scale;
-  a.out = out;
-  a.lse = lse;
-  return p.split != DecodeSplit::kLine ? OMNIMEM_OK : check_scratch(workspace, workspace_bytes, p.total);
+  a = DecodeLaunch{sc->dtype, sc->num_heads, sc->head_dim, sc->k_pages, sc->v_pages, nullptr,
+                   q,         q_stride,      num_q_heads,  window,      scale,       out, lse};
+  return check_decode(g, p, a, workspace, workspace_bytes);
+}
+
+omnimem_status_t check_decode_attn_quant(const omnimem_seq_cache_quant_t* sc, int32_t dtype, const void* q, int64_t q_stride,
+                                      int32_t num_q_heads, int32_t window, float scale, void* out, float* lse,
+                                      const void* workspace, size_t workspace_bytes, SeqGeom& g, DecodePlan& p,
+                                      DecodeLaunch& a) {
+  if (!known_dtype(dtype)) return OMNIMEM_EUNSUPPORTED;
+  omnimem_status_t st = resolve_quant_cache(sc, g, false);
+  if (st == OMNIMEM_OK) st = plan_decode(sc, g, num_q_heads, window, p);
+  if (st != OMNIMEM_OK) return st;
+  a = DecodeLaunch{dtype, sc->num_heads, sc->head_dim, sc->k_pages, sc->v_pages, sc->scales,
+                   q,     q_stride,      num_q_heads,  window,      scale,       out, lse};
+  return check_decode(g, p, a, workspace, workspace_bytes);
 }
 
 omnimem_status_t check_append_kv(const omnimem_seq_cache_t* sc, const void* k, int64_t k_stride, const void* v,
@@ -222,6 +269,54 @@ omnimem_status_t check_copy_pages(void* k_pages, void* v_pages, int64_t num_page
   a.pairs = pairs;
   a.count = count;
   a.max_pairs = max_pairs;
+  a.scales = nullptr;
+  a.page_scales = a.layer_scales = 0;
+  return OMNIMEM_OK;
+}
+
+omnimem_status_t check_append_kv_quant(const omnimem_seq_cache_quant_t* sc, int32_t dtype, const void* k, int64_t k_stride,
+                                    const void* v, int64_t v_stride, int32_t tokens, const int32_t* starts, SeqGeom& g,
+                                    AppendQuantLaunch& a) {
+  if (!known_dtype(dtype)) return OMNIMEM_EUNSUPPORTED;
+  const omnimem_status_t st = resolve_quant_cache(sc, g, false);
+  if (st != OMNIMEM_OK) return st;
+  if (tokens < 0 || (starts == nullptr && tokens != g.N) || !aligned(starts, 4)) return OMNIMEM_EINVAL;
+  const int64_t row = static_cast<int64_t>(sc->num_heads) * sc->head_dim, eb = elem_bytes(dtype);
+  if (!good_stride(k_stride, row, eb) || !good_stride(v_stride, row, eb)) return OMNIMEM_EINVAL;
+  if (tokens > 0 && (k == nullptr || v == nullptr || !aligned(k, 16) || !aligned(v, 16))) return OMNIMEM_EINVAL;
+  a = AppendQuantLaunch{dtype,  sc->num_heads, sc->head_dim, k, v, k_stride, v_stride, tokens,
+                     starts, sc->k_pages,   sc->v_pages,  sc->scales};
+  return OMNIMEM_OK;
+}
+
+omnimem_status_t check_read_kv_quant(const omnimem_seq_cache_quant_t* sc, int32_t dtype, int32_t tokens, const int32_t* starts,
+                                  const int32_t* first, void* out_k, void* out_v, SeqGeom& g, ReadQuantLaunch& a) {
+  if (!known_dtype(dtype)) return OMNIMEM_EUNSUPPORTED;
+  const omnimem_status_t st = resolve_quant_cache(sc, g, false);
+  if (st != OMNIMEM_OK) return st;
+  if (tokens < 0 || (starts == nullptr && tokens != g.N) || !aligned(starts, 4) || !aligned(first, 4)) return OMNIMEM_EINVAL;
+  if (tokens > 0 && (out_k == nullptr || out_v == nullptr)) return OMNIMEM_EINVAL;
+  if (!aligned(out_k, 16) || !aligned(out_v, 16)) return OMNIMEM_EINVAL;
+  a = ReadQuantLaunch{dtype,       sc->num_heads, sc->head_dim, tokens, starts, first,
+                   sc->k_pages, sc->v_pages,   sc->scales,   out_k,  out_v};
+  return OMNIMEM_OK;
+}
+
+omnimem_status_t check_copy_pages_quant(void* k_pages, void* v_pages, float* scales, int64_t num_pages, int32_t num_heads,
+                                     int32_t block_size, int32_t head_dim, int32_t layers, int64_t layer_stride,
+                                     int64_t scale_stride, const int32_t* pairs, const int32_t* count, int32_t max_pairs,
+                                     CopyLaunch& a) {
+  if ((block_size != 64 && block_size != 128) || (head_dim != 64 && head_dim != 128)) return OMNIMEM_EUNSUPPORTED;
+  if (num_heads < 1 || num_heads > (1 << 20)) return OMNIMEM_EINVAL;
+  const omnimem_status_t st = check_copy_pages(k_pages, v_pages, num_pages, static_cast<int64_t>(num_heads) * block_size * head_dim,
+                                               layers, layer_stride, pairs, count, max_pairs, a);
+  if (st != OMNIMEM_OK) return st;
+  if (scale_stride < 0 || scale_stride % 8 != 0 || !aligned(scales, 8)) return OMNIMEM_EINVAL;
+  if (layers > 1 && (scale_stride < num_pages * num_heads * 8 || scale_stride > (int64_t{1} << 44))) return OMNIMEM_EINVAL;
+  if (layers > 0 && num_pages > 0 && max_pairs > 0 && (v_pages == nullptr || scales == nullptr)) return OMNIMEM_EINVAL;
+  a.scales = scales;
+  a.page_scales = num_heads;
+  a.layer_scales = scale_stride / 8;
   return OMNIMEM_OK;
 }
 

@@ -53,6 +53,7 @@ struct DecodeLaunch {
   int dtype, H, D;
   const void* k_pages;
   const void* v_pages;
+  const float* scales;  // [page][head][2] of 8-bit pages, else null
   const void* q;
   int64_t q_stride;  // elements
   int Hq, window;
@@ -83,6 +84,33 @@ struct CopyLaunch {
   const int32_t* pairs;
   const int32_t* count;
   int max_pairs;
+  float* scales;                       // of 8-bit pages, else null
+  int64_t page_scales, layer_scales;   // (K, V) pairs
+};
+
+// ---------------------------------------------------------------- 8-bit pages
+struct AppendQuantLaunch {
+  int dtype, H, D;             // of k and v
+  const void* k;
+  const void* v;
+  int64_t k_stride, v_stride;  // elements
+  int tokens;
+  const int32_t* starts;       // or null: one token per sequence
+  void* k_pages;
+  void* v_pages;
+  float* scales;
+};
+
+struct ReadQuantLaunch {
+  int dtype, H, D;             // of the rows
+  int tokens;
+  const int32_t* starts;       // or null: one token per sequence
+  const int32_t* first;        // or null: each sequence's last tokens
+  const void* k_pages;
+  const void* v_pages;
+  const float* scales;
+  void* out_k;
+  void* out_v;
 };
 
 // Scratch of the table updates: a bitmap of the pool's pages, and where there are new rows a
@@ -124,6 +152,7 @@ struct SeqUpdateLaunch {
 
 size_t decode_workspace_bytes(const omnimem_seq_cache_t* sc, int32_t num_q_heads, int32_t window);
 size_t seq_workspace_bytes(const omnimem_seq_table_t* st, int32_t num_new);
+size_t decode_quant_workspace_bytes(const omnimem_seq_cache_quant_t* sc, int32_t num_q_heads, int32_t window);
 
 omnimem_status_t check_decode_attn(const omnimem_seq_cache_t* sc, const void* q, int64_t q_stride, int32_t num_q_heads,
                                    int32_t window, float scale, void* out, float* lse, const void* workspace,
@@ -133,6 +162,19 @@ omnimem_status_t check_append_kv(const omnimem_seq_cache_t* sc, const void* k, i
 omnimem_status_t check_copy_pages(void* k_pages, void* v_pages, int64_t num_pages, int64_t page_bytes, int32_t layers,
                                   int64_t layer_stride, const int32_t* pairs, const int32_t* count, int32_t max_pairs,
                                   CopyLaunch& a);
+omnimem_status_t check_decode_attn_quant(const omnimem_seq_cache_quant_t* sc, int32_t dtype, const void* q, int64_t q_stride,
+                                      int32_t num_q_heads, int32_t window, float scale, void* out, float* lse,
+                                      const void* workspace, size_t workspace_bytes, SeqGeom& g, DecodePlan& p,
+                                      DecodeLaunch& a);
+omnimem_status_t check_append_kv_quant(const omnimem_seq_cache_quant_t* sc, int32_t dtype, const void* k, int64_t k_stride,
+                                    const void* v, int64_t v_stride, int32_t tokens, const int32_t* starts, SeqGeom& g,
+                                    AppendQuantLaunch& a);
+omnimem_status_t check_read_kv_quant(const omnimem_seq_cache_quant_t* sc, int32_t dtype, int32_t tokens, const int32_t* starts,
+                                  const int32_t* first, void* out_k, void* out_v, SeqGeom& g, ReadQuantLaunch& a);
+omnimem_status_t check_copy_pages_quant(void* k_pages, void* v_pages, float* scales, int64_t num_pages, int32_t num_heads,
+                                     int32_t block_size, int32_t head_dim, int32_t layers, int64_t layer_stride,
+                                     int64_t scale_stride, const int32_t* pairs, const int32_t* count, int32_t max_pairs,
+                                     CopyLaunch& a);
 omnimem_status_t check_seq_update(const omnimem_seq_table_t* st, int32_t num_new, const int32_t* parent,
                                   const int32_t* keep, const int32_t* grow, int32_t* out_table, int32_t* out_lens,
                                   int32_t* copies, int32_t* info, const void* workspace, size_t workspace_bytes,

@@ -115,6 +115,17 @@ class omnimem_seq_cache_t(ctypes.Structure):
     ]
 
 
+class omnimem_seq_cache_quant_t(ctypes.Structure):
+    _fields_ = [
+        ("seqs", omnimem_seq_table_t),
+        ("num_heads", ctypes.c_int32),
+        ("head_dim", ctypes.c_int32),
+        ("k_pages", ctypes.c_void_p),
+        ("v_pages", ctypes.c_void_p),
+        ("scales", ctypes.c_void_p),
+    ]
+
+
 EXPORTED = [
     "omnimem_blocks_per_chunk",
     "omnimem_awe_active",
@@ -145,6 +156,11 @@ EXPORTED = [
     "omnimem_seq_workspace_bytes",
     "omnimem_seq_update",
     "omnimem_seq_compact",
+    "omnimem_decode_quant_workspace_bytes",
+    "omnimem_decode_attn_quant",
+    "omnimem_append_kv_quant",
+    "omnimem_read_kv_quant",
+    "omnimem_copy_pages_quant",
 ]
 
 
@@ -233,6 +249,17 @@ def _configure(L, required: bool = True):
     L.omnimem_seq_update.restype = i32
     L.omnimem_seq_compact.argtypes = [stp, vp, vp, vp, vp, sz, vp]
     L.omnimem_seq_compact.restype = i32
+    qcp = ctypes.POINTER(omnimem_seq_cache_quant_t)
+    L.omnimem_decode_quant_workspace_bytes.argtypes = [qcp, i32, i32]
+    L.omnimem_decode_quant_workspace_bytes.restype = sz
+    L.omnimem_decode_attn_quant.argtypes = [qcp, i32, vp, i64, i32, i32, f32, vp, vp, vp, sz, vp]
+    L.omnimem_decode_attn_quant.restype = i32
+    L.omnimem_append_kv_quant.argtypes = [qcp, i32, vp, i64, vp, i64, i32, vp, vp]
+    L.omnimem_append_kv_quant.restype = i32
+    L.omnimem_read_kv_quant.argtypes = [qcp, i32, i32, vp, vp, vp, vp, vp]
+    L.omnimem_read_kv_quant.restype = i32
+    L.omnimem_copy_pages_quant.argtypes = [vp, vp, vp, i64, i32, i32, i32, i32, i64, i64, vp, vp, i32, vp]
+    L.omnimem_copy_pages_quant.restype = i32
     return L
 
 
@@ -870,16 +897,17 @@ class SeqUpdate:
     info: torch.Tensor        # [4] int32: copies, pages in use, pages short, rows over capacity
 
 
-def _rows_stride(name: str, t, heads: Optional[int], like: torch.Tensor) -> int:
-    """Checks rows [n, H, d] of like's type and GPU, each row contiguous; elements from row to row."""
+def _rows_stride(name: str, t, heads: Optional[int], like: torch.Tensor, dtype: Optional[torch.dtype] = None) -> int:
+    """Checks rows [n, H, d] of like's type (or dtype) and GPU, each row contiguous; elements from row to row."""
     if not isinstance(t, torch.Tensor) or t.dim() != 3:
         raise ValueError(f"{name} must be a [rows, H, d] tensor")
     n, h, d = t.shape
     want = like.shape[3]
     if d != want or (heads is not None and h != heads):
         raise ValueError(f"{name} must have shape {(n, heads or h, want)}, not {tuple(t.shape)}")
-    if t.dtype is not like.dtype:
-        raise ValueError(f"{name} must be {like.dtype}, not {t.dtype}")
+    dtype = dtype or like.dtype
+    if t.dtype is not dtype:
+        raise ValueError(f"{name} must be {dtype}, not {t.dtype}")
     if t.get_device() != like.get_device():
         _on_gpu(like, **{name: t})
     if t.is_contiguous():
@@ -1098,6 +1126,201 @@ def omnimem_seq_compact(page_table: torch.Tensor, seq_lens: torch.Tensor, num_pa
     if st != 0:
         _check(st, "omnimem_seq_compact")
     return made
+
+
+# -------------------------------------------------------- 8-bit sequence cache
+
+_E4M3 = torch.float8_e4m3fn
+
+
+@dataclass
+class SeqKVCacheQuant:
+    """One layer's keys and values of many sequences over one page pool in 8 bits (device tensors
+    owned by the caller): a value is its code times the scale of its page and head.
+
+    k_pages, v_pages: [num_pages, H, B, d] float8_e4m3fn; scales: [num_pages, H, 2] fp32, of K and of
+    V; page_table, seq_lens, chunk_tokens: as SeqKVCache's."""
+    k_pages: torch.Tensor
+    v_pages: torch.Tensor
+    scales: torch.Tensor
+    page_table: torch.Tensor
+    seq_lens: torch.Tensor
+    chunk_tokens: int = 0
+
+    def descriptor(self) -> omnimem_seq_cache_quant_t:
+        kp, vp, sc, pt, sl = self.k_pages, self.v_pages, self.scales, self.page_table, self.seq_lens
+        shape = kp.shape
+        if kp.dtype is not _E4M3 or vp.dtype is not _E4M3:
+            raise TypeError("k_pages and v_pages must be torch.float8_e4m3fn")
+        if len(shape) != 4 or vp.shape != shape:
+            raise ValueError("k_pages and v_pages must share one [num_pages, H, B, d] shape")
+        if not (kp.is_contiguous() and vp.is_contiguous()):
+            raise ValueError("cache tensors must be contiguous")
+        num_pages, H, B, d = shape
+        _check_tensor("scales", sc, (num_pages, H, 2), torch.float32)
+        seqs = _seq_table(pt, sl, num_pages, B, self.chunk_tokens)
+        dev = kp.get_device()
+        if dev < 0 or not vp.get_device() == dev == pt.get_device() == sl.get_device() == sc.get_device():
+            _on_gpu(kp, v_pages=vp, scales=sc, page_table=pt, seq_lens=sl)
+        return omnimem_seq_cache_quant_t(seqs, H, d, kp.data_ptr(), vp.data_ptr(), sc.data_ptr())
+
+    def after(self, update: "SeqUpdate") -> "SeqKVCacheQuant":
+        """The same pool under the tables of an update."""
+        return replace(self, page_table=update.page_table, seq_lens=update.seq_lens)
+
+
+def _dtype_code(name: str, t) -> int:
+    code = _DTYPES.get(t.dtype) if isinstance(t, torch.Tensor) else None
+    _need(code is not None, f"{name} must be a bf16 or fp32 tensor")
+    return code
+
+
+def omnimem_decode_quant_workspace_bytes(cache: SeqKVCacheQuant, num_q_heads: int, window: int = 0) -> int:
+    return int(lib().omnimem_decode_quant_workspace_bytes(ctypes.byref(cache.descriptor()), int(num_q_heads), int(window)))
+
+
+def omnimem_decode_attn_quant(cache: SeqKVCacheQuant, q: torch.Tensor, scale: Optional[float] = None, *, window: int = 0,
+                           out: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None,
+                           want_lse: bool = True, workspace: Optional[torch.Tensor] = None, stream=None):
+    """omnimem_decode_attn over an 8-bit cache: q [N, Hq, d] in bf16 or fp32, out as q."""
+    kp = cache.k_pages
+    dev = kp.get_device()
+    if dev >= 0 and (stream is not None or dev != _current_device()):
+        with _elsewhere(kp, stream):
+            return omnimem_decode_attn_quant(cache, q, scale, window=window, out=out, lse=lse, want_lse=want_lse,
+                                          workspace=workspace)
+    code = _dtype_code("q", q)
+    desc = ctypes.byref(cache.descriptor())
+    stride = _rows_stride("q", q, None, kp, q.dtype)
+    n, hq, d = q.shape
+    H = kp.shape[1]
+    _need(hq >= 1 and hq % H == 0, "q must have a multiple of the cache's heads")
+    _need(n == cache.page_table.shape[0], "q must have one row per sequence")
+    _need(0 <= window <= _I32_MAX, "window must be 0 (all tokens) to 2^31 - 1")
+    if out is not None or lse is not None:
+        _check_outputs(q, out, lse)
+        _on_gpu(kp, out=out, lse=lse)
+    L = lib()
+    window = int(window)
+    need = L.omnimem_decode_quant_workspace_bytes(desc, hq, window)
+    if workspace is not None:
+        _check_workspace(workspace, need, q)
+    elif need > 256:   # 256: the call needs none
+        workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
+    if out is None:
+        out = torch.empty_like(q, memory_format=torch.contiguous_format)
+    if lse is None and want_lse:
+        lse = torch.empty((hq, n), dtype=torch.float32, device=q.device)
+    st = L.omnimem_decode_attn_quant(desc, code, q.data_ptr(), stride, hq, window,
+                                  d ** -0.5 if scale is None else float(scale), out.data_ptr(), _ptr(lse),
+                                  _ptr(workspace), need, _current_raw_stream())
+    if st != 0:
+        _check(st, "omnimem_decode_attn_quant")
+    return out, lse
+
+
+def omnimem_append_kv_quant(cache: SeqKVCacheQuant, k: torch.Tensor, v: torch.Tensor, starts: Optional[torch.Tensor] = None, *,
+                         stream=None) -> None:
+    """Quantises new tokens into their sequences' pages: rows as for omnimem_append_kv, k and v
+    [T, H, d] both in bf16 or both in fp32.  A block's scale is a power of two and grows with what is
+    appended to the block."""
+    kp = cache.k_pages
+    dev = kp.get_device()
+    if dev >= 0 and (stream is not None or dev != _current_device()):
+        with _elsewhere(kp, stream):
+            return omnimem_append_kv_quant(cache, k, v, starts)
+    code = _dtype_code("k", k)
+    desc = cache.descriptor()
+    H, seqs = kp.shape[1], cache.page_table.shape[0]
+    ks, vs = _rows_stride("k", k, H, kp, k.dtype), _rows_stride("v", v, H, kp, k.dtype)
+    n = k.shape[0]
+    _need(v.shape[0] == n, "k and v must have as many rows")
+    _check_starts(starts, n, seqs, "k and v")
+    if starts is not None and starts.get_device() != dev:
+        _on_gpu(kp, starts=starts)
+    st = lib().omnimem_append_kv_quant(ctypes.byref(desc), code, k.data_ptr(), ks, v.data_ptr(), vs, n, _ptr(starts),
+                                    _current_raw_stream())
+    if st != 0:
+        _check(st, "omnimem_append_kv_quant")
+
+
+def _check_starts(starts, rows: int, seqs: int, what: str):
+    if starts is None:
+        _need(rows == seqs, f"{what} must have one row per sequence without starts")
+    else:
+        _check_tensor("starts", starts, (seqs + 1,), torch.int32)
+
+
+def omnimem_read_kv_quant(cache: SeqKVCacheQuant, tokens: int, starts: Optional[torch.Tensor] = None, *,
+                       first: Optional[torch.Tensor] = None, dtype: torch.dtype = torch.bfloat16, out=None, stream=None):
+    """Reads tokens back as (k, v), [tokens, H, d] of dtype (bf16 or fp32) or the pair of tensors out:
+    rows starts[i] to starts[i + 1] are the tokens of sequence i from first[i] on ([N] int32; None:
+    its last ones); starts [N + 1] int32, None: one token per sequence.  Tokens that a sequence does not
+    have are zeros; rows of no sequence are left as they were, and undefined in tensors made here."""
+    kp = cache.k_pages
+    dev = kp.get_device()
+    if dev >= 0 and (stream is not None or dev != _current_device()):
+        with _elsewhere(kp, stream):
+            return omnimem_read_kv_quant(cache, tokens, starts, first=first, dtype=dtype, out=out)
+    desc = cache.descriptor()
+    _, H, _, d = kp.shape
+    seqs = cache.page_table.shape[0]
+    _need(0 <= tokens <= _I32_MAX, "tokens must be 0 to 2^31 - 1")
+    tokens = int(tokens)
+    _check_starts(starts, tokens, seqs, "the result")
+    if first is not None:
+        _check_tensor("first", first, (seqs,), torch.int32)
+    if out is None:
+        _need(dtype in _DTYPES, "dtype must be bf16 or fp32")
+        k, v = (torch.empty((tokens, H, d), dtype=dtype, device=kp.device) for _ in range(2))
+    else:
+        k, v = out
+        _dtype_code("out", k)
+        dtype = k.dtype
+        _check_tensor("out[0]", k, (tokens, H, d), dtype)
+        _check_tensor("out[1]", v, (tokens, H, d), dtype)
+    if out is not None or starts is not None or first is not None:
+        _on_gpu(kp, starts=starts, first=first, k=k, v=v)
+    st = lib().omnimem_read_kv_quant(ctypes.byref(desc), _DTYPES[dtype], tokens, _ptr(starts), _ptr(first), k.data_ptr(),
+                                  v.data_ptr(), _current_raw_stream())
+    if st != 0:
+        _check(st, "omnimem_read_kv_quant")
+    return k, v
+
+
+def omnimem_copy_pages_quant(k_pages: torch.Tensor, v_pages: torch.Tensor, scales: torch.Tensor, pairs: torch.Tensor,
+                          count: Optional[torch.Tensor] = None, *, stream=None) -> None:
+    """omnimem_copy_pages of 8-bit pages with their scales: pools [num_pages, H, B, d] and scales [num_pages,
+    H, 2], or, for several layers in one call, [layers, num_pages, ...] of all three."""
+    dev = k_pages.get_device()
+    if dev >= 0 and (stream is not None or dev != _current_device()):
+        with _elsewhere(k_pages, stream):
+            return omnimem_copy_pages_quant(k_pages, v_pages, scales, pairs, count)
+    shape = k_pages.shape
+    _need(len(shape) in (4, 5), "k_pages must be [num_pages, H, B, d] or [layers, num_pages, H, B, d]")
+    layers = 1 if len(shape) == 4 else shape[0]
+    step, scale_step = (0, 0) if len(shape) == 4 else (k_pages.stride(0), scales.stride(0))
+    for name, t, want, dtype in (("k_pages", k_pages, shape, _E4M3), ("v_pages", v_pages, shape, _E4M3),
+                                 ("scales", scales, shape[:-2] + (2,), torch.float32)):
+        _need(isinstance(t, torch.Tensor) and t.dtype is dtype, f"{name} must be {dtype}")
+        _need(t.shape == want, f"{name} must have shape {tuple(want)}, not {tuple(t.shape)}")
+        if not t.is_contiguous():   # layers may lie apart
+            _need(len(shape) == 5 and layers > 0 and t[0].is_contiguous(), f"{name} must be contiguous")
+    _need(layers <= 1 or v_pages.stride(0) == step, "v_pages must have k_pages' distance between layers")
+    _need(isinstance(pairs, torch.Tensor) and pairs.dim() == 2, "pairs must be an [n, 2] tensor")
+    n = pairs.shape[0]
+    _check_tensor("pairs", pairs, (n, 2), torch.int32)
+    _need(n <= _I32_MAX, "pairs must hold fewer than 2^31 pairs")
+    if count is not None:
+        _need(isinstance(count, torch.Tensor) and count.dtype is torch.int32 and count.numel() >= 1 and
+              count.is_contiguous(), "count must be an int32 tensor")
+    _on_gpu(k_pages, "k_pages", v_pages=v_pages, scales=scales, pairs=pairs, count=count)
+    st = lib().omnimem_copy_pages_quant(k_pages.data_ptr(), v_pages.data_ptr(), scales.data_ptr(), shape[-4], shape[-3],
+                                     shape[-2], shape[-1], layers, step if layers > 1 else 0,
+                                     4 * scale_step if layers > 1 else 0, pairs.data_ptr(), _ptr(count), n,
+                                     _current_raw_stream())
+    if st != 0:
+        _check(st, "omnimem_copy_pages_quant")
 
 
 # ------------------------------------------------------------ LRU hot cache

@@ -1,0 +1,258 @@
+"""omnimem_decode_attn_quant against fp64: types, head sizes, block and chunk sizes, groups of 1 to 40
+query heads, lengths around each border, windows, pages that are not resident, scales that are
+no powers of two.  Slots that hold no token of a sequence are NaN codes, and scales of pages
+that no sequence has are NaN, in every case."""
+import math
+
+import pytest
+import torch
+
+import quant_oracle
+import seq_oracle
+from parity import say
+from paper_2605_30519_amd import (OmniMemError, SeqKVCacheQuant, omnimem_decode_attn_quant,
+                                  omnimem_decode_quant_workspace_bytes)
+from paper_2605_30519_amd.omnimem import workspace_tensor
+
+pytestmark = pytest.mark.gpu
+BF16, F32, F8 = torch.bfloat16, torch.float32, torch.float8_e4m3fn
+
+
+@pytest.fixture(scope="module")
+def dev():
+    d = torch.device("cuda:0")
+    torch.cuda.set_device(d)
+    return d
+
+
+def build(dev, H, d, B, S, lens, seed, extra_blocks=1, spare=3, powers=True):
+    """A cache of the given lengths over shuffled pages, values of size 1, NaN wherever no token lies."""
+    g = torch.Generator().manual_seed(seed)
+    nb = [seq_oracle.blocks(t, S, B) for t in lens]
+    M = max(nb + [0]) + extra_blocks
+    P = sum(nb) + spare
+    ids = torch.randperm(P, generator=g).tolist()
+    table = [[ids.pop() for _ in range(n)] + [-5] * (M - n) for n in nb]
+    k = torch.full((P, H, B, d), quant_oracle.NAN_CODE, dtype=torch.uint8)
+    v = torch.full_like(k, 0xff)
+    scales = torch.exp2(torch.randint(-9, 4, (P, H, 2), generator=g).float())
+    if not powers:
+        scales *= 1 + torch.rand((P, H, 2), generator=g)
+    for row, t in zip(table, lens):
+        if t == 0:
+            continue
+        block, slot = (torch.tensor(x) for x in zip(*(seq_oracle.place(x, S, B) for x in range(t))))
+        page = torch.tensor(row)[block]
+        for which, pool in enumerate((k, v)):
+            x = torch.randn((t, H, d), generator=g)
+            pool[page, :, slot] = (x / scales[page, :, which, None]).clamp(-448, 448).to(F8).view(torch.uint8)
+    for p in ids:
+        scales[p] = float("nan")
+    cache = SeqKVCacheQuant(k.to(dev).view(F8), v.to(dev).view(F8), scales.to(dev),
+                            torch.tensor(table, dtype=torch.int32, device=dev).view(len(lens), M),
+                            torch.tensor(lens, dtype=torch.int32, device=dev), S)
+    return cache, g
+
+
+def queries(dev, dtype, N, Hq, d, g, std=1.5):
+    return (std * torch.randn((N, Hq, d), generator=g)).to(dtype).to(dev)
+
+
+def check(cache, q, window=0, scale=None, **kw):
+    B, d = cache.k_pages.shape[2:]
+    out, lse = omnimem_decode_attn_quant(cache, q, scale, window=window, **kw)
+    torch.cuda.synchronize()
+    O, L, ob, lb = quant_oracle.decode(q, cache.k_pages, cache.v_pages, cache.scales, cache.page_table, cache.seq_lens, B,
+                                       cache.chunk_tokens or B, window, scale or 1 / math.sqrt(d))
+    got, gl = out.double().cpu(), lse.double().cpu()
+    assert not torch.isnan(got).any() and not torch.isnan(gl).any()
+    empty = torch.isinf(L)
+    assert torch.equal(torch.isinf(gl), empty) and (gl[empty] < 0).all()
+    assert (got.transpose(0, 1)[empty] == 0).all()
+    over = ((got - O).abs() - ob).max().item()
+    assert over <= 0, f"O is {over:.3g} past its bound"
+    diff = ((gl - L).abs() - lb)[~empty]
+    assert diff.numel() == 0 or diff.max().item() <= 0, f"lse is {diff.max().item():.3g} past its bound"
+    return out, lse
+
+
+EDGES = [0, 1, 2, 15, 16, 17, 31, 32, 33, 63, 64, 65, 127, 128, 129, 255, 256, 257, 300, 0]
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("d,B,H,G", [(128, 64, 3, 1), (64, 64, 2, 5), (128, 128, 2, 5), (64, 128, 3, 1)])
+def test_lengths_around_every_border(dev, dtype, d, B, H, G):
+    say(f"decode edges {dtype} d={d} B={B} H={H} G={G}")
+    cache, g = build(dev, H, d, B, B, EDGES, 1)
+    check(cache, queries(dev, dtype, len(EDGES), H * G, d, g))
+
+
+@pytest.mark.parametrize("dtype,d", [(BF16, 128), (F32, 128), (BF16, 64), (F32, 64)])
+@pytest.mark.parametrize("G", [2, 15, 16, 17, 32, 33, 40])
+def test_query_heads_per_key_head(dev, dtype, d, G):
+    say(f"decode groups {dtype} d={d} G={G}")
+    cache, g = build(dev, 2, d, 64, 64, [200, 0, 70, 3000], 2)
+    check(cache, queries(dev, dtype, 4, 2 * G, d, g))
+
+
+@pytest.mark.parametrize("dtype,d,B,S", [(BF16, 128, 64, 100), (F32, 64, 64, 130), (BF16, 64, 128, 200), (F32, 128, 128, 70),
+                                         (BF16, 128, 64, 1), (BF16, 128, 64, 256), (BF16, 64, 128, 4680)])
+def test_chunks_with_partial_blocks(dev, dtype, d, B, S):
+    lens = [0, 1, S, S + 1, max(S - 1, 0), 2 * S, 3 * S + 70 % S] if S < 4680 else [4680, 4681, 9000]
+    say(f"decode chunks {dtype} d={d} B={B} S={S} lens={lens}")
+    cache, g = build(dev, 2, d, B, S, lens, 3)
+    for window in (0, 1, 90):
+        check(cache, queries(dev, dtype, len(lens), 4, d, g), window)
+
+
+@pytest.mark.parametrize("dtype,B,S", [(BF16, 64, 64), (F32, 128, 128), (BF16, 128, 300), (F32, 64, 4000)])
+@pytest.mark.parametrize("window", [1, 63, 64, 65, 200, 1000, 2 ** 31 - 1])
+def test_windows(dev, dtype, B, S, window):
+    """The tokens before a window, in its first block too, are NaN here, and so are the scales of pages
+    before it."""
+    lens = [0, 1, 64, 65, 128, 500, 1100]
+    say(f"decode window {dtype} B={B} S={S} window={window}")
+    cache, g = build(dev, 2, 128, B, S, lens, 4)
+    rows = cache.page_table.tolist()
+    for row, t in zip(rows, lens):
+        begin = max(0, t - window)
+        for x in range(begin):
+            b, s = seq_oracle.place(x, S, B)
+            cache.k_pages.view(torch.uint8)[row[b], :, s] = 0x7f
+            cache.v_pages.view(torch.uint8)[row[b], :, s] = 0x7f
+            if b < seq_oracle.place(begin, S, B)[0]:
+                cache.scales[row[b]] = float("nan")
+    check(cache, queries(dev, dtype, len(lens), 6, 128, g), window)
+
+
+def test_pages_not_resident(dev):
+    cache, g = build(dev, 2, 128, 64, 64, [640, 64, 130, 500], 5)
+    t = cache.page_table
+    t[0, 1] = -1
+    t[0, 4] = 2 ** 30           # no such page
+    t[0, 9] = cache.k_pages.shape[0]
+    t[1, 0] = -1                # nothing left
+    t[3, 0:8] = torch.tensor([-1, -1, int(t[3, 2]), -1, -1, -1, -1, -1])
+    out, lse = check(cache, queries(dev, BF16, 4, 4, 128, g))
+    assert (out[1] == 0).all() and torch.isinf(lse[:, 1]).all()
+
+
+def test_lengths_past_the_row_and_below_zero(dev):
+    cache, g = build(dev, 1, 64, 64, 64, [128, 128, 64], 6, extra_blocks=0)
+    cache.seq_lens.copy_(torch.tensor([2 ** 31 - 1, -3, 64]))
+    check(cache, queries(dev, F32, 3, 1, 64, g))
+
+
+@pytest.mark.parametrize("dtype,d", [(BF16, 128), (F32, 64)])
+def test_scales_of_any_kind(dev, dtype, d):
+    cache, g = build(dev, 3, d, 64, 64, [1000, 77, 64, 5000], 7, powers=False)
+    check(cache, queries(dev, dtype, 4, 6, d, g))
+
+
+def test_scales_far_apart(dev):
+    """V's scales from 2^-100 to 2^100 in one sequence: each block's share of the sum is right."""
+    cache, g = build(dev, 1, 128, 64, 64, [640], 8)
+    n = torch.arange(10, device=dev)
+    cache.scales[cache.page_table[0, :10].long(), 0, 0] = 2.0 ** -6
+    cache.scales[cache.page_table[0, :10].long(), 0, 1] = torch.exp2(-100 + 200 * n / 9).round().float()
+    for dtype in (F32, BF16):
+        check(cache, queries(dev, dtype, 1, 4, 128, g))
+
+
+def test_codes_of_every_value(dev):
+    """All finite codes, one token a sequence: the output is the value."""
+    finite = [c for c in range(256) if c & 127 != 127]
+    N = 2
+    codes = torch.tensor((finite + finite[:2]), dtype=torch.uint8, device=dev).view(N, 128)
+    k = torch.zeros((N, 1, 64, 128), dtype=torch.uint8, device=dev)
+    v = k.clone()
+    v[:, 0, 0] = codes
+    scales = torch.ones((N, 1, 2), device=dev)
+    cache = SeqKVCacheQuant(k.view(F8), v.view(F8), scales, torch.arange(N, dtype=torch.int32, device=dev).view(N, 1),
+                            torch.ones(N, dtype=torch.int32, device=dev))
+    for dtype in (BF16, F32):
+        out, lse = omnimem_decode_attn_quant(cache, torch.ones((N, 1, 128), dtype=dtype, device=dev))
+        assert torch.equal(out[:, 0].cpu().double(), quant_oracle.values(codes.cpu())) and (lse == 0).all()
+    # and as keys: q picks one dim
+    cache.k_pages.view(torch.uint8)[:, 0, 0] = codes
+    for dim in range(0, 128, 9):
+        q = torch.zeros((N, 1, 128), device=dev)
+        q[:, 0, dim] = 1
+        lse = omnimem_decode_attn_quant(cache, q, 1.0)[1]
+        want = quant_oracle.values(codes[:, dim].cpu())
+        assert ((lse[0].cpu().double() - want).abs() <= 4 * 2.0 ** -24 * want.abs()).all(), dim
+
+
+def test_fp32_queries_keep_all_bits(dev):
+    """Scores in which what a query's third eight bits hold is left, 2^-17 of it times a key of 448."""
+    k = torch.zeros((1, 1, 64, 64), dtype=torch.uint8, device=dev)
+    v = k.clone()
+    k[0, 0, 0, :2] = torch.tensor([0x7e, 0xfe])     # 448, -448
+    k[0, 0, 0, 2] = 0x38
+    cache = SeqKVCacheQuant(k.view(F8), v.view(F8), torch.ones((1, 1, 2), device=dev),
+                            torch.zeros((1, 1), dtype=torch.int32, device=dev), torch.ones(1, dtype=torch.int32, device=dev))
+    q = torch.zeros((1, 1, 64), device=dev)
+    q[0, 0, 0] = 1 + 2.0 ** -17
+    q[0, 0, 1] = 1
+    lse = omnimem_decode_attn_quant(cache, q, 1.0)[1]
+    # the running sum's rounding is 448 u a step, the number itself 128 of them
+    assert abs(float(lse) - 448 * 2.0 ** -17) <= 8 * 448 * 2.0 ** -24
+    q[0, 0, :2] = 0
+    q[0, 0, 2] = 1 + 2.0 ** -17
+    assert abs(float(omnimem_decode_attn_quant(cache, q, 1.0)[1]) - (1 + 2.0 ** -17)) <= 5 * 2.0 ** -24
+
+
+def test_probabilities_keep_their_bits(dev):
+    """Two keys whose values cancel but for what a probability's low bits hold."""
+    N, H, d = 1, 1, 64
+    k = torch.zeros((1, 1, 64, d), dtype=torch.uint8, device=dev)
+    v = k.clone()
+    k[0, 0, 1, 0] = 0x38
+    v[0, 0, 0] = 0x38
+    v[0, 0, 1] = 0xb8      # 1 and -1
+    cache = SeqKVCacheQuant(k.view(F8), v.view(F8), torch.ones((1, 1, 2), device=dev), torch.zeros((1, 1), dtype=torch.int32, device=dev),
+                            torch.full((1,), 2, dtype=torch.int32, device=dev))
+    for dtype in (BF16, F32):
+        for x in (0.01, 0.11, 0.37):
+            q = torch.zeros((1, 1, d), dtype=dtype, device=dev)
+            q[0, 0, 0] = x
+            out = omnimem_decode_attn_quant(cache, q, 1.0)[0].double().cpu()
+            s = float(q[0, 0, 0].double())
+            want = -math.tanh(s / 2)
+            # the two probabilities are 2^-22 off each, their pieces in bf16 2^-15
+            tol = 2.0 ** -20 + (2.0 ** -15 + 2.0 ** -8 * abs(want) if dtype is BF16 else 0)
+            assert (out - want).abs().max() <= tol, (dtype, x)
+
+
+def test_strided_queries_outputs_and_workspaces(dev):
+    cache, g = build(dev, 4, 128, 64, 64, [3000, 40, 500], 9)
+    for dtype in (BF16, F32):
+        fused = queries(dev, dtype, 3, 24, 128, g)
+        q = fused[:, 4:12]
+        want = check(cache, q.contiguous())
+        need = omnimem_decode_quant_workspace_bytes(cache, 8)
+        assert need > 256
+        ws, out, lse = workspace_tensor(need, dev), torch.empty_like(q.contiguous()), torch.empty((8, 3), device=dev)
+        ws.fill_(0xff)
+        omnimem_decode_attn_quant(cache, q, out=out, lse=lse, workspace=ws)
+        assert torch.equal(out, want[0]) and torch.equal(lse, want[1])
+        alone, none = omnimem_decode_attn_quant(cache, q, want_lse=False)
+        assert none is None and torch.equal(alone, out)
+    with pytest.raises(ValueError, match="workspace holds"):
+        omnimem_decode_attn_quant(cache, q, workspace=ws[:256])
+    with pytest.raises(OmniMemError):
+        omnimem_decode_attn_quant(cache, q, -1.0)
+    for n in (0, 1):
+        c = SeqKVCacheQuant(cache.k_pages, cache.v_pages, cache.scales, cache.page_table[:n], cache.seq_lens[:n])
+        out, lse = omnimem_decode_attn_quant(c, q[:n])
+        assert out.shape == (n, 8, 128) and lse.shape == (8, n)
+
+
+def test_rows_and_splits_of_every_kind(dev):
+    """Many short items (a wave's each), long ragged ones (shares of a line), one long one."""
+    for dtype, d, H, lens in ((BF16, 128, 8, [60 + i % 60 for i in range(200)]), (F32, 64, 16, [1 + i for i in range(120)]),
+                              (BF16, 64, 2, [20000]), (F32, 128, 1, [9000, 1, 4000] + [100] * 30),
+                              (BF16, 128, 2, [700] * 3 + [0] * 70 + [1300] * 2)):
+        say(f"decode splits {dtype} d={d} H={H} n={len(lens)}")
+        cache, g = build(dev, H, d, 64, 64, lens, 10)
+        check(cache, queries(dev, dtype, len(lens), H, d, g))
