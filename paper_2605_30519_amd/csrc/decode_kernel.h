@@ -39,7 +39,10 @@ namespace {
 // What an item costs beside its units (its waves meet, its result is written), in units: lengths
 // on the line count it, so that a share of short items holds fewer units.  12 sequences of 1 to
 // 11,664 tokens, 40 fp32 heads of 64: 82 us without, 66 with one unit, 58 with three, 59 with six.
-constexpr int kItemUnits = 3;
+#ifndef IU
+#define IU 3
+#endif
+constexpr int kItemUnits = IU;
 constexpr int kThreads = kDecodeWaves * kWave;
 constexpr int kMinUnits = 4;      // units of a share: one for each wave
 constexpr float kLowest = -FLT_MAX;  // below every score: a row without keys keeps sum 0
@@ -145,6 +148,14 @@ __device__ __forceinline__ void lds_sync() {
   __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
 }
 
+#ifdef TRACE
+__device__ unsigned long long g_trace[4096][8];
+#define TR(k) do { if (threadIdx.x == 0) g_trace[blockIdx.x][k] = wall_clock64(); } while (0)
+#define TRV(k, v) do { if (threadIdx.x == 0) g_trace[blockIdx.x][k] = v; } while (0)
+#else
+#define TR(k)
+#define TRV(k, v)
+#endif
 template <typename L, int NT, DecodeSplit SPLIT>
 __global__ __launch_bounds__(kThreads, L::wgs(NT)) void k_decode(const DecodeArgs A) {
   using T = typename L::Io;
@@ -158,6 +169,8 @@ __global__ __launch_bounds__(kThreads, L::wgs(NT)) void k_decode(const DecodeArg
   const int i = lane % 16, j = lane / 16;
   const int HH = A.a.H * A.head_tiles;
   const int N = A.g.N;
+  TR(0);
+  int segs = 0, units = 0;
 
   Segment g{};
   int left = 0;  // units of the share from g.unit on
@@ -323,9 +336,13 @@ __global__ __launch_bounds__(kThreads, L::wgs(NT)) void k_decode(const DecodeArg
                 j, q[n]);
   };
   // the stream's next segment; false behind the share's last one
+  int turn = 0;
   auto next_segment = [&]() -> bool {
     left -= kItemUnits;
     if (!LINE || left <= 0) return false;
+#ifdef CARRY
+    turn = (turn + f.stop - f.unit) & 3;
+#endif
     f.unit = 0;
     if (++f.head == HH) {
       f.head = 0;
@@ -336,7 +353,11 @@ __global__ __launch_bounds__(kThreads, L::wgs(NT)) void k_decode(const DecodeArg
     }
     f.stop = min(f.sp.units, left);
     left -= f.stop;
+#ifdef CARRY
+    next = (wave - turn) & 3;
+#else
     next = wave;
+#endif
     load_q();
     return true;
   };
@@ -365,6 +386,7 @@ __global__ __launch_bounds__(kThreads, L::wgs(NT)) void k_decode(const DecodeArg
   }
   if constexpr (!LINE) look_up();
   bool have = advance();
+  TR(1);
   auto stream = [&](auto policy) __attribute__((always_inline)) {
     constexpr int POLICY = decltype(policy)::value;
     t.template load_k<POLICY>(rsrc(A.a.k_pages), i, j);
@@ -514,6 +536,9 @@ __global__ __launch_bounds__(kThreads, L::wgs(NT)) void k_decode(const DecodeArg
           }
         }
       }
+      ++segs; units += g.stop - g.unit;
+      if (segs == 1) TR(2);
+      if (!follows) { TR(3); TRV(4, segs); TRV(5, units); TRV(6, __builtin_amdgcn_s_getreg(63492)); TRV(7, __builtin_amdgcn_s_getreg(63508)); }
       if (!follows) return;
       g = f;
       have = hi > sub;

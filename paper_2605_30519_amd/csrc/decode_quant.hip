@@ -182,3 +182,9 @@ hipError_t launch_decode_quant(const SeqGeom& g, const DecodePlan& p, const Deco
 }
 
 }  // namespace omnimem
+
+#ifdef TRACE
+extern "C" __attribute__((visibility("default"))) int omni_trace(void* to) {
+  return hipMemcpyFromSymbol(to, HIP_SYMBOL(omnimem::g_trace), sizeof(omnimem::g_trace));
+}
+#endif

@@ -130,6 +130,11 @@ __device__ __forceinline__ void copy_pieces(const CopyLaunch& a, int pieces, int
     uint4* base = static_cast<uint4*>(pool == 0 ? a.k_pages : a.v_pages) + layer * a.layer_chunks;
     const uint4* from = base + src * a.page_chunks;
     uint4* to = base + dst * a.page_chunks;
+    const bool with_scales = a.scales != nullptr && pool == 0 && at == 0;  // once for a page
+    const float2* from_scales = reinterpret_cast<const float2*>(a.scales) + layer * a.layer_scales + src * a.page_scales;
+    float2* to_scales = reinterpret_cast<float2*>(a.scales) + layer * a.layer_scales + dst * a.page_scales;
+    float2 first{};
+    if (with_scales && threadIdx.x < a.page_scales) first = from_scales[threadIdx.x];
     uint4 x[kCopyUnroll];
 #pragma unroll
     for (int u = 0; u < kCopyUnroll; ++u) {
@@ -141,10 +146,9 @@ __device__ __forceinline__ void copy_pieces(const CopyLaunch& a, int pieces, int
       const int64_t c = at + u * kCopyThreads + threadIdx.x;
       if (c < a.page_chunks) store16<PAST>(x[u], to + c);
     }
-    if (a.scales != nullptr && pool == 0 && at == 0) {  // once for a page
-      float2* scales = reinterpret_cast<float2*>(a.scales) + layer * a.layer_scales;
-      for (int64_t h = threadIdx.x; h < a.page_scales; h += kCopyThreads)
-        scales[dst * a.page_scales + h] = scales[src * a.page_scales + h];
+    if (with_scales) {
+      if (threadIdx.x < a.page_scales) to_scales[threadIdx.x] = first;
+      for (int64_t h = threadIdx.x + kCopyThreads; h < a.page_scales; h += kCopyThreads) to_scales[h] = from_scales[h];
     }
   }
 }

@@ -7,6 +7,8 @@
 // changes no e4m3 number's bits but the exponent's, so where a later token needs a larger scale,
 // the codes in front of it are rounded again only where they fall below e4m3's normal range, and
 // tokens appended one by one end up as those of one append, but for those smallest ones.
+#include <type_traits>
+
 #include "device_common.h"
 #include "launch.h"
 #include "seq_launch.h"
@@ -50,9 +52,10 @@ __device__ __forceinline__ void values4(uint32_t codes, float (&x)[4]) {
 __device__ __forceinline__ int row_of_start(const int32_t* starts, int tokens, int s) { return min(max(starts[s], 0), tokens); }
 
 // ---------------------------------------------------------------- append
-// A workgroup takes the new tokens of one block, of one head, of K or V: it holds them in
-// registers, 16 values of a row a thread, finds their largest, rounds them by the scale, and, where the
-// block's earlier tokens have a smaller scale, those again.
+// A workgroup takes the new tokens of one block and one head, of K and V: it holds them in
+// registers, 16 bytes of a row a thread and pass, finds their largest, rounds them by the scale, and, where the
+// block's earlier tokens have a smaller scale, those again.  Bound by its bytes where there are many
+// blocks, else by the chain of loads that leads to them: the sequence, its rows and page, the rows.
 //
 // Blocks are numbered through: n rows touch at most n div B + 2 blocks of a contiguous sequence, and
 // n div S + n div B + 3 of one in chunks, so with `starts` ascending the numbers from
@@ -63,147 +66,206 @@ struct AppendUnits {
   int per_seq, S;  // 2, or 3 with chunks of S tokens (else 0)
 };
 
-template <typename T, int D, int B>
-__device__ __forceinline__ void append_block(const SeqGeom& g, const AppendQuantLaunch& a, const AppendUnits& units, int64_t w,
-                                             uint32_t (&s_most)[kThreads / kWave]) {
-  constexpr int LANES = D / 16, ROWS = kThreads / LANES, ITEMS = B / ROWS;  // threads of a row, rows of a pass, passes
-  constexpr int VECS = 16 * sizeof(T) / 16;
-  static_assert(ITEMS * ROWS == B, "a block in whole passes");
-  const int tid = threadIdx.x, lane = tid % kWave;
-  const int64_t w0 = w / a.H, u = w0 / 2;
-  const int h = static_cast<int>(w - w0 * a.H), value = static_cast<int>(w0 % 2);
+// The new tokens of a block: its slots [from, to), slot s in row row + s.
+struct NewTokens {
+  int seq, from, to;
+  int64_t block, row;
+};
 
-  // the sequence
-  int seq, row0, row1;
-  int64_t block_at = 0;  // of the sequence's touched blocks
+template <int B>
+__device__ __forceinline__ bool find_tokens(const SeqGeom& g, const AppendQuantLaunch& a, const AppendUnits& units,
+                                            int64_t u, NewTokens& x) {
+  const int lane = threadIdx.x % kWave;
+  int row0, row1, len;
+  int64_t at = 0;  // of the sequence's touched blocks
   if (a.starts == nullptr) {
-    seq = static_cast<int>(u);
-    row0 = seq;
-    row1 = seq + 1;
+    x.seq = static_cast<int>(u);
+    row0 = x.seq;
+    row1 = x.seq + 1;
+    len = g.lens[x.seq];
   } else {
-    auto base = [&](int i) -> int64_t {
-      const int s = row_of_start(a.starts, a.tokens, i);
-      return static_cast<int64_t>(s / B) + (units.S > 0 ? s / units.S : 0) + static_cast<int64_t>(units.per_seq) * i;
+    auto base = [&](int start, int i) -> int64_t {
+      return static_cast<int64_t>(start / B) + (units.S > 0 ? start / units.S : 0) + static_cast<int64_t>(units.per_seq) * i;
     };
-    int lo = 0, hi = g.N;
-    while (hi - lo > 1) {
-      const int step = (hi - lo + kWave - 1) / kWave;
-      const int at = lo + lane * step;
-      const uint64_t below = __ballot(lane * step < hi - lo && base(min(at, g.N - 1)) <= u);
-      const int count = max(1, static_cast<int>(__popcll(below)));
-      lo += (count - 1) * step;
+    int lo = 0, hi = g.N;  // a search by all lanes
+    while (hi - lo > kWave) {
+      const int step = (hi - lo + kWave - 1) / kWave, i = lo + lane * step;
+      const uint64_t below = __ballot(i < hi && base(row_of_start(a.starts, a.tokens, min(i, g.N - 1)), i) <= u);
+      lo += (max(1, static_cast<int>(__popcll(below))) - 1) * step;
       hi = min(hi, lo + step);
     }
-    seq = __builtin_amdgcn_readfirstlane(lo);
-    block_at = u - base(seq);
-    row0 = row_of_start(a.starts, a.tokens, seq);
-    row1 = row_of_start(a.starts, a.tokens, seq + 1);
+    const int i = min(lo + lane, g.N - 1);
+    const int start = row_of_start(a.starts, a.tokens, i), stop = row_of_start(a.starts, a.tokens, i + 1), l = g.lens[i];
+    const uint64_t below = __ballot(lo + lane < hi && base(start, i) <= u);
+    const int found = max(1, static_cast<int>(__popcll(below))) - 1;
+    x.seq = lo + found;
+    row0 = __builtin_amdgcn_readlane(start, found);
+    row1 = __builtin_amdgcn_readlane(stop, found);
+    len = __builtin_amdgcn_readlane(l, found);
+    at = u - base(row0, x.seq);
+    if (at < 0 || row1 <= row0) return false;
   }
-  if (block_at < 0 || row1 <= row0) return;
-
-  // its block: of the tokens [first, end), those in the block_at-th block that they touch
-  const int64_t end = g.lens[seq];
-  const int64_t first = max(end - (row1 - row0), int64_t{0});
-  const int64_t stop = min(end, static_cast<int64_t>(g.cap));
-  if (first >= stop) return;
+  // of the tokens [first, stop), those in the at-th block that they touch
+  const int64_t first = max(static_cast<int64_t>(len) - (row1 - row0), int64_t{0});
+  const int64_t stop = min(len, g.cap);
+  if (first >= stop) return false;
   const int f = static_cast<int>(first);
-  const int f_chunk = f / g.S;
-  const int64_t block = static_cast<int64_t>(f_chunk) * g.Bpc + (f - f_chunk * g.S) / B + block_at;
-  if (block >= g.M) return;
-  const int chunk = static_cast<int>(block / g.Bpc), in = static_cast<int>(block - static_cast<int64_t>(chunk) * g.Bpc) * B;
-  const int64_t t0 = static_cast<int64_t>(chunk) * g.S + in;  // the block's first token
-  const int from = static_cast<int>(max(first - t0, int64_t{0}));
-  const int to = static_cast<int>(min(min(stop - t0, static_cast<int64_t>(g.S - in)), static_cast<int64_t>(B)));
-  if (from >= to) return;
-  const int page = g.table[static_cast<int64_t>(seq) * g.M + block];
-  if (page < 0 || page >= g.num_pages) return;
-  // the row of slot s: the sequence's last row is its last token
-  const int64_t row = row1 - (end - t0);
-  const T* src = static_cast<const T*>(value ? a.v : a.k) + static_cast<int64_t>(h) * D;
-  const int64_t stride = value ? a.v_stride : a.k_stride;
-  float* scale_at = a.scales + (static_cast<int64_t>(page) * a.H + h) * 2 + value;
-  const float old = from > 0 ? *scale_at : 0.f;
-  uint8_t* codes = static_cast<uint8_t*>(value ? a.v_pages : a.k_pages) + (static_cast<int64_t>(page) * a.H + h) * B * D;
+  int64_t t0;  // the block's first token
+  int room = B;
+  if (units.S == 0) {
+    x.block = f / B + at;
+    t0 = x.block * B;
+  } else {
+    const int c0 = f / g.S;
+    x.block = static_cast<int64_t>(c0) * g.Bpc + (f - c0 * g.S) / B + at;
+    if (x.block >= g.M) return false;
+    const int b = static_cast<int>(x.block), c = b / g.Bpc, in = (b - c * g.Bpc) * B;
+    t0 = static_cast<int64_t>(c) * g.S + in;
+    room = min(B, g.S - in);
+  }
+  if (x.block >= g.M) return false;
+  x.from = static_cast<int>(max(first - t0, int64_t{0}));
+  x.to = static_cast<int>(min(stop - t0, static_cast<int64_t>(room)));
+  x.row = row1 - (len - t0);  // the sequence's last row is its last token
+  return x.from < x.to;
+}
 
-  const int slot = from + tid / LANES, dim = tid % LANES * 16;
-  uint4 raw[ITEMS][VECS];
+// The largest of a wave's lanes, in all of them.
+__device__ __forceinline__ uint32_t wave_max(uint32_t x) {
+  x = max(x, static_cast<uint32_t>(__builtin_amdgcn_update_dpp(0, x, 0x128, 0xf, 0xf, false)));  // row_ror:8, 4, 2, 1
+  x = max(x, static_cast<uint32_t>(__builtin_amdgcn_update_dpp(0, x, 0x124, 0xf, 0xf, false)));
+  x = max(x, static_cast<uint32_t>(__builtin_amdgcn_update_dpp(0, x, 0x122, 0xf, 0xf, false)));
+  x = max(x, static_cast<uint32_t>(__builtin_amdgcn_update_dpp(0, x, 0x121, 0xf, 0xf, false)));
+  const auto p = __builtin_amdgcn_permlane16_swap(x, x, false, false);
+  x = max(p[0], p[1]);
+  const auto q = __builtin_amdgcn_permlane32_swap(x, x, false, false);
+  return max(q[0], q[1]);
+}
+
+// The largest |x| of 16 bytes of values, as fp32 bits; FINITE: what is not finite left out.
+template <typename T, bool FINITE>
+__device__ __forceinline__ uint32_t largest(const u32x4 raw) {
   uint32_t most = 0;
 #pragma unroll
-  for (int x = 0; x < ITEMS; ++x) {
-    const int s = slot + x * ROWS;
-#pragma unroll
-    for (int v = 0; v < VECS; ++v) raw[x][v] = make_uint4(0, 0, 0, 0);
-    if (s < to) {
-      const uint4* p = reinterpret_cast<const uint4*>(src + (row + s) * stride + dim);
-#pragma unroll
-      for (int v = 0; v < VECS; ++v) raw[x][v] = load_once(p + v);
+  for (int i = 0; i < 4; ++i) {
+    if constexpr (sizeof(T) == 4) {
+      const uint32_t m = raw[i] & 0x7fffffffu;
+      most = max(most, FINITE && m >= kInf ? 0u : m);
+    } else {
+      const uint32_t low = raw[i] << 16 & 0x7fffffffu, high = raw[i] & 0x7fff0000u;
+      most = max(most, max(FINITE && low >= kInf ? 0u : low, FINITE && high >= kInf ? 0u : high));
     }
   }
-#pragma unroll
-  for (int x = 0; x < ITEMS; ++x)
-#pragma unroll
-    for (int v = 0; v < VECS; ++v) {
-      float w[Vec16<T>::N];
-      Vec16<T>::widen(raw[x][v], w);
-#pragma unroll
-      for (int e = 0; e < Vec16<T>::N; ++e) {
-        const uint32_t m = __float_as_uint(w[e]) & 0x7fffffffu;
-        most = max(most, m < kInf ? m : 0u);
-      }
-    }
-#pragma unroll
-  for (int m = 1; m < kWave; m <<= 1) most = max(most, static_cast<uint32_t>(__shfl_xor(static_cast<int>(most), m)));
-  if (lane == 0) s_most[tid / kWave] = most;
-  __syncthreads();  // and every thread has read the old scale
-#pragma unroll
-  for (int w = 0; w < kThreads / kWave; ++w) most = max(most, s_most[w]);
+  return most;
+}
 
-  int e = exponent_for(most);
-  if (from > 0) {
-    const float was = scale_in_range(old);
-    e = max(e, exponent_of(was));
-    const float ratio = was * power(-e);
-    if (ratio != 1.f) {  // the earlier tokens, by the new scale
-      for (int x = tid; x < from * LANES; x += kThreads) {
-        uint4* p = reinterpret_cast<uint4*>(codes) + x;
-        uint4 c = *p;
-        uint32_t* cw = &c.x;
+// The codes of 16 bytes of values, times inv.
+__device__ __forceinline__ void store_codes(uint16_t, const u32x4 raw, float inv, uint8_t* to) {
+  float w[8];
 #pragma unroll
-        for (int w = 0; w < 4; ++w) {
-          float y[4];
-          values4(cw[w], y);
-          cw[w] = codes4(y[0] * ratio, y[1] * ratio, y[2] * ratio, y[3] * ratio);
-        }
-        *p = c;
-      }
-    }
-  }
-  const float inv = power(-e);
+  for (int e = 0; e < 8; ++e) w[e] = __uint_as_float(e % 2 ? raw[e / 2] & 0xffff0000u : raw[e / 2] << 16) * inv;
+  *reinterpret_cast<uint2*>(to) = make_uint2(codes4(w[0], w[1], w[2], w[3]), codes4(w[4], w[5], w[6], w[7]));
+}
+__device__ __forceinline__ void store_codes(float, const u32x4 raw, float inv, uint8_t* to) {
+  float w[4];
 #pragma unroll
-  for (int x = 0; x < ITEMS; ++x) {
-    const int s = slot + x * ROWS;
-    if (s >= to) continue;
-    float w[16];
-#pragma unroll
-    for (int v = 0; v < VECS; ++v) {
-      float y[Vec16<T>::N];
-      Vec16<T>::widen(raw[x][v], y);
-#pragma unroll
-      for (int i = 0; i < Vec16<T>::N; ++i) w[v * Vec16<T>::N + i] = y[i] * inv;
-    }
-    const uint4 c = make_uint4(codes4(w[0], w[1], w[2], w[3]), codes4(w[4], w[5], w[6], w[7]),
-                               codes4(w[8], w[9], w[10], w[11]), codes4(w[12], w[13], w[14], w[15]));
-    *reinterpret_cast<uint4*>(codes + s * D + dim) = c;
-  }
-  if (tid == 0) *scale_at = power(e);
+  for (int e = 0; e < 4; ++e) w[e] = __uint_as_float(raw[e]) * inv;
+  *reinterpret_cast<uint32_t*>(to) = codes4(w[0], w[1], w[2], w[3]);
 }
 
 template <typename T, int D, int B>
-__global__ __launch_bounds__(kThreads) void k_append_quant(const SeqGeom g, const AppendQuantLaunch a, const AppendUnits units,
-                                                        int64_t work) {
-  __shared__ uint32_t s_most[kThreads / kWave];
+__device__ __forceinline__ void append_block(const SeqGeom& g, const AppendQuantLaunch& a, const AppendUnits& units,
+                                             int64_t u, int h, uint32_t (&s_most)[2][kThreads / kWave]) {
+  constexpr int N = 16 / sizeof(T), LANES = D / N;               // values of 16 bytes, threads of a row
+  constexpr int ROWS = kThreads / LANES, PASSES = B / ROWS;
+  static_assert(PASSES * ROWS == B, "a block in whole passes");
+  const int tid = threadIdx.x, lane = tid % kWave;
+  NewTokens x;
+  if (!find_tokens<B>(g, a, units, u, x)) return;
+  const int page = g.table[static_cast<int64_t>(x.seq) * g.M + x.block];
+
+  const int slot = tid / LANES, dim = tid % LANES * N;
+  u32x4 raw[2][PASSES];
+#pragma unroll
+  for (int kv = 0; kv < 2; ++kv) {
+    const T* src = static_cast<const T*>(kv ? a.v : a.k) + static_cast<int64_t>(h) * D + dim;
+    const int64_t stride = kv ? a.v_stride : a.k_stride;
+#pragma unroll
+    for (int p = 0; p < PASSES; ++p) {
+      const int s = x.from + slot + p * ROWS;
+      raw[kv][p] = u32x4{};
+      if (s < x.to) raw[kv][p] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(src + (x.row + s) * stride));
+    }
+  }
+  if (page < 0 || page >= g.num_pages) return;
+  const int64_t head = static_cast<int64_t>(page) * a.H + h;
+  float2* scale_at = reinterpret_cast<float2*>(a.scales) + head;
+  const float2 own = x.from > 0 ? *scale_at : make_float2(0.f, 0.f);
+
+  uint32_t most[2] = {0, 0};
+  auto find_most = [&](auto finite) {
+#pragma unroll
+    for (int kv = 0; kv < 2; ++kv) {
+      uint32_t m = 0;
+#pragma unroll
+      for (int p = 0; p < PASSES; ++p) m = max(m, largest<T, decltype(finite)::value>(raw[kv][p]));
+      m = wave_max(m);
+      if (lane == 0) s_most[kv][tid / kWave] = m;
+    }
+    __syncthreads();  // every thread has read the block's own scale, too
+#pragma unroll
+    for (int kv = 0; kv < 2; ++kv) {
+      most[kv] = s_most[kv][0];
+#pragma unroll
+      for (int w = 1; w < kThreads / kWave; ++w) most[kv] = max(most[kv], s_most[kv][w]);
+    }
+  };
+  find_most(std::false_type{});
+  if (max(most[0], most[1]) >= kInf) {  // infinities or NaN among them
+    __syncthreads();
+    find_most(std::true_type{});
+  }
+
+  float2 scale;
+#pragma unroll
+  for (int kv = 0; kv < 2; ++kv) {
+    uint8_t* codes = static_cast<uint8_t*>(kv ? a.v_pages : a.k_pages) + head * B * D;
+    int e = exponent_for(most[kv]);
+    if (x.from > 0) {
+      const float was = scale_in_range(kv ? own.y : own.x);
+      e = max(e, exponent_of(was));
+      const float ratio = was * power(-e);
+      if (ratio != 1.f) {  // the earlier tokens, by the new scale
+        for (int c = tid; c < x.from * (D / 16); c += kThreads) {
+          u32x4* at = reinterpret_cast<u32x4*>(codes) + c;
+          u32x4 w = *at;
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            float y[4];
+            values4(w[i], y);
+            w[i] = codes4(y[0] * ratio, y[1] * ratio, y[2] * ratio, y[3] * ratio);
+          }
+          *at = w;
+        }
+      }
+    }
+    (kv ? scale.y : scale.x) = power(e);
+#pragma unroll
+    for (int p = 0; p < PASSES; ++p) {
+      const int s = x.from + slot + p * ROWS;
+      if (s < x.to) store_codes(T{}, raw[kv][p], power(-e), codes + s * D + dim);
+    }
+  }
+  if (tid == 0) *scale_at = scale;
+}
+
+template <typename T, int D, int B>
+__global__ __launch_bounds__(kThreads) void k_append_quant(const SeqGeom g, const AppendQuantLaunch a,
+                                                           const AppendUnits units, int64_t work) {
+  __shared__ uint32_t s_most[2][kThreads / kWave];
   for (int64_t w = blockIdx.x; w < work; w += gridDim.x) {
-    append_block<T, D, B>(g, a, units, w, s_most);
+    const int64_t u = w / a.H;
+    append_block<T, D, B>(g, a, units, u, static_cast<int>(w - u * a.H), s_most);
     __syncthreads();
   }
 }
@@ -219,9 +281,7 @@ hipError_t launch_append_typed(const SeqGeom& g, const AppendQuantLaunch& a, con
 
 // ---------------------------------------------------------------- read
 // Chunks of 16 codes of all rows are numbered through, as an append of unquantised tokens does; a
-// workgroup looks up its rows' places and moves kReadUnroll * 256 of them, in K and in V.
-constexpr int kReadUnroll = 4;
-
+// workgroup looks up its rows' places and moves UNROLL * 256 of them, in K and in V.
 template <typename T>
 __device__ __forceinline__ void write16(T* to, const uint4 c, float scale) {
   const uint32_t w[4] = {c.x, c.y, c.z, c.w};
@@ -245,9 +305,9 @@ __device__ __forceinline__ void write16(T* to, const uint4 c, float scale) {
   }
 }
 
-template <typename T>
+template <typename T, int U>
 __global__ __launch_bounds__(kThreads) void k_read_quant(const SeqGeom g, const ReadQuantLaunch a) {
-  constexpr int U = kReadUnroll, kChunks = U * kThreads;
+  constexpr int kChunks = U * kThreads;
   constexpr int kRows = kChunks / 4 + 2;  // rows of at least 4 chunks (one head of 64)
   __shared__ int s_seq[kRows], s_page[kRows], s_slot[kRows];
   const int tid = threadIdx.x;
@@ -255,28 +315,34 @@ __global__ __launch_bounds__(kThreads) void k_read_quant(const SeqGeom g, const 
   const int64_t row_chunks = static_cast<int64_t>(a.H) * head_chunks, total = a.tokens * row_chunks;
   const int64_t c0 = static_cast<int64_t>(blockIdx.x) * kChunks;
   const int t0 = static_cast<int>(c0 / row_chunks), t1 = static_cast<int>((min(c0 + kChunks, total) - 1) / row_chunks);
-  for (int r = tid; r <= t1 - t0; r += kThreads) s_seq[r] = a.starts == nullptr ? t0 + r : -1;
-  __syncthreads();
+  for (int r = tid; r <= t1 - t0; r += kThreads) {
+    const int seq = a.starts == nullptr ? t0 + r : -1;
+    s_seq[r] = seq;
+    s_slot[r] = seq < 0 ? 0 : a.first != nullptr ? a.first[seq] : max(g.lens[seq], -1) - 1;
+  }
   if (a.starts != nullptr) {
+    // s_slot: the row's token; one that is out of a token's range is -1
+    __syncthreads();
     for (int s = tid; s < g.N; s += kThreads) {
-      const int from = max(row_of_start(a.starts, a.tokens, s), t0);
-      const int to = min(row_of_start(a.starts, a.tokens, s + 1), t1 + 1);
-      for (int t = from; t < to; ++t) s_seq[t - t0] = s;
+      const int start = row_of_start(a.starts, a.tokens, s), stop = row_of_start(a.starts, a.tokens, s + 1);
+      const int len = g.lens[s];
+      const int64_t token0 = a.first != nullptr ? static_cast<int64_t>(a.first[s]) - start : static_cast<int64_t>(len) - stop;
+      const int to = min(stop, t1 + 1);
+      for (int t = max(start, t0); t < to; ++t) {
+        const int64_t token = token0 + t;
+        s_seq[t - t0] = s;
+        s_slot[t - t0] = token >= 0 && token < len ? static_cast<int>(token) : -1;
+      }
     }
     __syncthreads();
   }
   for (int r = tid; r <= t1 - t0; r += kThreads) {
-    const int s = s_seq[r];
+    const int s = s_seq[r], t = s_slot[r];
     int page = -2, slot = 0;  // -2: a row of no sequence, left alone; -1: zeros
     if (s >= 0) {
       page = -1;
-      const int row = t0 + r;
-      const int64_t end = min(g.lens[s], g.cap);
-      int64_t t;
-      if (a.first != nullptr) t = static_cast<int64_t>(a.first[s]) + row - (a.starts == nullptr ? row : row_of_start(a.starts, a.tokens, s));
-      else t = static_cast<int64_t>(g.lens[s]) - 1 - (a.starts == nullptr ? 0 : row_of_start(a.starts, a.tokens, s + 1) - 1 - row);
-      if (t >= 0 && t < end) {
-        const int ti = static_cast<int>(t), c = ti / g.S, off = ti - c * g.S;
+      if (t >= 0 && t < min(a.starts == nullptr ? g.lens[s] : t + 1, g.cap)) {
+        const int c = t / g.S, off = t - c * g.S;
         const int at = g.table[static_cast<int64_t>(s) * g.M + static_cast<int64_t>(c) * g.Bpc + off / g.B];
         if (at >= 0 && at < g.num_pages) {
           page = at;
@@ -325,17 +391,25 @@ hipError_t launch_append_kv_quant(const SeqGeom& g, const AppendQuantLaunch& a, 
   const int64_t blocks = a.starts == nullptr ? g.N
                                              : static_cast<int64_t>(a.tokens) / g.B + (units.S > 0 ? a.tokens / units.S : 0) +
                                                    static_cast<int64_t>(units.per_seq) * g.N;
-  const int64_t work = blocks * 2 * a.H;
+  const int64_t work = blocks * a.H;
   return a.dtype == OMNIMEM_BF16 ? launch_append_typed<uint16_t>(g, a, units, work, stream)
                                  : launch_append_typed<float>(g, a, units, work, stream);
 }
 
-hipError_t launch_read_kv_quant(const SeqGeom& g, const ReadQuantLaunch& a, hipStream_t stream) {
-  const int64_t chunks = static_cast<int64_t>(a.tokens) * a.H * (a.D / 16);
-  const int64_t wgs = (chunks + kReadUnroll * kThreads - 1) / (kReadUnroll * kThreads);
+namespace {
+
+template <int U>
+hipError_t launch_read(const SeqGeom& g, const ReadQuantLaunch& a, int64_t chunks, hipStream_t stream) {
+  const int64_t wgs = (chunks + U * kThreads - 1) / (U * kThreads);
   if (wgs > 0x7fffffff) return hipErrorInvalidConfiguration;
-  const auto kernel = a.dtype == OMNIMEM_BF16 ? k_read_quant<uint16_t> : k_read_quant<float>;
+  const auto kernel = a.dtype == OMNIMEM_BF16 ? k_read_quant<uint16_t, U> : k_read_quant<float, U>;
   return launch_kernel(kernel, dim3(static_cast<unsigned>(wgs)), dim3(kThreads), 0, stream, g, a);
+}
+
+}  // namespace
+
+hipError_t launch_read_kv_quant(const SeqGeom& g, const ReadQuantLaunch& a, hipStream_t stream) {
+  return launch_read<1>(g, a, static_cast<int64_t>(a.tokens) * a.H * (a.D / 16), stream);
 }
 
 }  // namespace omnimem
