@@ -26,6 +26,7 @@ struct Tile<uint16_t, D> {
   static constexpr int kDim = D;
   static constexpr bool kScaled = false;
   static constexpr int wgs(int) { return 2; }
+  static constexpr bool kTwoPolicies = true;
   static constexpr int ROW = D * 2, KEYS = 8192 / ROW, KB = KEYS / 32, QS = ROW / 64, VW = D / 16;
   static constexpr int RT = KEYS / 16;  // 16-key row tiles
   static constexpr int UNIT = KEYS;
@@ -134,6 +135,7 @@ struct Tile<float, D> {
   static constexpr int kDim = D;
   static constexpr bool kScaled = false;
   static constexpr int wgs(int) { return 2; }
+  static constexpr bool kTwoPolicies = true;
   static constexpr int ROW = D * 4, KEYS = 8192 / ROW, RT = KEYS / 16, QS = ROW / 64, VW = D / 16, UNIT = 32;
   u32x4 k[RT][QS];
   u32x4 v[RT][4][VW / 4];

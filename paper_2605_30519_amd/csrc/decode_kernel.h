@@ -24,6 +24,7 @@
 //   RT, QS, VW          16-key row tiles, 16-byte words of a lane's part of a query, 16-dim tiles of O
 //   kScaled             pages have scales: codes count times them
 //   wgs(NT)             workgroups that a CU shall hold
+//   kTwoPolicies        pages that sequences share are looked for (a second loop)
 //   load_q, load_k, load_v, clear_v_below, scores, pv, key, dim
 #pragma once
 
@@ -39,10 +40,7 @@ namespace {
 // What an item costs beside its units (its waves meet, its result is written), in units: lengths
 // on the line count it, so that a share of short items holds fewer units.  12 sequences of 1 to
 // 11,664 tokens, 40 fp32 heads of 64: 82 us without, 66 with one unit, 58 with three, 59 with six.
-#ifndef IU
-#define IU 3
-#endif
-constexpr int kItemUnits = IU;
+constexpr int kItemUnits = 3;
 constexpr int kThreads = kDecodeWaves * kWave;
 constexpr int kMinUnits = 4;      // units of a share: one for each wave
 constexpr float kLowest = -FLT_MAX;  // below every score: a row without keys keeps sum 0
@@ -148,14 +146,6 @@ __device__ __forceinline__ void lds_sync() {
   __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
 }
 
-#ifdef TRACE
-__device__ unsigned long long g_trace[4096][8];
-#define TR(k) do { if (threadIdx.x == 0) g_trace[blockIdx.x][k] = wall_clock64(); } while (0)
-#define TRV(k, v) do { if (threadIdx.x == 0) g_trace[blockIdx.x][k] = v; } while (0)
-#else
-#define TR(k)
-#define TRV(k, v)
-#endif
 template <typename L, int NT, DecodeSplit SPLIT>
 __global__ __launch_bounds__(kThreads, L::wgs(NT)) void k_decode(const DecodeArgs A) {
   using T = typename L::Io;
@@ -169,8 +159,6 @@ __global__ __launch_bounds__(kThreads, L::wgs(NT)) void k_decode(const DecodeArg
   const int i = lane % 16, j = lane / 16;
   const int HH = A.a.H * A.head_tiles;
   const int N = A.g.N;
-  TR(0);
-  int segs = 0, units = 0;
 
   Segment g{};
   int left = 0;  // units of the share from g.unit on
@@ -336,13 +324,9 @@ __global__ __launch_bounds__(kThreads, L::wgs(NT)) void k_decode(const DecodeArg
                 j, q[n]);
   };
   // the stream's next segment; false behind the share's last one
-  int turn = 0;
   auto next_segment = [&]() -> bool {
     left -= kItemUnits;
     if (!LINE || left <= 0) return false;
-#ifdef CARRY
-    turn = (turn + f.stop - f.unit) & 3;
-#endif
     f.unit = 0;
     if (++f.head == HH) {
       f.head = 0;
@@ -353,11 +337,7 @@ __global__ __launch_bounds__(kThreads, L::wgs(NT)) void k_decode(const DecodeArg
     }
     f.stop = min(f.sp.units, left);
     left -= f.stop;
-#ifdef CARRY
-    next = (wave - turn) & 3;
-#else
     next = wave;
-#endif
     load_q();
     return true;
   };
@@ -373,7 +353,7 @@ __global__ __launch_bounds__(kThreads, L::wgs(NT)) void k_decode(const DecodeArg
   // the answer, and with more than 16 query heads to a key head a second loop costs registers that
   // there are not.
   bool shared = false;
-  if constexpr (LINE && NT == 1) {
+  if constexpr (LINE && NT == 1 && L::kTwoPolicies) {
     const int u = f.unit + lane;
     bool same = false;
     if (long_share && u < f.stop && N > 1) {
@@ -386,7 +366,6 @@ __global__ __launch_bounds__(kThreads, L::wgs(NT)) void k_decode(const DecodeArg
   }
   if constexpr (!LINE) look_up();
   bool have = advance();
-  TR(1);
   auto stream = [&](auto policy) __attribute__((always_inline)) {
     constexpr int POLICY = decltype(policy)::value;
     t.template load_k<POLICY>(rsrc(A.a.k_pages), i, j);
@@ -536,15 +515,12 @@ __global__ __launch_bounds__(kThreads, L::wgs(NT)) void k_decode(const DecodeArg
           }
         }
       }
-      ++segs; units += g.stop - g.unit;
-      if (segs == 1) TR(2);
-      if (!follows) { TR(3); TRV(4, segs); TRV(5, units); TRV(6, __builtin_amdgcn_s_getreg(63492)); TRV(7, __builtin_amdgcn_s_getreg(63508)); }
       if (!follows) return;
       g = f;
       have = hi > sub;
     }
   };
-  if constexpr (LINE && NT == 1) {
+  if constexpr (LINE && NT == 1 && L::kTwoPolicies) {
     if (shared) return stream(std::integral_constant<int, 0>{});
   }
   stream(std::integral_constant<int, kNontemporal>{});

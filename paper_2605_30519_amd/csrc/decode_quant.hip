@@ -39,7 +39,8 @@ struct TileQuant {
   static constexpr int KC = D / 64;  // 16-byte chunks of a lane's part of a key
   static constexpr int PIECES = kF32 ? 3 : 1, STEPS = 2 * KC, QS = STEPS * PIECES;
   static constexpr int P_PIECES = kF32 ? 3 : 2;
-  static constexpr int wgs(int nt) { return kF32 && nt == 2 && D == 128 ? 1 : 2; }
+  static constexpr int wgs(int nt) { return nt == 2 && D == 128 ? 1 : 2; }
+  static constexpr bool kTwoPolicies = !(kF32 && D == 128);
   typedef uint32_t vraw __attribute__((ext_vector_type(VW / 4)));  // a lane's V dims of one key
   u32x4 k[KB][2][KC];
   vraw v[KB][8];
@@ -182,9 +183,3 @@ hipError_t launch_decode_quant(const SeqGeom& g, const DecodePlan& p, const Deco
 }
 
 }  // namespace omnimem
-
-#ifdef TRACE
-extern "C" __attribute__((visibility("default"))) int omni_trace(void* to) {
-  return hipMemcpyFromSymbol(to, HIP_SYMBOL(omnimem::g_trace), sizeof(omnimem::g_trace));
-}
-#endif

@@ -114,42 +114,84 @@ __global__ __launch_bounds__(kAppendThreads) void k_append_kv(const SeqGeom g, c
 // pairs is read on the device.  Bound by its bytes: 300 pages of 12 heads x 64 x 128 bf16 in six
 // layers (1.4 GB read and written) 279 us, 5.1 TB/s, as a large tensor copy (5.0); 16 pages 4.2 us.
 constexpr int kCopyThreads = 256, kCopyUnroll = 4, kCopyPiece = kCopyThreads * kCopyUnroll;
-constexpr int kCopyMaxWgs = 2048;
+constexpr int kCopyMaxWgs = 1536;
 
+// A workgroup's piece: 16 KB of a page, from its chunk `at` on, and with a page's first piece of the
+// first pool its scales.
+struct Piece {
+  const uint4* from;
+  uint4* to;
+  int64_t at;
+  const float2* from_scales;  // null: none
+  float2* to_scales;
+  bool real;
+};
+
+__device__ __forceinline__ Piece piece_of(const CopyLaunch& a, int pieces, int pools, int64_t per_pair, int64_t w) {
+  const int64_t p = w / per_pair;
+  const int64_t rest = w - p * per_pair;
+  const int64_t lp = rest / pieces;
+  const int layer = static_cast<int>(lp / pools), pool = static_cast<int>(lp % pools);
+  Piece x{};
+  x.at = (rest - lp * pieces) * kCopyPiece;
+  const int src = a.pairs[2 * p], dst = a.pairs[2 * p + 1];
+  x.real = src >= 0 && src < a.num_pages && dst >= 0 && dst < a.num_pages;
+  uint4* base = static_cast<uint4*>(pool == 0 ? a.k_pages : a.v_pages) + layer * a.layer_chunks;
+  x.from = base + src * a.page_chunks;
+  x.to = base + dst * a.page_chunks;
+  if (a.scales != nullptr && pool == 0 && x.at == 0) {
+    float2* scales = reinterpret_cast<float2*>(a.scales) + layer * a.layer_scales;
+    x.from_scales = scales + src * a.page_scales;
+    x.to_scales = scales + dst * a.page_scales;
+  }
+  return x;
+}
+
+__device__ __forceinline__ void load_piece(const CopyLaunch& a, const Piece& x, uint4 (&data)[kCopyUnroll], float2& scale) {
+  if (!x.real) return;
+  if (x.from_scales != nullptr && threadIdx.x < a.page_scales) scale = x.from_scales[threadIdx.x];
+#pragma unroll
+  for (int u = 0; u < kCopyUnroll; ++u) {
+    const int64_t c = x.at + u * kCopyThreads + threadIdx.x;
+    if (c < a.page_chunks) data[u] = load_once(x.from + c);
+  }
+}
+
+// The next piece's loads are out before the present one is stored.
 template <bool PAST>
 __device__ __forceinline__ void copy_pieces(const CopyLaunch& a, int pieces, int pools, int64_t per_pair,
                                             int64_t total) {
-  for (int64_t w = blockIdx.x; w < total; w += gridDim.x) {
-    const int64_t p = w / per_pair;
-    const int64_t rest = w - p * per_pair;
-    const int64_t lp = rest / pieces;
-    const int layer = static_cast<int>(lp / pools), pool = static_cast<int>(lp % pools);
-    const int64_t at = (rest - lp * pieces) * kCopyPiece;
-    const int src = a.pairs[2 * p], dst = a.pairs[2 * p + 1];
-    if (src < 0 || src >= a.num_pages || dst < 0 || dst >= a.num_pages) continue;
-    uint4* base = static_cast<uint4*>(pool == 0 ? a.k_pages : a.v_pages) + layer * a.layer_chunks;
-    const uint4* from = base + src * a.page_chunks;
-    uint4* to = base + dst * a.page_chunks;
-    const bool with_scales = a.scales != nullptr && pool == 0 && at == 0;  // once for a page
-    const float2* from_scales = reinterpret_cast<const float2*>(a.scales) + layer * a.layer_scales + src * a.page_scales;
-    float2* to_scales = reinterpret_cast<float2*>(a.scales) + layer * a.layer_scales + dst * a.page_scales;
-    float2 first{};
-    if (with_scales && threadIdx.x < a.page_scales) first = from_scales[threadIdx.x];
-    uint4 x[kCopyUnroll];
+  int64_t w = blockIdx.x;
+  if (w >= total) return;
+  Piece x = piece_of(a, pieces, pools, per_pair, w);
+  uint4 data[kCopyUnroll] = {};
+  float2 scale{};
+  load_piece(a, x, data, scale);
+  while (true) {
+    w += gridDim.x;
+    Piece next{};
+    uint4 next_data[kCopyUnroll] = {};
+    float2 next_scale{};
+    if (w < total) {
+      next = piece_of(a, pieces, pools, per_pair, w);
+      load_piece(a, next, next_data, next_scale);
+    }
+    if (x.real) {
 #pragma unroll
-    for (int u = 0; u < kCopyUnroll; ++u) {
-      const int64_t c = at + u * kCopyThreads + threadIdx.x;
-      if (c < a.page_chunks) x[u] = load_once(from + c);
+      for (int u = 0; u < kCopyUnroll; ++u) {
+        const int64_t c = x.at + u * kCopyThreads + threadIdx.x;
+        if (c < a.page_chunks) store16<PAST>(data[u], x.to + c);
+      }
+      if (x.from_scales != nullptr) {
+        if (threadIdx.x < a.page_scales) x.to_scales[threadIdx.x] = scale;
+        for (int64_t h = threadIdx.x + kCopyThreads; h < a.page_scales; h += kCopyThreads) x.to_scales[h] = x.from_scales[h];
+      }
     }
+    if (w >= total) return;
+    x = next;
+    scale = next_scale;
 #pragma unroll
-    for (int u = 0; u < kCopyUnroll; ++u) {
-      const int64_t c = at + u * kCopyThreads + threadIdx.x;
-      if (c < a.page_chunks) store16<PAST>(x[u], to + c);
-    }
-    if (with_scales) {
-      if (threadIdx.x < a.page_scales) to_scales[threadIdx.x] = first;
-      for (int64_t h = threadIdx.x + kCopyThreads; h < a.page_scales; h += kCopyThreads) to_scales[h] = from_scales[h];
-    }
+    for (int u = 0; u < kCopyUnroll; ++u) data[u] = next_data[u];
   }
 }
 

@@ -87,9 +87,16 @@ constexpr int64_t kDecodeWgs = 256, kDecodeManyWgs = 512;
 constexpr int64_t kItemUnitsMost = 20, kWaveUnitsMost = 8, kWaveItems = 1024;
 constexpr int64_t kItemOverhead = 64;  // of an item's length on the line, no less than the kernel adds
 
-// unit: tokens of a unit
-omnimem_status_t plan_decode(int32_t num_heads, int32_t head_dim, int64_t unit, const SeqGeom& g, int32_t num_q_heads,
-                             int32_t window, DecodePlan& p) {
+// What a plan goes by, of a kind of pages: tokens of a unit; units of the longest item that is a
+// workgroup's, and of one that a window bounds where there is an item for each CU; workgroups of a line
+// where there are no more items than CUs and where there are, and of one with two column tiles (0: no
+// other rule).
+struct DecodeTuning {
+  int64_t unit, item_units, window_units, wgs, many_wgs, wide_wgs;
+};
+
+omnimem_status_t plan_decode(int32_t num_heads, int32_t head_dim, const DecodeTuning& t, const SeqGeom& g,
+                             int32_t num_q_heads, int32_t window, DecodePlan& p) {
   if (num_q_heads < 1 || num_q_heads % num_heads != 0) return OMNIMEM_EINVAL;
   p.G = num_q_heads / num_heads;
   p.tile_rows = p.G <= kDecodeHeadRows ? kDecodeHeadRows : 2 * kDecodeHeadRows;
@@ -103,16 +110,17 @@ omnimem_status_t plan_decode(int32_t num_heads, int32_t head_dim, int64_t unit, 
     const int64_t runs = g.Bpc == 1 && g.S == g.B ? 1 : int64_t{window} / g.S + 2;
     blocks = window / g.B + 2 * runs < blocks ? window / g.B + 2 * runs : blocks;
   }
-  const int64_t units = blocks * (g.B / unit);
+  const int64_t unit = t.unit, units = blocks * (g.B / unit);
   // a sum of the sequences' units in 31 bits, positions on the line in 40
   if (items > 0x7fffffff / 256 || static_cast<int64_t>(g.N) * (static_cast<int64_t>(g.M) * (g.B / unit) + kItemOverhead) > 0x7fffffff ||
       (items > 0 && units > (int64_t{1} << 40) / items))
     return OMNIMEM_EINVAL;
+  const int64_t item_units = window > 0 && items >= kDecodeWgs ? t.window_units : t.item_units;
   p.split = units <= kWaveUnitsMost && items >= kWaveItems ? DecodeSplit::kWave
-            : units <= kItemUnitsMost                         ? DecodeSplit::kItem
+            : units <= item_units                             ? DecodeSplit::kItem
                                                               : DecodeSplit::kLine;
   const int64_t most = items * (units + kItemOverhead);
-  const int64_t wgs = items > kDecodeWgs ? kDecodeManyWgs : kDecodeWgs;
+  const int64_t wgs = p.tile_rows > kDecodeHeadRows && t.wide_wgs > 0 ? t.wide_wgs : items > kDecodeWgs ? t.many_wgs : t.wgs;
   if (most > wgs * 0x7fffffff) return OMNIMEM_EINVAL;  // a workgroup's share of the line in 31 bits
   p.wgs = static_cast<int>(p.split == DecodeSplit::kLine   ? (most < wgs ? most : wgs)
                            : p.split == DecodeSplit::kItem ? items
@@ -129,13 +137,23 @@ omnimem_status_t plan_decode(int32_t num_heads, int32_t head_dim, int64_t unit, 
 
 omnimem_status_t plan_decode(const omnimem_seq_cache_t* sc, const SeqGeom& g, int32_t num_q_heads, int32_t window,
                              DecodePlan& p) {
-  const int64_t unit = sc->dtype == OMNIMEM_BF16 && sc->head_dim == 64 ? 64 : 32;
-  return plan_decode(sc->num_heads, sc->head_dim, unit, g, num_q_heads, window, p);
+  const DecodeTuning t{sc->dtype == OMNIMEM_BF16 && sc->head_dim == 64 ? 64 : 32, kItemUnitsMost, kItemUnitsMost, kDecodeWgs,
+                       kDecodeManyWgs, 0};
+  return plan_decode(sc->num_heads, sc->head_dim, t, g, num_q_heads, window, p);
 }
 
+// 8-bit pages (the kernels' times, with the join's, in a graph).  A wave's tile of 64-dim heads is 8 KB
+// instead of 16, so two workgroups a CU: 12 sequences of 4,000 to 30,000 tokens, 16 key heads, 62.7 ->
+// 58.3 us; an item of one goes twice as far: a window of 1,560 tokens, 256 items 23.6 -> 12.7, 4 items
+// 10.2 -> 11.6, but a launch less.  Two column tiles of 128-dim heads need a CU's registers for one workgroup:
+// 16 sequences of 3,000 to 9,000 tokens, 17 query heads on each of 4, bf16, 36.0 -> 32.9 (two spill).
+// Windows make items of one length: 256 of 2,400 tokens, bf16 heads of 128, 36.2 -> 28.1, fp32 heads of
+// 64 28.3 -> 17.1, where 32 items lose (15.4 -> 20.1, 14.0 -> 15.0).
 omnimem_status_t plan_decode(const omnimem_seq_cache_quant_t* sc, const SeqGeom& g, int32_t num_q_heads, int32_t window,
                              DecodePlan& p) {
-  return plan_decode(sc->num_heads, sc->head_dim, 64, g, num_q_heads, window, p);
+  const DecodeTuning t = sc->head_dim == 64 ? DecodeTuning{64, 28, 48, kDecodeManyWgs, kDecodeManyWgs, kDecodeManyWgs}
+                                            : DecodeTuning{64, 20, 48, kDecodeWgs, kDecodeManyWgs, kDecodeWgs};
+  return plan_decode(sc->num_heads, sc->head_dim, t, g, num_q_heads, window, p);
 }
 
 omnimem_status_t check_scratch(const void* workspace, size_t have, size_t need) {
