@@ -6,14 +6,16 @@ The functions carry the C names: omnimem_select, omnimem_sparse_attn,
 omnimem_dense_attn, omnimem_union_gather_attn, the compressed-history calls
 omnimem_compress_chunk, omnimem_select_compressed and omnimem_cmp_attn, Eq. 1's
 gated fusion omnimem_gated_combine, the sequence cache's omnimem_decode_attn,
-omnimem_append_kv, omnimem_copy_pages, omnimem_seq_update and omnimem_seq_compact, plus
-the host-side helpers.
+omnimem_append_kv, omnimem_copy_pages, omnimem_seq_update and omnimem_seq_compact, the 8-bit
+sequence cache's omnimem_decode_attn_quant, omnimem_append_kv_quant, omnimem_read_kv_quant and
+omnimem_copy_pages_quant, plus the host-side helpers.
 """
 from __future__ import annotations
 
 import ctypes
 import math
 import os
+import struct
 import threading
 from dataclasses import dataclass, replace
 from typing import Optional
@@ -249,7 +251,7 @@ def _configure(L, required: bool = True):
     L.omnimem_seq_update.restype = i32
     L.omnimem_seq_compact.argtypes = [stp, vp, vp, vp, vp, sz, vp]
     L.omnimem_seq_compact.restype = i32
-    qcp = ctypes.POINTER(omnimem_seq_cache_quant_t)
+    qcp = vp   # an omnimem_seq_cache_quant_t, by reference or as its bytes
     L.omnimem_decode_quant_workspace_bytes.argtypes = [qcp, i32, i32]
     L.omnimem_decode_quant_workspace_bytes.restype = sz
     L.omnimem_decode_attn_quant.argtypes = [qcp, i32, vp, i64, i32, i32, f32, vp, vp, vp, sz, vp]
@@ -1159,14 +1161,46 @@ class SeqKVCacheQuant:
         num_pages, H, B, d = shape
         _check_tensor("scales", sc, (num_pages, H, 2), torch.float32)
         seqs = _seq_table(pt, sl, num_pages, B, self.chunk_tokens)
-        dev = kp.get_device()
-        if dev < 0 or not vp.get_device() == dev == pt.get_device() == sl.get_device() == sc.get_device():
-            _on_gpu(kp, v_pages=vp, scales=sc, page_table=pt, seq_lens=sl)
+        _on_gpu(kp, v_pages=vp, scales=sc, page_table=pt, seq_lens=sl)
         return omnimem_seq_cache_quant_t(seqs, H, d, kp.data_ptr(), vp.data_ptr(), sc.data_ptr())
+
+    def packed(self) -> bytes:
+        """The descriptor's bytes: its checks in one condition, and itself where that fails."""
+        kp, vp, sc, pt, sl, S = self.k_pages, self.v_pages, self.scales, self.page_table, self.seq_lens, self.chunk_tokens
+        shape, rows = kp.shape, pt.shape
+        if len(shape) == 4 and len(rows) == 2:
+            P, H, B, d = shape
+            n, m = rows
+            dev = kp.get_device()
+            if (dev >= 0 and kp.dtype is _E4M3 and vp.dtype is _E4M3 and sc.dtype is _F32 and pt.dtype is _I32 and
+                    sl.dtype is _I32 and vp.shape == shape and sc.shape == (P, H, 2) and sl.shape == (n,) and
+                    kp.is_contiguous() and vp.is_contiguous() and sc.is_contiguous() and pt.is_contiguous() and
+                    sl.is_contiguous() and vp.get_device() == dev and sc.get_device() == dev and pt.get_device() == dev and
+                    sl.get_device() == dev and n * m <= _I32_MAX and 0 <= S <= _I32_MAX and
+                    max(H, B, d) <= _I32_MAX):
+                return _pack_quant(n, m, B, S or B, P, pt.data_ptr(), sl.data_ptr(), H, d, kp.data_ptr(), vp.data_ptr(),
+                                   sc.data_ptr())
+        return bytes(self.descriptor())
 
     def after(self, update: "SeqUpdate") -> "SeqKVCacheQuant":
         """The same pool under the tables of an update."""
         return replace(self, page_table=update.page_table, seq_lens=update.seq_lens)
+
+
+_F32, _I32 = torch.float32, torch.int32
+_pack_quant = struct.Struct("@iiiiqPPiiPPP").pack   # the fields of an omnimem_seq_cache_quant_t in a row
+
+
+def _quant_rows(t, heads: Optional[int], like: torch.Tensor, dtype) -> int:
+    """Elements from row to row of rows [n, heads, d] of dtype on like's GPU, each row contiguous; 0: not
+    such a tensor, or one row, which _rows_stride looks at."""
+    if t.dtype is dtype and t.get_device() == like.get_device():
+        shape = t.shape
+        if len(shape) == 3 and shape[2] == like.shape[3] and (heads is None or shape[1] == heads) and shape[0] > 1:
+            s0, s1, s2 = t.stride()
+            if s2 == 1 and s1 == shape[2]:
+                return s0
+    return 0
 
 
 def _dtype_code(name: str, t) -> int:
@@ -1176,7 +1210,7 @@ def _dtype_code(name: str, t) -> int:
 
 
 def omnimem_decode_quant_workspace_bytes(cache: SeqKVCacheQuant, num_q_heads: int, window: int = 0) -> int:
-    return int(lib().omnimem_decode_quant_workspace_bytes(ctypes.byref(cache.descriptor()), int(num_q_heads), int(window)))
+    return int(lib().omnimem_decode_quant_workspace_bytes(cache.packed(), int(num_q_heads), int(window)))
 
 
 def omnimem_decode_attn_quant(cache: SeqKVCacheQuant, q: torch.Tensor, scale: Optional[float] = None, *, window: int = 0,
@@ -1190,8 +1224,8 @@ def omnimem_decode_attn_quant(cache: SeqKVCacheQuant, q: torch.Tensor, scale: Op
             return omnimem_decode_attn_quant(cache, q, scale, window=window, out=out, lse=lse, want_lse=want_lse,
                                           workspace=workspace)
     code = _dtype_code("q", q)
-    desc = ctypes.byref(cache.descriptor())
-    stride = _rows_stride("q", q, None, kp, q.dtype)
+    desc = cache.packed()
+    stride = _quant_rows(q, None, kp, q.dtype) or _rows_stride("q", q, None, kp, q.dtype)
     n, hq, d = q.shape
     H = kp.shape[1]
     _need(hq >= 1 and hq % H == 0, "q must have a multiple of the cache's heads")
@@ -1230,15 +1264,16 @@ def omnimem_append_kv_quant(cache: SeqKVCacheQuant, k: torch.Tensor, v: torch.Te
         with _elsewhere(kp, stream):
             return omnimem_append_kv_quant(cache, k, v, starts)
     code = _dtype_code("k", k)
-    desc = cache.descriptor()
-    H, seqs = kp.shape[1], cache.page_table.shape[0]
-    ks, vs = _rows_stride("k", k, H, kp, k.dtype), _rows_stride("v", v, H, kp, k.dtype)
+    desc = cache.packed()
+    H, seqs, dtype = kp.shape[1], cache.page_table.shape[0], k.dtype
+    ks = _quant_rows(k, H, kp, dtype) or _rows_stride("k", k, H, kp, dtype)
+    vs = _quant_rows(v, H, kp, dtype) or _rows_stride("v", v, H, kp, dtype)
     n = k.shape[0]
     _need(v.shape[0] == n, "k and v must have as many rows")
     _check_starts(starts, n, seqs, "k and v")
     if starts is not None and starts.get_device() != dev:
         _on_gpu(kp, starts=starts)
-    st = lib().omnimem_append_kv_quant(ctypes.byref(desc), code, k.data_ptr(), ks, v.data_ptr(), vs, n, _ptr(starts),
+    st = lib().omnimem_append_kv_quant(desc, code, k.data_ptr(), ks, v.data_ptr(), vs, n, _ptr(starts),
                                     _current_raw_stream())
     if st != 0:
         _check(st, "omnimem_append_kv_quant")
@@ -1262,7 +1297,7 @@ def omnimem_read_kv_quant(cache: SeqKVCacheQuant, tokens: int, starts: Optional[
     if dev >= 0 and (stream is not None or dev != _current_device()):
         with _elsewhere(kp, stream):
             return omnimem_read_kv_quant(cache, tokens, starts, first=first, dtype=dtype, out=out)
-    desc = cache.descriptor()
+    desc = cache.packed()
     _, H, _, d = kp.shape
     seqs = cache.page_table.shape[0]
     _need(0 <= tokens <= _I32_MAX, "tokens must be 0 to 2^31 - 1")
@@ -1272,16 +1307,17 @@ def omnimem_read_kv_quant(cache: SeqKVCacheQuant, tokens: int, starts: Optional[
         _check_tensor("first", first, (seqs,), torch.int32)
     if out is None:
         _need(dtype in _DTYPES, "dtype must be bf16 or fp32")
-        k, v = (torch.empty((tokens, H, d), dtype=dtype, device=kp.device) for _ in range(2))
+        k = torch.empty((tokens, H, d), dtype=dtype, device=kp.device)
+        v = torch.empty_like(k)
     else:
         k, v = out
         _dtype_code("out", k)
         dtype = k.dtype
         _check_tensor("out[0]", k, (tokens, H, d), dtype)
         _check_tensor("out[1]", v, (tokens, H, d), dtype)
-    if out is not None or starts is not None or first is not None:
+    if not (out is None and (starts is None or starts.get_device() == dev) and (first is None or first.get_device() == dev)):
         _on_gpu(kp, starts=starts, first=first, k=k, v=v)
-    st = lib().omnimem_read_kv_quant(ctypes.byref(desc), _DTYPES[dtype], tokens, _ptr(starts), _ptr(first), k.data_ptr(),
+    st = lib().omnimem_read_kv_quant(desc, _DTYPES[dtype], tokens, _ptr(starts), _ptr(first), k.data_ptr(),
                                   v.data_ptr(), _current_raw_stream())
     if st != 0:
         _check(st, "omnimem_read_kv_quant")
@@ -1299,26 +1335,29 @@ def omnimem_copy_pages_quant(k_pages: torch.Tensor, v_pages: torch.Tensor, scale
     shape = k_pages.shape
     _need(len(shape) in (4, 5), "k_pages must be [num_pages, H, B, d] or [layers, num_pages, H, B, d]")
     layers = 1 if len(shape) == 4 else shape[0]
-    step, scale_step = (0, 0) if len(shape) == 4 else (k_pages.stride(0), scales.stride(0))
     for name, t, want, dtype in (("k_pages", k_pages, shape, _E4M3), ("v_pages", v_pages, shape, _E4M3),
-                                 ("scales", scales, shape[:-2] + (2,), torch.float32)):
+                                 ("scales", scales, shape[:-2] + (2,), _F32)):
+        if isinstance(t, torch.Tensor) and t.dtype is dtype and t.shape == want and t.is_contiguous():
+            continue   # the common case, without building any message
         _need(isinstance(t, torch.Tensor) and t.dtype is dtype, f"{name} must be {dtype}")
         _need(t.shape == want, f"{name} must have shape {tuple(want)}, not {tuple(t.shape)}")
-        if not t.is_contiguous():   # layers may lie apart
-            _need(len(shape) == 5 and layers > 0 and t[0].is_contiguous(), f"{name} must be contiguous")
+        # layers may lie apart
+        _need(len(shape) == 5 and layers > 0 and t[0].is_contiguous(), f"{name} must be contiguous")
+    step, scale_step = (k_pages.stride(0), scales.stride(0)) if layers > 1 else (0, 0)
     _need(layers <= 1 or v_pages.stride(0) == step, "v_pages must have k_pages' distance between layers")
     _need(isinstance(pairs, torch.Tensor) and pairs.dim() == 2, "pairs must be an [n, 2] tensor")
     n = pairs.shape[0]
-    _check_tensor("pairs", pairs, (n, 2), torch.int32)
+    _check_tensor("pairs", pairs, (n, 2), _I32)
     _need(n <= _I32_MAX, "pairs must hold fewer than 2^31 pairs")
     if count is not None:
-        _need(isinstance(count, torch.Tensor) and count.dtype is torch.int32 and count.numel() >= 1 and
+        _need(isinstance(count, torch.Tensor) and count.dtype is _I32 and count.numel() >= 1 and
               count.is_contiguous(), "count must be an int32 tensor")
-    _on_gpu(k_pages, "k_pages", v_pages=v_pages, scales=scales, pairs=pairs, count=count)
+    if not (dev >= 0 and v_pages.get_device() == dev and scales.get_device() == dev and pairs.get_device() == dev and
+            (count is None or count.get_device() == dev)):
+        _on_gpu(k_pages, "k_pages", v_pages=v_pages, scales=scales, pairs=pairs, count=count)
     st = lib().omnimem_copy_pages_quant(k_pages.data_ptr(), v_pages.data_ptr(), scales.data_ptr(), shape[-4], shape[-3],
-                                     shape[-2], shape[-1], layers, step if layers > 1 else 0,
-                                     4 * scale_step if layers > 1 else 0, pairs.data_ptr(), _ptr(count), n,
-                                     _current_raw_stream())
+                                        shape[-2], shape[-1], layers, step, 4 * scale_step, pairs.data_ptr(),
+                                        _ptr(count), n, _current_raw_stream())
     if st != 0:
         _check(st, "omnimem_copy_pages_quant")
 
