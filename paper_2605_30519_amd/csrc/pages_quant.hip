@@ -16,6 +16,8 @@
 namespace omnimem {
 namespace {
 
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+
 constexpr int kThreads = 256;
 constexpr uint32_t kInf = 0x7f800000u;
 constexpr int kLowest = -110, kHighest = 120;  // exponents of a scale: its inverse is a normal fp32 number
@@ -159,21 +161,33 @@ __device__ __forceinline__ uint32_t largest(const u32x4 raw) {
   return most;
 }
 
+// Stores past the caches pay for what the 256 MB memory-side cache cannot hold beside what is read:
+// 115 MB of codes 71.2 -> 68.3 us, 172 MB 110 -> 101, 86 MB 51.9 both, 14 MB 12.5 -> 12.9.
+constexpr int64_t kPastBytes = 96ll << 20;  // written
+
+template <bool PAST, typename U>
+__device__ __forceinline__ void store(U x, void* to) {
+  if constexpr (PAST) __builtin_nontemporal_store(x, static_cast<U*>(to));
+  else *static_cast<U*>(to) = x;
+}
+
 // The codes of 16 bytes of values, times inv.
+template <bool PAST>
 __device__ __forceinline__ void store_codes(uint16_t, const u32x4 raw, float inv, uint8_t* to) {
   float w[8];
 #pragma unroll
   for (int e = 0; e < 8; ++e) w[e] = __uint_as_float(e % 2 ? raw[e / 2] & 0xffff0000u : raw[e / 2] << 16) * inv;
-  *reinterpret_cast<uint2*>(to) = make_uint2(codes4(w[0], w[1], w[2], w[3]), codes4(w[4], w[5], w[6], w[7]));
+  store<PAST>(u32x2{codes4(w[0], w[1], w[2], w[3]), codes4(w[4], w[5], w[6], w[7])}, to);
 }
+template <bool PAST>
 __device__ __forceinline__ void store_codes(float, const u32x4 raw, float inv, uint8_t* to) {
   float w[4];
 #pragma unroll
   for (int e = 0; e < 4; ++e) w[e] = __uint_as_float(raw[e]) * inv;
-  *reinterpret_cast<uint32_t*>(to) = codes4(w[0], w[1], w[2], w[3]);
+  store<PAST>(codes4(w[0], w[1], w[2], w[3]), to);
 }
 
-template <typename T, int D, int B>
+template <typename T, int D, int B, bool PAST>
 __device__ __forceinline__ void append_block(const SeqGeom& g, const AppendQuantLaunch& a, const AppendUnits& units,
                                              int64_t u, int h, uint32_t (&s_most)[2][kThreads / kWave]) {
   constexpr int N = 16 / sizeof(T), LANES = D / N;               // values of 16 bytes, threads of a row
@@ -253,35 +267,41 @@ __device__ __forceinline__ void append_block(const SeqGeom& g, const AppendQuant
 #pragma unroll
     for (int p = 0; p < PASSES; ++p) {
       const int s = x.from + slot + p * ROWS;
-      if (s < x.to) store_codes(T{}, raw[kv][p], power(-e), codes + s * D + dim);
+      if (s < x.to) store_codes<PAST>(T{}, raw[kv][p], power(-e), codes + s * D + dim);
     }
   }
   if (tid == 0) *scale_at = scale;
 }
 
-template <typename T, int D, int B>
+template <typename T, int D, int B, bool PAST>
 __global__ __launch_bounds__(kThreads) void k_append_quant(const SeqGeom g, const AppendQuantLaunch a,
                                                            const AppendUnits units, int64_t work) {
   __shared__ uint32_t s_most[2][kThreads / kWave];
   for (int64_t w = blockIdx.x; w < work; w += gridDim.x) {
     const int64_t u = w / a.H;
-    append_block<T, D, B>(g, a, units, u, static_cast<int>(w - u * a.H), s_most);
+    append_block<T, D, B, PAST>(g, a, units, u, static_cast<int>(w - u * a.H), s_most);
     __syncthreads();
   }
 }
 
-template <typename T>
-hipError_t launch_append_typed(const SeqGeom& g, const AppendQuantLaunch& a, const AppendUnits& units, int64_t work,
-                               hipStream_t stream) {
-  const auto kernel = a.D == 128 ? (g.B == 128 ? k_append_quant<T, 128, 128> : k_append_quant<T, 128, 64>)
-                                 : (g.B == 128 ? k_append_quant<T, 64, 128> : k_append_quant<T, 64, 64>);
+template <typename T, bool PAST>
+hipError_t launch_append(const SeqGeom& g, const AppendQuantLaunch& a, const AppendUnits& units, int64_t work,
+                         hipStream_t stream) {
+  const auto kernel = a.D == 128 ? (g.B == 128 ? k_append_quant<T, 128, 128, PAST> : k_append_quant<T, 128, 64, PAST>)
+                                 : (g.B == 128 ? k_append_quant<T, 64, 128, PAST> : k_append_quant<T, 64, 64, PAST>);
   const int64_t wgs = work < kAppendMaxWgs ? work : kAppendMaxWgs;
   return launch_kernel(kernel, dim3(static_cast<unsigned>(wgs)), dim3(kThreads), 0, stream, g, a, units, work);
 }
 
 // ---------------------------------------------------------------- read
 // Chunks of 16 bytes of all rows are numbered through, as an append of unquantised tokens does; a
-// workgroup looks up its rows' places and fills U * 256 of them, of K and of V.
+// workgroup looks up its rows' places and fills U * 256 of them, of K and of V.  Bound by its bytes: four
+// chunks of 4,680 tokens, 12 heads, bf16 (173 MB) 31.3 us, 5.5 TB/s; with 16 codes a thread, whose
+// stores lie 32 bytes apart, 32.2, ragged fp32 rows (64 bytes apart) 15.8 instead of 12.
+constexpr int kReadUnroll = 2;  // of 1, 2 and 4: 38.1, 31.1 and 31.9 us
+// Stores past the caches: 345 MB of bf16 rows 96.2 -> 91.0 us, 460 MB of fp32 rows 118 -> 115, but 230 MB 56 -> 63.
+constexpr int64_t kReadPastBytes = 288ll << 20;  // written
+
 // Codes of 16 bytes of values, and the values, times scale.
 template <typename T>
 struct Codes;
@@ -293,7 +313,8 @@ struct Codes<uint16_t> {
     const auto v = __builtin_nontemporal_load(static_cast<const uint64_t*>(p));
     c = make_uint2(static_cast<uint32_t>(v), static_cast<uint32_t>(v >> 32));
   }
-  __device__ __forceinline__ void store(uint16_t* to, float scale) const {
+  template <bool PAST>
+  __device__ __forceinline__ void write(uint16_t* to, float scale) const {
     float x[4], y[4];
     values4(c.x, x);
     values4(c.y, y);
@@ -303,7 +324,7 @@ struct Codes<uint16_t> {
       b[e] = static_cast<__bf16>(x[e] * scale);
       b[e + 4] = static_cast<__bf16>(y[e] * scale);
     }
-    *reinterpret_cast<bf16x8*>(to) = b;
+    store<PAST>(b, to);
   }
 };
 
@@ -311,14 +332,15 @@ template <>
 struct Codes<float> {
   uint32_t c = 0;
   __device__ __forceinline__ void load(const void* p) { c = __builtin_nontemporal_load(static_cast<const uint32_t*>(p)); }
-  __device__ __forceinline__ void store(float* to, float scale) const {
+  template <bool PAST>
+  __device__ __forceinline__ void write(float* to, float scale) const {
     float x[4];
     values4(c, x);
-    *reinterpret_cast<f32x4*>(to) = f32x4{x[0] * scale, x[1] * scale, x[2] * scale, x[3] * scale};
+    store<PAST>(f32x4{x[0] * scale, x[1] * scale, x[2] * scale, x[3] * scale}, to);
   }
 };
 
-template <typename T, int U>
+template <typename T, int U, bool PAST>
 __global__ __launch_bounds__(kThreads) void k_read_quant(const SeqGeom g, const ReadQuantLaunch a) {
   constexpr int kChunks = U * kThreads;
   constexpr int N = 16 / sizeof(T);         // values of a chunk
@@ -392,8 +414,8 @@ __global__ __launch_bounds__(kThreads) void k_read_quant(const SeqGeom g, const 
 #pragma unroll
   for (int u = 0; u < U; ++u) {
     if (to[u] < 0) continue;
-    kk[u].store(static_cast<T*>(a.out_k) + to[u], scale[u].x);
-    vv[u].store(static_cast<T*>(a.out_v) + to[u], scale[u].y);
+    kk[u].template write<PAST>(static_cast<T*>(a.out_k) + to[u], scale[u].x);
+    vv[u].template write<PAST>(static_cast<T*>(a.out_v) + to[u], scale[u].y);
   }
 }
 
@@ -405,27 +427,21 @@ hipError_t launch_append_kv_quant(const SeqGeom& g, const AppendQuantLaunch& a, 
                                              : static_cast<int64_t>(a.tokens) / g.B + (units.S > 0 ? a.tokens / units.S : 0) +
                                                    static_cast<int64_t>(units.per_seq) * g.N;
   const int64_t work = blocks * a.H;
-  return a.dtype == OMNIMEM_BF16 ? launch_append_typed<uint16_t>(g, a, units, work, stream)
-                                 : launch_append_typed<float>(g, a, units, work, stream);
+  const bool past = static_cast<int64_t>(a.tokens) * a.H * a.D * 2 > kPastBytes;
+  const auto launch = a.dtype == OMNIMEM_BF16 ? (past ? launch_append<uint16_t, true> : launch_append<uint16_t, false>)
+                                              : (past ? launch_append<float, true> : launch_append<float, false>);
+  return launch(g, a, units, work, stream);
 }
-
-namespace {
-
-template <int U>
-hipError_t launch_read(const SeqGeom& g, const ReadQuantLaunch& a, hipStream_t stream) {
-  const int64_t chunks = static_cast<int64_t>(a.tokens) * a.H * (a.D / (a.dtype == OMNIMEM_BF16 ? 8 : 4));
-  const int64_t wgs = (chunks + U * kThreads - 1) / (U * kThreads);
-  if (wgs > 0x7fffffff) return hipErrorInvalidConfiguration;
-  const auto kernel = a.dtype == OMNIMEM_BF16 ? k_read_quant<uint16_t, U> : k_read_quant<float, U>;
-  return launch_kernel(kernel, dim3(static_cast<unsigned>(wgs)), dim3(kThreads), 0, stream, g, a);
-}
-
-}  // namespace
-
-constexpr int kReadUnroll = 2;  // of 1, 2 and 4: four chunks of 4,680 tokens 38.1, 31.1 and 31.9 us
 
 hipError_t launch_read_kv_quant(const SeqGeom& g, const ReadQuantLaunch& a, hipStream_t stream) {
-  return launch_read<kReadUnroll>(g, a, stream);
+  const int64_t values = static_cast<int64_t>(a.tokens) * a.H * a.D, size = a.dtype == OMNIMEM_BF16 ? 2 : 4;
+  constexpr int64_t kBytes = kReadUnroll * kThreads * 16;  // of K that a workgroup writes
+  const int64_t wgs = (values * size + kBytes - 1) / kBytes;
+  if (wgs > 0x7fffffff) return hipErrorInvalidConfiguration;
+  const bool past = 2 * values * size > kReadPastBytes;
+  const auto kernel = a.dtype == OMNIMEM_BF16 ? (past ? k_read_quant<uint16_t, kReadUnroll, true> : k_read_quant<uint16_t, kReadUnroll, false>)
+                                              : (past ? k_read_quant<float, kReadUnroll, true> : k_read_quant<float, kReadUnroll, false>);
+  return launch_kernel(kernel, dim3(static_cast<unsigned>(wgs)), dim3(kThreads), 0, stream, g, a);
 }
 
 }  // namespace omnimem

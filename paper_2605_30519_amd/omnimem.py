@@ -1244,7 +1244,7 @@ def omnimem_decode_attn_quant(cache: SeqKVCacheQuant, q: torch.Tensor, scale: Op
     if out is None:
         out = torch.empty_like(q, memory_format=torch.contiguous_format)
     if lse is None and want_lse:
-        lse = torch.empty((hq, n), dtype=torch.float32, device=q.device)
+        lse = q.new_empty((hq, n), dtype=_F32)
     st = L.omnimem_decode_attn_quant(desc, code, q.data_ptr(), stride, hq, window,
                                   d ** -0.5 if scale is None else float(scale), out.data_ptr(), _ptr(lse),
                                   _ptr(workspace), need, _current_raw_stream())
