@@ -146,17 +146,22 @@ __device__ __forceinline__ void lds_sync() {
   __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
 }
 
-template <typename L, int NT, DecodeSplit SPLIT>
+// PAIR: two column tiles, one of them every other wave's, so that a key and a value come from memory once
+// for both and a wave's registers hold one (NT = 1).
+template <typename L, int NT, DecodeSplit SPLIT, bool PAIR = false>
 __global__ __launch_bounds__(kThreads, L::wgs(NT)) void k_decode(const DecodeArgs A) {
   using T = typename L::Io;
   constexpr int D = L::kDim, RT = L::RT, VW = L::VW, QS = L::QS, UT = L::UNIT;
   constexpr bool LINE = SPLIT == DecodeSplit::kLine, BY_WAVE = SPLIT == DecodeSplit::kWave;
-  constexpr int TEAM = BY_WAVE ? 1 : kDecodeWaves;  // waves that share a segment
+  constexpr int TILES = PAIR ? 2 : 1;
+  constexpr int TEAM = BY_WAVE ? 1 : kDecodeWaves / TILES;  // waves that share a segment, of a column tile
+  static_assert(!PAIR || (NT == 1 && !BY_WAVE), "a pair of tiles is a workgroup's");
   __shared__ __align__(16) float s_o[kDecodeWaves][NT * 16][D];
   __shared__ float s_top[kDecodeWaves][NT * 16], s_sum[kDecodeWaves][NT * 16];
   const int tid = threadIdx.x, lane = tid % kWave;
   const int wave = __builtin_amdgcn_readfirstlane(tid / kWave);
   const int i = lane % 16, j = lane / 16;
+  const int place = BY_WAVE ? 0 : wave / TILES, row0 = PAIR ? wave % TILES * 16 : 0;  // in its team, of its tile's heads
   const int HH = A.a.H * A.head_tiles;
   const int N = A.g.N;
 
@@ -173,7 +178,7 @@ __global__ __launch_bounds__(kThreads, L::wgs(NT)) void k_decode(const DecodeArg
     if (left == 0) {
       const int h = g.head / A.head_tiles, tile = g.head % A.head_tiles;
       const int rows = min(A.tile_rows, A.G - tile * A.tile_rows);
-      for (int e = BY_WAVE ? lane : tid; e < rows * (D / 4); e += TEAM * kWave)
+      for (int e = BY_WAVE ? lane : tid; e < rows * (D / 4); e += (BY_WAVE ? 1 : kDecodeWaves) * kWave)
         finish<T>(A, g.seq, h * A.G + tile * A.tile_rows + e / (D / 4), e % (D / 4) * 4, f32x4{}, 0.f, 0.f);
       return;
     }
@@ -252,7 +257,7 @@ __global__ __launch_bounds__(kThreads, L::wgs(NT)) void k_decode(const DecodeArg
   // most one in front of g; its units are looked up 64 at a time, lane l the l-th one's page and,
   // in one register, its first token row and its rows in use.
   Segment f = g;
-  int next = f.unit + (BY_WAVE ? 0 : wave);
+  int next = f.unit + place;
   uint64_t mask = 0;
   int l_page = 0;
   uint32_t l_rows = 0;
@@ -320,7 +325,7 @@ __global__ __launch_bounds__(kThreads, L::wgs(NT)) void k_decode(const DecodeArg
 #pragma unroll
     for (int n = 0; n < NT; ++n)  // rows past the last query head repeat it and are not written
       L::load_q(static_cast<const T*>(A.a.q) + f.seq * A.a.q_stride +
-                    static_cast<int64_t>(hq0 + min(n * 16 + i, rows - 1)) * D,
+                    static_cast<int64_t>(hq0 + min(row0 + n * 16 + i, rows - 1)) * D,
                 j, q[n]);
   };
   // the stream's next segment; false behind the share's last one
@@ -337,7 +342,7 @@ __global__ __launch_bounds__(kThreads, L::wgs(NT)) void k_decode(const DecodeArg
     }
     f.stop = min(f.sp.units, left);
     left -= f.stop;
-    next = wave;
+    next = place;
     load_q();
     return true;
   };
@@ -353,7 +358,7 @@ __global__ __launch_bounds__(kThreads, L::wgs(NT)) void k_decode(const DecodeArg
   // the answer, and with more than 16 query heads to a key head a second loop costs registers that
   // there are not.
   bool shared = false;
-  if constexpr (LINE && NT == 1 && L::kTwoPolicies) {
+  if constexpr (LINE && NT == 1 && L::kTwoPolicies && !PAIR) {
     const int u = f.unit + lane;
     bool same = false;
     if (long_share && u < f.stop && N > 1) {
@@ -470,7 +475,7 @@ __global__ __launch_bounds__(kThreads, L::wgs(NT)) void k_decode(const DecodeArg
 #pragma unroll
       for (int n = 0; n < NT; ++n) {
         const float total = sum_over_groups(sum[n]);
-        if (n * 16 + i < rows) {
+        if (row0 + n * 16 + i < rows) {
           if (j == 0) {
             s_top[wave][n * 16 + i] = top[n];
             s_sum[wave][n * 16 + i] = total;
@@ -492,16 +497,17 @@ __global__ __launch_bounds__(kThreads, L::wgs(NT)) void k_decode(const DecodeArg
       float* slot = A.part + (static_cast<int64_t>(blockIdx.x) * 2 + (first ? 0 : 1)) * A.slot_floats;
       for (int e = tid; e < rows * (D / 4); e += kThreads) {
         const int r = e / (D / 4), d = e % (D / 4) * 4;
-        float m = s_top[0][r];
+        const int w0 = PAIR ? r / 16 : 0, at = PAIR ? r % 16 : r;  // the first of its tile's waves, its row there
+        float m = s_top[w0][at];
 #pragma unroll
-        for (int w = 1; w < kDecodeWaves; ++w) m = fmaxf(m, s_top[w][r]);
+        for (int w = TILES; w < kDecodeWaves; w += TILES) m = fmaxf(m, s_top[w0 + w][at]);
         float total = 0.f;
         f32x4 x{};
 #pragma unroll
-        for (int w = 0; w < kDecodeWaves; ++w) {
-          const float c = exp2f(s_top[w][r] - m);
-          total += c * s_sum[w][r];
-          const f32x4 y = *reinterpret_cast<const f32x4*>(&s_o[w][r][d]);
+        for (int w = 0; w < kDecodeWaves; w += TILES) {
+          const float c = exp2f(s_top[w0 + w][at] - m);
+          total += c * s_sum[w0 + w][at];
+          const f32x4 y = *reinterpret_cast<const f32x4*>(&s_o[w0 + w][at][d]);
 #pragma unroll
           for (int v = 0; v < 4; ++v) x[v] += c * y[v];
         }
@@ -520,18 +526,18 @@ __global__ __launch_bounds__(kThreads, L::wgs(NT)) void k_decode(const DecodeArg
       have = hi > sub;
     }
   };
-  if constexpr (LINE && NT == 1 && L::kTwoPolicies) {
+  if constexpr (LINE && NT == 1 && L::kTwoPolicies && !PAIR) {
     if (shared) return stream(std::integral_constant<int, 0>{});
   }
-  stream(std::integral_constant<int, kNontemporal>{});
+  stream(std::integral_constant<int, PAIR ? 0 : kNontemporal>{});
 }
 
 // The shares of an item that several workgroups took, joined in the order of the line by the
 // workgroups of the item's second share.  x: that share, y: ROWS query heads of the tile.  The
 // threads of a row take its dims by four, in sets that take the shares in turn and meet in LDS.
-template <typename T, int D, int ROWS>
-__global__ __launch_bounds__(256) void k_decode_join(const DecodeArgs A) {
-  constexpr int LANES = D / 4, SETS = 256 / LANES / ROWS;
+template <typename T, int D, int ROWS, int THREADS = 256, int UNROLL = 4>
+__global__ __launch_bounds__(THREADS) void k_decode_join(const DecodeArgs A) {
+  constexpr int LANES = D / 4, SETS = THREADS / LANES / ROWS;
   __shared__ float s_top[ROWS][SETS], s_sum[ROWS][SETS];
   __shared__ __align__(16) float s_o[ROWS][SETS][D];
   const DecodeStart st = A.starts[blockIdx.x];
@@ -548,7 +554,7 @@ __global__ __launch_bounds__(256) void k_decode_join(const DecodeArgs A) {
   float m = kLowest, total = 0.f;
   f32x4 o{};
   if (real) {
-#pragma unroll 4
+#pragma unroll UNROLL
     for (int p = set; p < parts; p += SETS) {
       const float* s = A.part + (static_cast<int64_t>(w0 + p) * 2 + (p == 0 ? tail : 0)) * A.slot_floats;
       const float mp = s[A.rows * D + r], lp = s[A.rows * (D + 1) + r];
@@ -584,25 +590,22 @@ __global__ __launch_bounds__(256) void k_decode_join(const DecodeArgs A) {
   if (real) finish<T>(A, st.seq, hq, d, o, m, total);
 }
 
-template <typename L, int NT>
-hipError_t launch_rows(const DecodeArgs& A, const DecodePlan& p, hipStream_t stream) {
-  const auto kernel = p.split == DecodeSplit::kLine   ? k_decode<L, NT, DecodeSplit::kLine>
-                      : p.split == DecodeSplit::kItem ? k_decode<L, NT, DecodeSplit::kItem>
-                                                      : k_decode<L, NT, DecodeSplit::kWave>;
+// join: k_decode_join of join_threads threads for p.join_rows rows.
+template <typename Kernel, typename Join>
+hipError_t launch_with_join(Kernel kernel, Join join, int join_threads, const DecodeArgs& A, const DecodePlan& p,
+                            hipStream_t stream) {
   LaunchStatus st;
   st(kernel, dim3(p.wgs), dim3(kThreads), 0, stream, A);
-  if (p.split == DecodeSplit::kLine && p.wgs > 1) {
-    using T = typename L::Io;
-    constexpr int D = L::kDim;
-    const auto join = p.join_rows == 1 ? k_decode_join<T, D, 1> : p.join_rows == 2 ? k_decode_join<T, D, 2> : k_decode_join<T, D, 4>;
-    st(join, dim3(p.wgs, (p.rows + p.join_rows - 1) / p.join_rows), dim3(256), 0, stream, A);
-  }
+  if (p.split == DecodeSplit::kLine && p.wgs > 1)
+    st(join, dim3(p.wgs, (p.rows + p.join_rows - 1) / p.join_rows), dim3(join_threads), 0, stream, A);
   return st.err;
 }
 
-template <typename L>
-hipError_t launch_tile(const DecodeArgs& A, const DecodePlan& p, hipStream_t stream) {
-  return p.tile_rows == kDecodeHeadRows ? launch_rows<L, 1>(A, p, stream) : launch_rows<L, 2>(A, p, stream);
+template <typename L, int NT>
+auto kernel_of(const DecodePlan& p) {
+  return p.split == DecodeSplit::kLine   ? k_decode<L, NT, DecodeSplit::kLine>
+         : p.split == DecodeSplit::kItem ? k_decode<L, NT, DecodeSplit::kItem>
+                                         : k_decode<L, NT, DecodeSplit::kWave>;
 }
 
 DecodeArgs decode_args(const SeqGeom& g, const DecodePlan& p, const DecodeLaunch& a, void* workspace) {

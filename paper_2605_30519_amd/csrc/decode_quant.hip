@@ -100,23 +100,25 @@ struct TileQuant {
   }
   template <int NT>
   __device__ __forceinline__ void scores(const u32x4 (&q)[NT][QS], f32x4 (&s)[NT][RT]) const {
+    // the row tiles' chains side by side: a product waits for the one before it in its own
 #pragma unroll
-    for (int t = 0; t < RT; ++t) {
+    for (int x = 0; x < STEPS; ++x) {
+      u32x4 a[RT];
 #pragma unroll
-      for (int n = 0; n < NT; ++n) s[n][t] = f32x4{};
-#pragma unroll
-      for (int x = 0; x < STEPS; ++x) {
+      for (int t = 0; t < RT; ++t) {
         const u32x4 c = k[t / 2][t % 2][x / 2];
         const int w = x % 2 * 2;
-        const u32x4 a = {widen2<false>(c[w]), widen2<true>(c[w]), widen2<false>(c[w + 1]), widen2<true>(c[w + 1])};
-#pragma unroll
-        for (int p = 0; p < PIECES; ++p)
-#pragma unroll
-          for (int n = 0; n < NT; ++n)
-            s[n][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a),
-                                                              __builtin_bit_cast(bf16x8, q[n][p * STEPS + x]), s[n][t],
-                                                              0, 0, 0);
+        a[t] = u32x4{widen2<false>(c[w]), widen2<true>(c[w]), widen2<false>(c[w + 1]), widen2<true>(c[w + 1])};
       }
+#pragma unroll
+      for (int p = 0; p < PIECES; ++p)
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+          for (int t = 0; t < RT; ++t)
+            s[n][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+                __builtin_bit_cast(bf16x8, a[t]), __builtin_bit_cast(bf16x8, q[n][p * STEPS + x]),
+                x == 0 && p == 0 ? f32x4{} : s[n][t], 0, 0, 0);
     }
   }
   // O^T row tiles m: dims VW * (row of the tile) + m.  Four keys' words of four dims are turned into
@@ -156,21 +158,40 @@ struct TileQuant {
           d[f][2] = __builtin_amdgcn_perm(gh2, ac2, 0x05040100u);
           d[f][3] = __builtin_amdgcn_perm(gh2, ac2, 0x07060302u);
         }
+        u32x4 a[4];
 #pragma unroll
-        for (int m = 0; m < 4; ++m) {
-          const u32x4 a = {widen2<false>(d[0][m]), widen2<true>(d[0][m]), widen2<false>(d[1][m]), widen2<true>(d[1][m])};
+        for (int m = 0; m < 4; ++m)
+          a[m] = u32x4{widen2<false>(d[0][m]), widen2<true>(d[0][m]), widen2<false>(d[1][m]), widen2<true>(d[1][m])};
 #pragma unroll
-          for (int z = 0; z < P_PIECES; ++z)
+        for (int z = 0; z < P_PIECES; ++z)
 #pragma unroll
-            for (int n = 0; n < NT; ++n)
+          for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int m = 0; m < 4; ++m)
               o[n][4 * w + m] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
-                  __builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, piece[n][z]), o[n][4 * w + m], 0, 0, 0);
-        }
+                  __builtin_bit_cast(bf16x8, a[m]), __builtin_bit_cast(bf16x8, piece[n][z]), o[n][4 * w + m], 0, 0, 0);
       }
     }
   }
   __device__ __forceinline__ static int dim(int row, int x) { return VW * row + 4 * x; }
 };
+
+template <typename L>
+hipError_t launch_tile(const DecodeArgs& A, const DecodePlan& p, hipStream_t stream) {
+  using T = typename L::Io;
+  constexpr int D = L::kDim;
+  const auto kernel = p.tile_rows == kDecodeHeadRows   ? kernel_of<L, 1>(p)
+                      : !p.pair                       ? k_decode<L, 2, DecodeSplit::kLine>
+                      : p.split == DecodeSplit::kLine ? k_decode<L, 1, DecodeSplit::kLine, true>
+                                                      : k_decode<L, 1, DecodeSplit::kItem, true>;
+  // The shares of a long item are many, and a set of threads takes its part of them one behind the other:
+  // 512 threads a row where an item has 64 shares and more (one of 100,000 tokens, 8 query heads, 15.8 ->
+  // 8.5 us), else two rows of 128 with eight shares' loads in flight (18 ragged items of 24 query heads, four rows
+  // and four shares 13.6, this 8.0; 32 items of 32 heads 11.4 / 5.9; 384 items 4.7 both).
+  const auto join = p.join_rows == 1 ? (p.long_items ? k_decode_join<T, D, 1, 512, 8> : k_decode_join<T, D, 1>)
+                                     : k_decode_join<T, D, 2, 256, 8>;
+  return launch_with_join(kernel, join, p.long_items ? 512 : 256, A, p, stream);
+}
 
 }  // namespace
 

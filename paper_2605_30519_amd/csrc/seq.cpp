@@ -85,24 +85,34 @@ constexpr int64_t kDecodeWgs = 256, kDecodeManyWgs = 512;
 // 60 tokens, 24 query heads, 17.2 -> 11.8 us (4 query heads 10.6 -> 8.2, one fp32 17.4 -> 13.8); 512
 // items 9.0 / 8.9 (5.9 / 6.8, 9.5 / 10.8), 64 items of 120 tokens 4.9 -> 9.0.
 constexpr int64_t kItemUnitsMost = 20, kWaveUnitsMost = 8, kWaveItems = 1024;
+// Two column tiles over 8-bit pages, from this many bytes of the table's capacity on both a wave's, which is
+// then held up less by memory than by a key's and a value's widening, once for both; below, each every
+// other wave's.  24 query heads a key head, bf16, 4 sequences of 60 to 90 thousand tokens (620 MB) 116 us
+// against 143, 7 of 3 to 21 thousand (131 MB) 40.8 / 44.8; 40 of 1 to 3 thousand (145 MB) 49.0 / 52.0, fp32 65.6 /
+// 55.5; 49 of up to 1,752 (19 MB) 23.2 / 20.4, fp32 28.1 / 22.3.
+constexpr double kBothBytes = 256 << 20;
 constexpr int64_t kItemOverhead = 64;  // of an item's length on the line, no less than the kernel adds
 
 // What a plan goes by, of a kind of pages: tokens of a unit; units of the longest item that is a
 // workgroup's, and of one that a window bounds where there is an item for each CU; workgroups of a line
-// where there are no more items than CUs and where there are, and of one with two column tiles (0: no
-// other rule).
+// where there are no more items than CUs and where there are; whether these are 8-bit pages, whose
+// kernels have one column tile a wave and joins of their own.
 struct DecodeTuning {
-  int64_t unit, item_units, window_units, wgs, many_wgs, wide_wgs;
+  int64_t unit, item_units, window_units, wgs, many_wgs;
+  bool eight_bit;
 };
 
 omnimem_status_t plan_decode(int32_t num_heads, int32_t head_dim, const DecodeTuning& t, const SeqGeom& g,
                              int32_t num_q_heads, int32_t window, DecodePlan& p) {
   if (num_q_heads < 1 || num_q_heads % num_heads != 0) return OMNIMEM_EINVAL;
   p.G = num_q_heads / num_heads;
-  p.tile_rows = p.G <= kDecodeHeadRows ? kDecodeHeadRows : 2 * kDecodeHeadRows;
-  p.head_tiles = (p.G + p.tile_rows - 1) / p.tile_rows;
-  p.rows = p.G < p.tile_rows ? p.G : p.tile_rows;
-  const int64_t items = static_cast<int64_t>(g.N) * num_heads * p.head_tiles;
+  const auto tile = [&p](int rows) {
+    p.tile_rows = rows;
+    p.head_tiles = (p.G + rows - 1) / rows;
+    p.rows = p.G < rows ? p.G : rows;
+  };
+  tile(p.G <= kDecodeHeadRows ? kDecodeHeadRows : 2 * kDecodeHeadRows);
+  int64_t items = static_cast<int64_t>(g.N) * num_heads * p.head_tiles;
   // Blocks and units of an item, at most.  A window reaches into window / S + 2 chunks, and
   // tokens of one run lie in no more than a B-th of them, and two, blocks.
   int64_t blocks = g.M;
@@ -119,13 +129,23 @@ omnimem_status_t plan_decode(int32_t num_heads, int32_t head_dim, const DecodeTu
   p.split = units <= kWaveUnitsMost && items >= kWaveItems ? DecodeSplit::kWave
             : units <= item_units                             ? DecodeSplit::kItem
                                                               : DecodeSplit::kLine;
+  if (p.split == DecodeSplit::kWave && t.eight_bit) {
+    tile(kDecodeHeadRows);
+    items = static_cast<int64_t>(g.N) * num_heads * p.head_tiles;
+  }
   const int64_t most = items * (units + kItemOverhead);
-  const int64_t wgs = p.tile_rows > kDecodeHeadRows && t.wide_wgs > 0 ? t.wide_wgs : items > kDecodeWgs ? t.many_wgs : t.wgs;
+  p.pair = t.eight_bit && p.tile_rows > kDecodeHeadRows;
+  const double bytes = 2. * g.N * g.M * num_heads * g.B * head_dim;
+  const bool both = p.pair && p.split == DecodeSplit::kLine && bytes >= kBothBytes;
+  if (both) p.pair = false;
+  const int64_t wgs = both && head_dim == 128 ? kDecodeWgs : items > kDecodeWgs ? t.many_wgs : t.wgs;
   if (most > wgs * 0x7fffffff) return OMNIMEM_EINVAL;  // a workgroup's share of the line in 31 bits
   p.wgs = static_cast<int>(p.split == DecodeSplit::kLine   ? (most < wgs ? most : wgs)
                            : p.split == DecodeSplit::kItem ? items
                                                            : (items + kDecodeWaves - 1) / kDecodeWaves);
-  p.join_rows = items * 16 <= p.wgs ? 1 : p.rows >= 4 ? 4 : p.rows >= 2 ? 2 : 1;
+  p.long_items = t.eight_bit && items * 64 <= p.wgs;
+  if (!t.eight_bit) p.join_rows = items * 16 <= p.wgs ? 1 : p.rows >= 4 ? 4 : p.rows >= 2 ? 2 : 1;
+  else p.join_rows = p.long_items || p.rows == 1 ? 1 : 2;
   p.slot_floats = static_cast<size_t>(p.rows) * (head_dim + 2);
   p.slot_floats = (p.slot_floats + 3) / 4 * 4;
   p.off_part = 0;
@@ -138,7 +158,7 @@ omnimem_status_t plan_decode(int32_t num_heads, int32_t head_dim, const DecodeTu
 omnimem_status_t plan_decode(const omnimem_seq_cache_t* sc, const SeqGeom& g, int32_t num_q_heads, int32_t window,
                              DecodePlan& p) {
   const DecodeTuning t{sc->dtype == OMNIMEM_BF16 && sc->head_dim == 64 ? 64 : 32, kItemUnitsMost, kItemUnitsMost, kDecodeWgs,
-                       kDecodeManyWgs, 0};
+                       kDecodeManyWgs, false};
   return plan_decode(sc->num_heads, sc->head_dim, t, g, num_q_heads, window, p);
 }
 
@@ -151,8 +171,8 @@ omnimem_status_t plan_decode(const omnimem_seq_cache_t* sc, const SeqGeom& g, in
 // 64 28.3 -> 17.1, where 32 items lose (15.4 -> 20.1, 14.0 -> 15.0).
 omnimem_status_t plan_decode(const omnimem_seq_cache_quant_t* sc, const SeqGeom& g, int32_t num_q_heads, int32_t window,
                              DecodePlan& p) {
-  const DecodeTuning t = sc->head_dim == 64 ? DecodeTuning{64, 28, 48, kDecodeManyWgs, kDecodeManyWgs, kDecodeManyWgs}
-                                            : DecodeTuning{64, 20, 48, kDecodeWgs, kDecodeManyWgs, kDecodeWgs};
+  const DecodeTuning t = sc->head_dim == 64 ? DecodeTuning{64, 28, 48, kDecodeManyWgs, kDecodeManyWgs, true}
+                                            : DecodeTuning{64, 20, 48, kDecodeWgs, kDecodeManyWgs, true};
   return plan_decode(sc->num_heads, sc->head_dim, t, g, num_q_heads, window, p);
 }
 

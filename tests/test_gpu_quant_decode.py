@@ -90,9 +90,11 @@ def test_lengths_around_every_border(dev, dtype, d, B, H, G):
 @pytest.mark.parametrize("dtype,d", [(BF16, 128), (F32, 128), (BF16, 64), (F32, 64)])
 @pytest.mark.parametrize("G", [2, 15, 16, 17, 32, 33, 40])
 def test_query_heads_per_key_head(dev, dtype, d, G):
-    say(f"decode groups {dtype} d={d} G={G}")
-    cache, g = build(dev, 2, d, 64, 64, [200, 0, 70, 3000], 2)
-    check(cache, queries(dev, dtype, 4, 2 * G, d, g))
+    # items of a workgroup, shares of a line, and of a line over a table of half a gigabyte and more
+    for lens, more in (([200, 0, 70, 900], 1), ([200, 0, 70, 3000], 1), ([200, 0, 70, 3000], 9000)):
+        say(f"decode groups {dtype} d={d} G={G} lens={lens} M={more}")
+        cache, g = build(dev, 2, d, 64, 64, lens, 2, extra_blocks=more)
+        check(cache, queries(dev, dtype, 4, 2 * G, d, g))
 
 
 @pytest.mark.parametrize("dtype,d,B,S", [(BF16, 128, 64, 100), (F32, 64, 64, 130), (BF16, 64, 128, 200), (F32, 128, 128, 70),
@@ -256,3 +258,21 @@ def test_rows_and_splits_of_every_kind(dev):
         say(f"decode splits {dtype} d={d} H={H} n={len(lens)}")
         cache, g = build(dev, H, d, 64, 64, lens, 10)
         check(cache, queries(dev, dtype, len(lens), H, d, g))
+
+
+@pytest.mark.parametrize("dtype,d", [(BF16, 128), (F32, 128), (BF16, 64), (F32, 64)])
+def test_many_query_heads_over_every_split(dev, dtype, d):
+    """More than 16 query heads a key head: a wave's items, of which each has 16 of them, and long ones of few
+    heads, whose shares larger workgroups join."""
+    for H, G, lens in ((8, 20, [1 + i % 64 for i in range(140)]), (1, 33, [9000]), (1, 3, [12000]), (2, 24, [1, 8000, 0, 3])):
+        say(f"decode many heads {dtype} d={d} H={H} G={G} n={len(lens)}")
+        cache, g = build(dev, H, d, 64, 64, lens, 11)
+        check(cache, queries(dev, dtype, len(lens), H * G, d, g))
+
+
+@pytest.mark.parametrize("dtype,G", [(BF16, 24), (F32, 24), (BF16, 5)])
+def test_windows_of_many_items(dev, dtype, G):
+    """Windows that bound an item for each CU: longer items than else are a workgroup's."""
+    lens = [3000 + 7 * i for i in range(40)] + [0, 5]
+    cache, g = build(dev, 7, 64, 64, 64, lens, 12)
+    check(cache, queries(dev, dtype, len(lens), 7 * G, 64, g), window=2700)
