@@ -588,16 +588,16 @@ typedef struct {
  * For each block, head and pool the new tokens of the block need the scale 2^e with the smallest
  * e >= -110 that has |x| <= 448 * 2^e for all their finite values x.  Where they begin the
  * block, that is its scale, whatever the page held.  Where they follow others, the scale is the larger
- * of it and the block's own (rounded up to a power of two in [2^-110, 2^120]; a block's scale never falls while it
- * has tokens), and if that is not the block's own, the earlier tokens' codes c become
+ * of it and the block's own (rounded up to a power of two in [2^-110, 2^120], NaN to 2^-110; a block's scale never
+ * falls while it has tokens), and if that is not the block's own, the earlier tokens' codes c become
  * rne(c * own / new).  A new value becomes rne(x / scale); rne: to the nearest e4m3 number, ties to even.
  * Infinities and NaN become NaN.  Between powers of two only values below 2^-6 * scale are rounded
  * a second time, so that it hardly matters in how many calls a block is filled.
  * Two tokens in one slot, or a page that two blocks of the call are on: the page's contents are undefined.
  */
-omnimem_status_t omnimem_append_kv_quant(const omnimem_seq_cache_quant_t* sc, int32_t dtype, const void* k, int64_t k_stride,
-                                      const void* v, int64_t v_stride, int32_t tokens, const int32_t* starts,
-                                      void* stream);
+omnimem_status_t omnimem_append_kv_quant(const omnimem_seq_cache_quant_t* sc, int32_t dtype, const void* k,
+                                         int64_t k_stride, const void* v, int64_t v_stride, int32_t tokens,
+                                         const int32_t* starts, void* stream);
 
 /* Bytes of device workspace omnimem_decode_attn_quant needs; as omnimem_decode_workspace_bytes. */
 size_t omnimem_decode_quant_workspace_bytes(const omnimem_seq_cache_quant_t* sc, int32_t num_q_heads, int32_t window);
@@ -607,11 +607,13 @@ size_t omnimem_decode_quant_workspace_bytes(const omnimem_seq_cache_quant_t* sc,
  * be powers of two.  Slots that hold none of the attended tokens, and scales of pages that hold none,
  * do not matter, NaN included.
  * Codes take part exactly.  bf16: P enters PV in two bf16 pieces, 2^-15 off; f32: Q and P in three, which
- * hold all of their bits; sums are fp32.
+ * hold all of their bits; sums are fp32.  V's scale is multiplied into P in front of that, so that what scales
+ * below 2^-90 leave of P's last pieces may be below bf16's range and lost.
  */
-omnimem_status_t omnimem_decode_attn_quant(const omnimem_seq_cache_quant_t* sc, int32_t dtype, const void* q, int64_t q_stride,
-                                        int32_t num_q_heads, int32_t window, float scale, void* out, float* lse,
-                                        void* workspace, size_t workspace_bytes, void* stream);
+omnimem_status_t omnimem_decode_attn_quant(const omnimem_seq_cache_quant_t* sc, int32_t dtype, const void* q,
+                                           int64_t q_stride, int32_t num_q_heads, int32_t window, float scale,
+                                           void* out, float* lse, void* workspace, size_t workspace_bytes,
+                                           void* stream);
 
 /*
  * Reads tokens back: rows starts[i] to starts[i+1] of out_k and out_v are the tokens of
@@ -623,18 +625,19 @@ omnimem_status_t omnimem_decode_attn_quant(const omnimem_seq_cache_quant_t* sc, 
  * starts: [N + 1] int32, ascending, values outside [0, tokens] clamped; NULL: one token
  *         for each sequence (tokens = N).  first: [N] int32.
  */
-omnimem_status_t omnimem_read_kv_quant(const omnimem_seq_cache_quant_t* sc, int32_t dtype, int32_t tokens, const int32_t* starts,
-                                    const int32_t* first, void* out_k, void* out_v, void* stream);
+omnimem_status_t omnimem_read_kv_quant(const omnimem_seq_cache_quant_t* sc, int32_t dtype, int32_t tokens,
+                                       const int32_t* starts, const int32_t* first, void* out_k, void* out_v,
+                                       void* stream);
 
 /*
  * omnimem_copy_pages of 8-bit pages, K and V with their scales, in one call.
  * k_pages, v_pages: layer l's pool at + l*layer_stride bytes, num_pages pages [num_heads][block_size][head_dim];
  * scales: layer l's at + l*scale_stride bytes (a multiple of 8).
  */
-omnimem_status_t omnimem_copy_pages_quant(void* k_pages, void* v_pages, float* scales, int64_t num_pages, int32_t num_heads,
-                                       int32_t block_size, int32_t head_dim, int32_t layers, int64_t layer_stride,
-                                       int64_t scale_stride, const int32_t* pairs, const int32_t* count,
-                                       int32_t max_pairs, void* stream);
+omnimem_status_t omnimem_copy_pages_quant(void* k_pages, void* v_pages, float* scales, int64_t num_pages,
+                                          int32_t num_heads, int32_t block_size, int32_t head_dim, int32_t layers,
+                                          int64_t layer_stride, int64_t scale_stride, const int32_t* pairs,
+                                          const int32_t* count, int32_t max_pairs, void* stream);
 
 /*
  * Binds the calling thread to the NUMA node of GPU `device`'s PCI function (App. B

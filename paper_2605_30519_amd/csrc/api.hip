@@ -248,14 +248,14 @@ OMNIMEM_API omnimem_status_t omnimem_seq_compact(const omnimem_seq_table_t* st, 
 }
 
 OMNIMEM_API size_t omnimem_decode_quant_workspace_bytes(const omnimem_seq_cache_quant_t* sc, int32_t num_q_heads,
-                                                     int32_t window) {
+                                                        int32_t window) {
   return omnimem::decode_quant_workspace_bytes(sc, num_q_heads, window);
 }
 
 OMNIMEM_API omnimem_status_t omnimem_decode_attn_quant(const omnimem_seq_cache_quant_t* sc, int32_t dtype, const void* q,
-                                                    int64_t q_stride, int32_t num_q_heads, int32_t window, float scale,
-                                                    void* out, float* lse, void* workspace, size_t workspace_bytes,
-                                                    void* stream) {
+                                                       int64_t q_stride, int32_t num_q_heads, int32_t window, float scale,
+                                                       void* out, float* lse, void* workspace, size_t workspace_bytes,
+                                                       void* stream) {
   omnimem::SeqGeom g;
   omnimem::DecodePlan p;
   omnimem::DecodeLaunch a;
@@ -266,8 +266,8 @@ OMNIMEM_API omnimem_status_t omnimem_decode_attn_quant(const omnimem_seq_cache_q
 }
 
 OMNIMEM_API omnimem_status_t omnimem_append_kv_quant(const omnimem_seq_cache_quant_t* sc, int32_t dtype, const void* k,
-                                                  int64_t k_stride, const void* v, int64_t v_stride, int32_t tokens,
-                                                  const int32_t* starts, void* stream) {
+                                                     int64_t k_stride, const void* v, int64_t v_stride, int32_t tokens,
+                                                     const int32_t* starts, void* stream) {
   omnimem::SeqGeom g;
   omnimem::AppendQuantLaunch a;
   const omnimem_status_t st = omnimem::check_append_kv_quant(sc, dtype, k, k_stride, v, v_stride, tokens, starts, g, a);
@@ -276,8 +276,8 @@ OMNIMEM_API omnimem_status_t omnimem_append_kv_quant(const omnimem_seq_cache_qua
 }
 
 OMNIMEM_API omnimem_status_t omnimem_read_kv_quant(const omnimem_seq_cache_quant_t* sc, int32_t dtype, int32_t tokens,
-                                                const int32_t* starts, const int32_t* first, void* out_k, void* out_v,
-                                                void* stream) {
+                                                   const int32_t* starts, const int32_t* first, void* out_k, void* out_v,
+                                                   void* stream) {
   omnimem::SeqGeom g;
   omnimem::ReadQuantLaunch a;
   const omnimem_status_t st = omnimem::check_read_kv_quant(sc, dtype, tokens, starts, first, out_k, out_v, g, a);
@@ -286,10 +286,10 @@ OMNIMEM_API omnimem_status_t omnimem_read_kv_quant(const omnimem_seq_cache_quant
 }
 
 OMNIMEM_API omnimem_status_t omnimem_copy_pages_quant(void* k_pages, void* v_pages, float* scales, int64_t num_pages,
-                                                   int32_t num_heads, int32_t block_size, int32_t head_dim,
-                                                   int32_t layers, int64_t layer_stride, int64_t scale_stride,
-                                                   const int32_t* pairs, const int32_t* count, int32_t max_pairs,
-                                                   void* stream) {
+                                                      int32_t num_heads, int32_t block_size, int32_t head_dim,
+                                                      int32_t layers, int64_t layer_stride, int64_t scale_stride,
+                                                      const int32_t* pairs, const int32_t* count, int32_t max_pairs,
+                                                      void* stream) {
   omnimem::CopyLaunch a;
   const omnimem_status_t st = omnimem::check_copy_pages_quant(k_pages, v_pages, scales, num_pages, num_heads, block_size,
                                                            head_dim, layers, layer_stride, scale_stride, pairs, count,

@@ -112,7 +112,10 @@ __global__ __launch_bounds__(kAppendThreads) void k_append_kv(const SeqGeom g, c
 // ---------------------------------------------------------------- copies of pages
 // A grid that is resident at once walks pieces of 16 KB of (pair, layer, pool); the number of
 // pairs is read on the device.  Bound by its bytes: 300 pages of 12 heads x 64 x 128 bf16 in six
-// layers (1.4 GB read and written) 279 us, 5.1 TB/s, as a large tensor copy (5.0); 16 pages 4.2 us.
+// layers (1.4 GB read and written) 279 us, 5.1 TB/s, as a large tensor copy (5.0), of 8-bit codes with their
+// scales 139 us; 16 pages 4.5 us.  The next piece's loads are out before the present one is stored: without,
+// 8-bit pages took 150 us, and a grid of every piece, which does not need that, 6 us more for a call
+// without a copy.
 constexpr int kCopyThreads = 256, kCopyUnroll = 4, kCopyPiece = kCopyThreads * kCopyUnroll;
 constexpr int kCopyMaxWgs = 1536;
 

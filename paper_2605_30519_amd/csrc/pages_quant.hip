@@ -30,7 +30,9 @@ __device__ __forceinline__ int exponent_for(uint32_t most) {
 }
 
 // A scale as memory has it, brought into [2^-110, 2^120].
-__device__ __forceinline__ float scale_in_range(float s) { return s >= power(kLowest) ? fminf(s, power(kHighest)) : power(kLowest); }
+__device__ __forceinline__ float scale_in_range(float s) {
+  return s >= power(kLowest) ? fminf(s, power(kHighest)) : power(kLowest);
+}
 
 __device__ __forceinline__ int exponent_of(float s) {  // the smallest e with s <= 2^e
   const uint32_t u = __float_as_uint(s);
@@ -51,13 +53,18 @@ __device__ __forceinline__ void values4(uint32_t codes, float (&x)[4]) {
   x[3] = high[1];
 }
 
-__device__ __forceinline__ int row_of_start(const int32_t* starts, int tokens, int s) { return min(max(starts[s], 0), tokens); }
+__device__ __forceinline__ int row_of_start(const int32_t* starts, int tokens, int s) {
+  return min(max(starts[s], 0), tokens);
+}
 
 // ---------------------------------------------------------------- append
 // A workgroup takes the new tokens of one block and one head, of K and V: it holds them in
 // registers, 16 bytes of a row a thread and pass, finds their largest, rounds them by the scale, and, where the
 // block's earlier tokens have a smaller scale, those again.  Bound by its bytes where there are many
-// blocks, else by the chain of loads that leads to them: the sequence, its rows and page, the rows.
+// blocks: eight chunks of 4,680 tokens, 12 heads, bf16 (345 MB) 68.5 us, 5.0 TB/s (K and V in workgroups of
+// their own and 16 values a thread, whose loads lie 32 bytes apart: 84.5; fp32 rows, 64 bytes apart, 39.8 instead
+// of 24.1).  Else by the chain of loads that leads to them, the sequence, its rows and page, the rows: 64
+// single tokens 5.6 us.
 //
 // Blocks are numbered through: n rows touch at most n div B + 2 blocks of a contiguous sequence, and
 // n div S + n div B + 3 of one in chunks, so with `starts` ascending the numbers from
@@ -362,7 +369,7 @@ __global__ __launch_bounds__(kThreads) void k_read_quant(const SeqGeom g, const 
     for (int s = tid; s < g.N; s += kThreads) {
       const int start = row_of_start(a.starts, a.tokens, s), stop = row_of_start(a.starts, a.tokens, s + 1);
       const int len = g.lens[s];
-      const int64_t token0 = a.first != nullptr ? static_cast<int64_t>(a.first[s]) - start : static_cast<int64_t>(len) - stop;
+      const int64_t token0 = a.first != nullptr ? int64_t{a.first[s]} - start : int64_t{len} - stop;
       const int to = min(stop, t1 + 1);
       for (int t = max(start, t0); t < to; ++t) {
         const int64_t token = token0 + t;
@@ -439,8 +446,9 @@ hipError_t launch_read_kv_quant(const SeqGeom& g, const ReadQuantLaunch& a, hipS
   const int64_t wgs = (values * size + kBytes - 1) / kBytes;
   if (wgs > 0x7fffffff) return hipErrorInvalidConfiguration;
   const bool past = 2 * values * size > kReadPastBytes;
-  const auto kernel = a.dtype == OMNIMEM_BF16 ? (past ? k_read_quant<uint16_t, kReadUnroll, true> : k_read_quant<uint16_t, kReadUnroll, false>)
-                                              : (past ? k_read_quant<float, kReadUnroll, true> : k_read_quant<float, kReadUnroll, false>);
+  constexpr int U = kReadUnroll;
+  const auto kernel = a.dtype == OMNIMEM_BF16 ? (past ? k_read_quant<uint16_t, U, true> : k_read_quant<uint16_t, U, false>)
+                                              : (past ? k_read_quant<float, U, true> : k_read_quant<float, U, false>);
   return launch_kernel(kernel, dim3(static_cast<unsigned>(wgs)), dim3(kThreads), 0, stream, g, a);
 }
 

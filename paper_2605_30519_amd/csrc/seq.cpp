@@ -252,9 +252,9 @@ omnimem_status_t check_decode_attn(const omnimem_seq_cache_t* sc, const void* q,
 }
 
 omnimem_status_t check_decode_attn_quant(const omnimem_seq_cache_quant_t* sc, int32_t dtype, const void* q, int64_t q_stride,
-                                      int32_t num_q_heads, int32_t window, float scale, void* out, float* lse,
-                                      const void* workspace, size_t workspace_bytes, SeqGeom& g, DecodePlan& p,
-                                      DecodeLaunch& a) {
+                                         int32_t num_q_heads, int32_t window, float scale, void* out, float* lse,
+                                         const void* workspace, size_t workspace_bytes, SeqGeom& g, DecodePlan& p,
+                                         DecodeLaunch& a) {
   if (!known_dtype(dtype)) return OMNIMEM_EUNSUPPORTED;
   omnimem_status_t st = resolve_quant_cache(sc, g, false);
   if (st == OMNIMEM_OK) st = plan_decode(sc, g, num_q_heads, window, p);
@@ -313,8 +313,8 @@ omnimem_status_t check_copy_pages(void* k_pages, void* v_pages, int64_t num_page
 }
 
 omnimem_status_t check_append_kv_quant(const omnimem_seq_cache_quant_t* sc, int32_t dtype, const void* k, int64_t k_stride,
-                                    const void* v, int64_t v_stride, int32_t tokens, const int32_t* starts, SeqGeom& g,
-                                    AppendQuantLaunch& a) {
+                                       const void* v, int64_t v_stride, int32_t tokens, const int32_t* starts, SeqGeom& g,
+                                       AppendQuantLaunch& a) {
   if (!known_dtype(dtype)) return OMNIMEM_EUNSUPPORTED;
   const omnimem_status_t st = resolve_quant_cache(sc, g, false);
   if (st != OMNIMEM_OK) return st;
@@ -328,11 +328,12 @@ omnimem_status_t check_append_kv_quant(const omnimem_seq_cache_quant_t* sc, int3
 }
 
 omnimem_status_t check_read_kv_quant(const omnimem_seq_cache_quant_t* sc, int32_t dtype, int32_t tokens, const int32_t* starts,
-                                  const int32_t* first, void* out_k, void* out_v, SeqGeom& g, ReadQuantLaunch& a) {
+                                     const int32_t* first, void* out_k, void* out_v, SeqGeom& g, ReadQuantLaunch& a) {
   if (!known_dtype(dtype)) return OMNIMEM_EUNSUPPORTED;
   const omnimem_status_t st = resolve_quant_cache(sc, g, false);
   if (st != OMNIMEM_OK) return st;
-  if (tokens < 0 || (starts == nullptr && tokens != g.N) || !aligned(starts, 4) || !aligned(first, 4)) return OMNIMEM_EINVAL;
+  if (tokens < 0 || (starts == nullptr && tokens != g.N) || !aligned(starts, 4) || !aligned(first, 4))
+    return OMNIMEM_EINVAL;
   if (tokens > 0 && (out_k == nullptr || out_v == nullptr)) return OMNIMEM_EINVAL;
   if (!aligned(out_k, 16) || !aligned(out_v, 16)) return OMNIMEM_EINVAL;
   a = ReadQuantLaunch{dtype,       sc->num_heads, sc->head_dim, tokens, starts, first,
@@ -341,13 +342,14 @@ omnimem_status_t check_read_kv_quant(const omnimem_seq_cache_quant_t* sc, int32_
 }
 
 omnimem_status_t check_copy_pages_quant(void* k_pages, void* v_pages, float* scales, int64_t num_pages, int32_t num_heads,
-                                     int32_t block_size, int32_t head_dim, int32_t layers, int64_t layer_stride,
-                                     int64_t scale_stride, const int32_t* pairs, const int32_t* count, int32_t max_pairs,
-                                     CopyLaunch& a) {
+                                        int32_t block_size, int32_t head_dim, int32_t layers, int64_t layer_stride,
+                                        int64_t scale_stride, const int32_t* pairs, const int32_t* count, int32_t max_pairs,
+                                        CopyLaunch& a) {
   if ((block_size != 64 && block_size != 128) || (head_dim != 64 && head_dim != 128)) return OMNIMEM_EUNSUPPORTED;
   if (num_heads < 1 || num_heads > (1 << 20)) return OMNIMEM_EINVAL;
-  const omnimem_status_t st = check_copy_pages(k_pages, v_pages, num_pages, static_cast<int64_t>(num_heads) * block_size * head_dim,
-                                               layers, layer_stride, pairs, count, max_pairs, a);
+  const int64_t page_bytes = static_cast<int64_t>(num_heads) * block_size * head_dim;
+  const omnimem_status_t st =
+      check_copy_pages(k_pages, v_pages, num_pages, page_bytes, layers, layer_stride, pairs, count, max_pairs, a);
   if (st != OMNIMEM_OK) return st;
   if (scale_stride < 0 || scale_stride % 8 != 0 || !aligned(scales, 8)) return OMNIMEM_EINVAL;
   if (layers > 1 && (scale_stride < num_pages * num_heads * 8 || scale_stride > (int64_t{1} << 44))) return OMNIMEM_EINVAL;

@@ -165,18 +165,18 @@ omnimem_status_t check_copy_pages(void* k_pages, void* v_pages, int64_t num_page
                                   int64_t layer_stride, const int32_t* pairs, const int32_t* count, int32_t max_pairs,
                                   CopyLaunch& a);
 omnimem_status_t check_decode_attn_quant(const omnimem_seq_cache_quant_t* sc, int32_t dtype, const void* q, int64_t q_stride,
-                                      int32_t num_q_heads, int32_t window, float scale, void* out, float* lse,
-                                      const void* workspace, size_t workspace_bytes, SeqGeom& g, DecodePlan& p,
-                                      DecodeLaunch& a);
+                                         int32_t num_q_heads, int32_t window, float scale, void* out, float* lse,
+                                         const void* workspace, size_t workspace_bytes, SeqGeom& g, DecodePlan& p,
+                                         DecodeLaunch& a);
 omnimem_status_t check_append_kv_quant(const omnimem_seq_cache_quant_t* sc, int32_t dtype, const void* k, int64_t k_stride,
-                                    const void* v, int64_t v_stride, int32_t tokens, const int32_t* starts, SeqGeom& g,
-                                    AppendQuantLaunch& a);
+                                       const void* v, int64_t v_stride, int32_t tokens, const int32_t* starts, SeqGeom& g,
+                                       AppendQuantLaunch& a);
 omnimem_status_t check_read_kv_quant(const omnimem_seq_cache_quant_t* sc, int32_t dtype, int32_t tokens, const int32_t* starts,
-                                  const int32_t* first, void* out_k, void* out_v, SeqGeom& g, ReadQuantLaunch& a);
+                                     const int32_t* first, void* out_k, void* out_v, SeqGeom& g, ReadQuantLaunch& a);
 omnimem_status_t check_copy_pages_quant(void* k_pages, void* v_pages, float* scales, int64_t num_pages, int32_t num_heads,
-                                     int32_t block_size, int32_t head_dim, int32_t layers, int64_t layer_stride,
-                                     int64_t scale_stride, const int32_t* pairs, const int32_t* count, int32_t max_pairs,
-                                     CopyLaunch& a);
+                                        int32_t block_size, int32_t head_dim, int32_t layers, int64_t layer_stride,
+                                        int64_t scale_stride, const int32_t* pairs, const int32_t* count, int32_t max_pairs,
+                                        CopyLaunch& a);
 omnimem_status_t check_seq_update(const omnimem_seq_table_t* st, int32_t num_new, const int32_t* parent,
                                   const int32_t* keep, const int32_t* grow, int32_t* out_table, int32_t* out_lens,
                                   int32_t* copies, int32_t* info, const void* workspace, size_t workspace_bytes,

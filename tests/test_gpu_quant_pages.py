@@ -243,6 +243,23 @@ def test_tokens_read_back(dev, dtype, d, B, H, S):
         assert torch.equal(x.double().cpu().nan_to_num(-1), w.float().to(dtype).double().nan_to_num(-1))
 
 
+def test_one_token_read_from_inside(dev):
+    """One token a sequence at a place of its own, without starts; places that a sequence does not have are 0."""
+    g = torch.Generator().manual_seed(17)
+    lens = [5, 64, 130, 0, -2, 300, 64]
+    first = [4, 0, 129, 0, 0, 300, -1]
+    table, P = tables(lens, 64, 64, g)
+    k, v, scales = pools(P, 2, 64, 64, g)
+    cache = SeqKVCacheQuant(k.to(dev).view(F8), v.to(dev).view(F8), scales.to(dev), i32(table, dev), i32(lens, dev))
+    want = [torch.zeros((7, 2, 64), dtype=torch.float64) for _ in range(2)]
+    quant_oracle.read(k, v, scales, table, lens, 7, None, first, 64, *want)
+    for dtype in (F32, BF16):
+        got = omnimem_read_kv_quant(cache, 7, first=i32(first, dev), dtype=dtype)
+        for x, w in zip(got, want):
+            assert torch.equal(x.double().cpu().nan_to_num(-1), w.float().to(dtype).double().nan_to_num(-1))
+            assert (x[3:] == 0).all()
+
+
 def test_what_is_appended_is_read(dev):
     """Values that e4m3 holds come back as they were, in bf16 and fp32."""
     g = torch.Generator().manual_seed(13)
