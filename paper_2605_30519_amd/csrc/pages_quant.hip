@@ -303,8 +303,9 @@ hipError_t launch_append(const SeqGeom& g, const AppendQuantLaunch& a, const App
 // ---------------------------------------------------------------- read
 // Chunks of 16 bytes of all rows are numbered through, as an append of unquantised tokens does; a
 // workgroup looks up its rows' places and fills U * 256 of them, of K and of V.  Bound by its bytes: four
-// chunks of 4,680 tokens, 12 heads, bf16 (173 MB) 31.3 us, 5.5 TB/s; with 16 codes a thread, whose
-// stores lie 32 bytes apart, 32.2, ragged fp32 rows (64 bytes apart) 15.8 instead of 12.
+// chunks of 4,680 tokens, 12 heads, bf16 (173 MB) 31.3 us, 5.5 TB/s, into memory that is written again and
+// again, 37 into fresh memory; with 16 codes a thread, whose stores lie 32 bytes apart, 32.2, ragged fp32 rows
+// (64 bytes apart, 35 MB) 15.8 instead of 11.1.
 constexpr int kReadUnroll = 2;  // of 1, 2 and 4: 38.1, 31.1 and 31.9 us
 // Stores past the caches: 345 MB of bf16 rows 96.2 -> 91.0 us, 460 MB of fp32 rows 118 -> 115, but 230 MB 56 -> 63.
 constexpr int64_t kReadPastBytes = 288ll << 20;  // written
@@ -354,10 +355,14 @@ __global__ __launch_bounds__(kThreads) void k_read_quant(const SeqGeom g, const 
   constexpr int kRows = kChunks / (64 / N) + 2;  // rows of at least one head of 64
   __shared__ int s_seq[kRows], s_page[kRows], s_slot[kRows];
   const int tid = threadIdx.x;
-  const int head_chunks = a.D / N;
-  const int64_t row_chunks = static_cast<int64_t>(a.H) * head_chunks, total = a.tokens * row_chunks;
+  const int head_shift = 6 + (a.D >> 7) - (N == 8 ? 3 : 2);  // log2 of a head's chunks
+  const uint32_t row_chunks = static_cast<uint32_t>(a.H) << head_shift;
+  const int64_t total = static_cast<int64_t>(a.tokens) * row_chunks;
   const int64_t c0 = static_cast<int64_t>(blockIdx.x) * kChunks;
-  const int t0 = static_cast<int>(c0 / row_chunks), t1 = static_cast<int>((min(c0 + kChunks, total) - 1) / row_chunks);
+  const int t0 = static_cast<int>(c0 / row_chunks);
+  const uint32_t in0 = static_cast<uint32_t>(c0 - static_cast<int64_t>(t0) * row_chunks);  // the first chunk in its row
+  const uint32_t mine = static_cast<uint32_t>(min(total - c0, int64_t{kChunks}));
+  const int t1 = t0 + static_cast<int>((in0 + mine - 1) / row_chunks);
   for (int r = tid; r <= t1 - t0; r += kThreads) {
     const int seq = a.starts == nullptr ? t0 + r : -1;
     s_seq[r] = seq;
@@ -402,18 +407,18 @@ __global__ __launch_bounds__(kThreads) void k_read_quant(const SeqGeom g, const 
   int64_t to[U];
 #pragma unroll
   for (int u = 0; u < U; ++u) {
-    const int64_t c = c0 + u * kThreads + tid;
+    const uint32_t c = u * kThreads + tid;
     to[u] = -1;
     scale[u] = make_float2(0.f, 0.f);
-    if (c >= total) continue;
-    const int row = static_cast<int>(c / row_chunks), in = static_cast<int>(c - row * row_chunks);
-    const int page = s_page[row - t0];
+    if (c >= mine) continue;
+    const uint32_t row = (in0 + c) / row_chunks, in = in0 + c - row * row_chunks;
+    const int page = s_page[row];
     if (page == -2) continue;
-    to[u] = c * N;
+    to[u] = (c0 + c) * N;
     if (page < 0) continue;
-    const int h = in / head_chunks;
+    const uint32_t h = in >> head_shift;
     const int64_t head = static_cast<int64_t>(page) * a.H + h;
-    const int64_t at = (head * g.B + s_slot[row - t0]) * a.D + (in - h * head_chunks) * N;
+    const int64_t at = (head * g.B + s_slot[row]) * a.D + (in - (h << head_shift)) * N;
     kk[u].load(static_cast<const uint8_t*>(a.k_pages) + at);
     vv[u].load(static_cast<const uint8_t*>(a.v_pages) + at);
     scale[u] = *reinterpret_cast<const float2*>(a.scales + head * 2);
