@@ -196,7 +196,7 @@ __device__ __forceinline__ void store_codes(float, const u32x4 raw, float inv, u
 
 template <typename T, int D, int B, bool PAST>
 __device__ __forceinline__ void append_block(const SeqGeom& g, const AppendQuantLaunch& a, const AppendUnits& units,
-                                             int64_t u, int h, uint32_t (&s_most)[2][kThreads / kWave]) {
+                                             int64_t u, int h, uint32_t (&s_most)[2][kThreads / kWave], float2& s_own) {
   constexpr int N = 16 / sizeof(T), LANES = D / N;               // values of 16 bytes, threads of a row
   constexpr int ROWS = kThreads / LANES, PASSES = B / ROWS;
   static_assert(PASSES * ROWS == B, "a block in whole passes");
@@ -221,7 +221,7 @@ __device__ __forceinline__ void append_block(const SeqGeom& g, const AppendQuant
   if (page < 0 || page >= g.num_pages) return;
   const int64_t head = static_cast<int64_t>(page) * a.H + h;
   float2* scale_at = reinterpret_cast<float2*>(a.scales) + head;
-  const float2 own = x.from > 0 ? *scale_at : make_float2(0.f, 0.f);
+  if (tid == 0 && x.from > 0) s_own = *scale_at;  // by the thread that will write it
 
   uint32_t most[2] = {0, 0};
   auto find_most = [&](auto finite) {
@@ -233,7 +233,7 @@ __device__ __forceinline__ void append_block(const SeqGeom& g, const AppendQuant
       m = wave_max(m);
       if (lane == 0) s_most[kv][tid / kWave] = m;
     }
-    __syncthreads();  // every thread has read the block's own scale, too
+    __syncthreads();
 #pragma unroll
     for (int kv = 0; kv < 2; ++kv) {
       most[kv] = s_most[kv][0];
@@ -253,7 +253,7 @@ __device__ __forceinline__ void append_block(const SeqGeom& g, const AppendQuant
     uint8_t* codes = static_cast<uint8_t*>(kv ? a.v_pages : a.k_pages) + head * B * D;
     int e = exponent_for(most[kv]);
     if (x.from > 0) {
-      const float was = scale_in_range(kv ? own.y : own.x);
+      const float was = scale_in_range(kv ? s_own.y : s_own.x);
       e = max(e, exponent_of(was));
       const float ratio = was * power(-e);
       if (ratio != 1.f) {  // the earlier tokens, by the new scale
@@ -284,9 +284,10 @@ template <typename T, int D, int B, bool PAST>
 __global__ __launch_bounds__(kThreads) void k_append_quant(const SeqGeom g, const AppendQuantLaunch a,
                                                            const AppendUnits units, int64_t work) {
   __shared__ uint32_t s_most[2][kThreads / kWave];
+  __shared__ float2 s_own;
   for (int64_t w = blockIdx.x; w < work; w += gridDim.x) {
     const int64_t u = w / a.H;
-    append_block<T, D, B, PAST>(g, a, units, u, static_cast<int>(w - u * a.H), s_most);
+    append_block<T, D, B, PAST>(g, a, units, u, static_cast<int>(w - u * a.H), s_most, s_own);
     __syncthreads();
   }
 }
