@@ -1141,7 +1141,8 @@ class SeqKVCacheQuant:
     owned by the caller): a value is its code times the scale of its page and head.
 
     k_pages, v_pages: [num_pages, H, B, d] float8_e4m3fn; scales: [num_pages, H, 2] fp32, of K and of
-    V; page_table, seq_lens, chunk_tokens: as SeqKVCache's."""
+    V; page_table, seq_lens, chunk_tokens: as SeqKVCache's.  Neither pages nor scales need initial
+    values; pages are copied by omnimem_copy_pages_quant, which takes their scales along."""
     k_pages: torch.Tensor
     v_pages: torch.Tensor
     scales: torch.Tensor

@@ -79,6 +79,40 @@ def check(cache, q, window=0, scale=None, **kw):
 EDGES = [0, 1, 2, 15, 16, 17, 31, 32, 33, 63, 64, 65, 127, 128, 129, 255, 256, 257, 300, 0]
 
 
+@pytest.mark.parametrize("dtype,d,H,G", [(BF16, 128, 4, 2), (F32, 128, 4, 1), (BF16, 64, 8, 1), (F32, 64, 8, 3), (BF16, 128, 4, 20)])
+def test_sequences_that_share_their_pages(dev, dtype, d, H, G):
+    """Long sequences over one prompt's pages, which are then kept in the caches, and over copies of them:
+    the same bits, and those of fp64 for the first of them."""
+    N, n = 4, 1150                                                # 64 units and more for each of 256 workgroups, of 512
+    n = n if d == 128 else 2 * n
+    g = torch.Generator(device=dev).manual_seed(40)
+    k, v = (torch.randint(0, 100, (n, H, 64, d), generator=g, device=dev, dtype=torch.uint8) for _ in range(2))
+    k |= torch.randint(0, 2, k.shape, generator=g, device=dev, dtype=torch.uint8) << 7
+    scales = torch.exp2(torch.randint(-8, -5, (n, H, 2), generator=g, device=dev).float())
+    order = torch.randperm(n, generator=g, device=dev).int()
+    lens = torch.tensor([64 * n - 3 * i for i in range(N)], dtype=torch.int32, device=dev)
+    q = torch.randn((N, H * G, d), generator=g, device=dev).to(dtype)
+    one = SeqKVCacheQuant(k.view(F8), v.view(F8), scales, order.repeat(N, 1), lens)
+    rows = torch.stack([order + i * n for i in range(N)])
+    own = SeqKVCacheQuant(k.repeat(N, 1, 1, 1).view(F8), v.repeat(N, 1, 1, 1).view(F8), scales.repeat(N, 1, 1), rows, lens)
+    a, b = omnimem_decode_attn_quant(one, q), omnimem_decode_attn_quant(own, q)
+    assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
+    picked = [0, H * G - 1]                                       # two heads against fp64
+    for h in picked:
+        pages = order.long()
+        kd = quant_oracle.values(k[pages, h // G].cpu()) * scales[pages, h // G, :1, None].cpu().double()
+        vd = quant_oracle.values(v[pages, h // G].cpu()) * scales[pages, h // G, 1:, None].cpu().double()
+        kd, vd = kd.reshape(-1, d), vd.reshape(-1, d)
+        s = kd @ q[0, h].double().cpu() * d ** -0.5
+        p = torch.softmax(s, 0)[:, None]
+        e = 2.0 ** -24 * (3 * d + 9) * float((kd.abs() @ q[0, h].double().cpu().abs()).max()) * d ** -0.5 + 2.0 ** -22
+        e += (kd.shape[0] + 80) * 2.0 ** -24
+        bound = (p * vd.abs()).sum(0) * (2 * e + 3 * kd.shape[0] * 2.0 ** -24 + (2.0 ** -15 if dtype is BF16 else 0))
+        O = (p * vd).sum(0)
+        bound += O.abs() * (2.0 ** -8 if dtype is BF16 else 2.0 ** -24)
+        assert ((a[0][0, h].double().cpu() - O).abs() <= bound).all()
+
+
 @pytest.mark.parametrize("dtype", [BF16, F32])
 @pytest.mark.parametrize("d,B,H,G", [(128, 64, 3, 1), (64, 64, 2, 5), (128, 128, 2, 5), (64, 128, 3, 1)])
 def test_lengths_around_every_border(dev, dtype, d, B, H, G):
