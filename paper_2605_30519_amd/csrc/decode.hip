@@ -216,7 +216,7 @@ hipError_t launch_tile(const DecodeArgs& A, const DecodePlan& p, hipStream_t str
   const auto join = p.join_rows == 1   ? k_decode_join<T, D, 1>
                     : p.join_rows == 2 ? k_decode_join<T, D, 2>
                                        : k_decode_join<T, D, 4>;
-  return launch_with_join(p.tile_rows == kDecodeHeadRows ? kernel_of<L, 1>(p) : kernel_of<L, 2>(p), join, 256, A, p, stream);
+  return launch_with_join(p.tile_rows == kDecodeHeadRows ? kernel_of<L, 1>(p) : kernel_of<L, 2>(p), kThreads, join, 256, A, p, stream);
 }
 
 }  // namespace

@@ -148,16 +148,16 @@ __device__ __forceinline__ void lds_sync() {
 
 // PAIR: two column tiles, one of them every other wave's, so that a key and a value come from memory once
 // for both and a wave's registers hold one (NT = 1).
-template <typename L, int NT, DecodeSplit SPLIT, bool PAIR = false>
-__global__ __launch_bounds__(kThreads, L::wgs(NT)) void k_decode(const DecodeArgs A) {
+template <typename L, int NT, DecodeSplit SPLIT, bool PAIR = false, int WAVES = kDecodeWaves>
+__global__ __launch_bounds__(WAVES * kWave, L::wgs(NT)) void k_decode(const DecodeArgs A) {
   using T = typename L::Io;
   constexpr int D = L::kDim, RT = L::RT, VW = L::VW, QS = L::QS, UT = L::UNIT;
   constexpr bool LINE = SPLIT == DecodeSplit::kLine, BY_WAVE = SPLIT == DecodeSplit::kWave;
   constexpr int TILES = PAIR ? 2 : 1;
-  constexpr int TEAM = BY_WAVE ? 1 : kDecodeWaves / TILES;  // waves that share a segment, of a column tile
+  constexpr int TEAM = BY_WAVE ? 1 : WAVES / TILES;  // waves that share a segment, of a column tile
   static_assert(!PAIR || (NT == 1 && !BY_WAVE), "a pair of tiles is a workgroup's");
-  __shared__ __align__(16) float s_o[kDecodeWaves][NT * 16][D];
-  __shared__ float s_top[kDecodeWaves][NT * 16], s_sum[kDecodeWaves][NT * 16];
+  __shared__ __align__(16) float s_o[WAVES][NT * 16][D];
+  __shared__ float s_top[WAVES][NT * 16], s_sum[WAVES][NT * 16];
   const int tid = threadIdx.x, lane = tid % kWave;
   const int wave = __builtin_amdgcn_readfirstlane(tid / kWave);
   const int i = lane % 16, j = lane / 16;
@@ -169,7 +169,7 @@ __global__ __launch_bounds__(kThreads, L::wgs(NT)) void k_decode(const DecodeArg
   int left = 0;  // units of the share from g.unit on
   bool long_share = false;
   if constexpr (!LINE) {
-    const int item = BY_WAVE ? blockIdx.x * kDecodeWaves + wave : blockIdx.x;
+    const int item = BY_WAVE ? blockIdx.x * WAVES + wave : blockIdx.x;
     g.seq = item / HH;
     g.head = item - g.seq * HH;
     if (g.seq >= N) return;  // behind the last item, where every wave has its own
@@ -178,7 +178,7 @@ __global__ __launch_bounds__(kThreads, L::wgs(NT)) void k_decode(const DecodeArg
     if (left == 0) {
       const int h = g.head / A.head_tiles, tile = g.head % A.head_tiles;
       const int rows = min(A.tile_rows, A.G - tile * A.tile_rows);
-      for (int e = BY_WAVE ? lane : tid; e < rows * (D / 4); e += (BY_WAVE ? 1 : kDecodeWaves) * kWave)
+      for (int e = BY_WAVE ? lane : tid; e < rows * (D / 4); e += (BY_WAVE ? 1 : WAVES) * kWave)
         finish<T>(A, g.seq, h * A.G + tile * A.tile_rows + e / (D / 4), e % (D / 4) * 4, f32x4{}, 0.f, 0.f);
       return;
     }
@@ -211,7 +211,7 @@ __global__ __launch_bounds__(kThreads, L::wgs(NT)) void k_decode(const DecodeArg
       for (int64_t s0 = static_cast<int64_t>(blockIdx.x) * each; s0 < end; s0 += kWave) {
         uint64_t none = __ballot(s0 + lane < end && span_of<UT>(A, A.g.lens[min(s0 + lane, int64_t{N} - 1)]).units == 0);
         for (; none != 0; none &= none - 1)
-          for (int e = tid; e < A.a.Hq * (D / 4); e += kThreads)
+          for (int e = tid; e < A.a.Hq * (D / 4); e += (WAVES * kWave))
             finish<T>(A, static_cast<int>(s0) + __builtin_ctzll(none), e / (D / 4), e % (D / 4) * 4, f32x4{}, 0.f, 0.f);
       }
     }
@@ -495,16 +495,16 @@ __global__ __launch_bounds__(kThreads, L::wgs(NT)) void k_decode(const DecodeArg
       lds_sync();
       const bool complete = !LINE || (g.unit == 0 && g.stop == g.sp.units);
       float* slot = A.part + (static_cast<int64_t>(blockIdx.x) * 2 + (first ? 0 : 1)) * A.slot_floats;
-      for (int e = tid; e < rows * (D / 4); e += kThreads) {
+      for (int e = tid; e < rows * (D / 4); e += (WAVES * kWave)) {
         const int r = e / (D / 4), d = e % (D / 4) * 4;
         const int w0 = PAIR ? r / 16 : 0, at = PAIR ? r % 16 : r;  // the first of its tile's waves, its row there
         float m = s_top[w0][at];
 #pragma unroll
-        for (int w = TILES; w < kDecodeWaves; w += TILES) m = fmaxf(m, s_top[w0 + w][at]);
+        for (int w = TILES; w < WAVES; w += TILES) m = fmaxf(m, s_top[w0 + w][at]);
         float total = 0.f;
         f32x4 x{};
 #pragma unroll
-        for (int w = 0; w < kDecodeWaves; w += TILES) {
+        for (int w = 0; w < WAVES; w += TILES) {
           const float c = exp2f(s_top[w0 + w][at] - m);
           total += c * s_sum[w0 + w][at];
           const f32x4 y = *reinterpret_cast<const f32x4*>(&s_o[w0 + w][at][d]);
@@ -590,12 +590,12 @@ __global__ __launch_bounds__(THREADS) void k_decode_join(const DecodeArgs A) {
   if (real) finish<T>(A, st.seq, hq, d, o, m, total);
 }
 
-// join: k_decode_join of join_threads threads for p.join_rows rows.
+// kernel: k_decode of `threads`; join: k_decode_join of join_threads for p.join_rows rows.
 template <typename Kernel, typename Join>
-hipError_t launch_with_join(Kernel kernel, Join join, int join_threads, const DecodeArgs& A, const DecodePlan& p,
-                            hipStream_t stream) {
+hipError_t launch_with_join(Kernel kernel, int threads, Join join, int join_threads, const DecodeArgs& A,
+                            const DecodePlan& p, hipStream_t stream) {
   LaunchStatus st;
-  st(kernel, dim3(p.wgs), dim3(kThreads), 0, stream, A);
+  st(kernel, dim3(p.wgs), dim3(threads), 0, stream, A);
   if (p.split == DecodeSplit::kLine && p.wgs > 1)
     st(join, dim3(p.wgs, (p.rows + p.join_rows - 1) / p.join_rows), dim3(join_threads), 0, stream, A);
   return st.err;

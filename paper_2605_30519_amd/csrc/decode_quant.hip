@@ -188,17 +188,24 @@ template <typename L>
 hipError_t launch_tile(const DecodeArgs& A, const DecodePlan& p, hipStream_t stream) {
   using T = typename L::Io;
   constexpr int D = L::kDim;
-  const auto kernel = p.tile_rows == kDecodeHeadRows   ? kernel_of<L, 1>(p)
-                      : !p.pair                       ? k_decode<L, 2, DecodeSplit::kLine>
-                      : p.split == DecodeSplit::kLine ? k_decode<L, 1, DecodeSplit::kLine, true>
-                                                      : k_decode<L, 1, DecodeSplit::kItem, true>;
+  auto kernel = p.tile_rows == kDecodeHeadRows   ? kernel_of<L, 1>(p)
+                : !p.pair                       ? k_decode<L, 2, DecodeSplit::kLine>
+                : p.split == DecodeSplit::kLine ? k_decode<L, 1, DecodeSplit::kLine, true>
+                                                : k_decode<L, 1, DecodeSplit::kItem, true>;
+  int threads = kThreads;
+  if constexpr (D == 64) {
+    if (p.eight_waves) {
+      kernel = k_decode<L, 1, DecodeSplit::kItem, false, 8>;
+      threads = 8 * kWave;
+    }
+  }
   // The shares of a long item are many, and a set of threads takes its part of them one behind the other:
   // 512 threads a row where an item has 64 shares and more (one of 100,000 tokens, 8 query heads, 15.8 ->
   // 8.5 us), else two rows of 128 with eight shares' loads in flight (18 ragged items of 24 query heads, four rows
   // and four shares 13.6, this 8.0; 32 items of 32 heads 11.4 / 5.9; 384 items 4.7 both).
   const auto join = p.join_rows == 1 ? (p.long_items ? k_decode_join<T, D, 1, 512, 8> : k_decode_join<T, D, 1>)
                                      : k_decode_join<T, D, 2, 256, 8>;
-  return launch_with_join(kernel, join, p.long_items ? 512 : 256, A, p, stream);
+  return launch_with_join(kernel, threads, join, p.long_items ? 512 : 256, A, p, stream);
 }
 
 }  // namespace

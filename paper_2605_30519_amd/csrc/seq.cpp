@@ -125,7 +125,8 @@ omnimem_status_t plan_decode(int32_t num_heads, int32_t head_dim, const DecodeTu
   if (items > 0x7fffffff / 256 || static_cast<int64_t>(g.N) * (static_cast<int64_t>(g.M) * (g.B / unit) + kItemOverhead) > 0x7fffffff ||
       (items > 0 && units > (int64_t{1} << 40) / items))
     return OMNIMEM_EINVAL;
-  const int64_t item_units = window > 0 && items >= kDecodeWgs ? t.window_units : t.item_units;
+  const bool pair = t.eight_bit && p.tile_rows > kDecodeHeadRows;
+  const int64_t item_units = window > 0 && items >= kDecodeWgs ? t.window_units : pair ? t.item_units * 2 / 3 : t.item_units;
   p.split = units <= kWaveUnitsMost && items >= kWaveItems ? DecodeSplit::kWave
             : units <= item_units                             ? DecodeSplit::kItem
                                                               : DecodeSplit::kLine;
@@ -134,7 +135,9 @@ omnimem_status_t plan_decode(int32_t num_heads, int32_t head_dim, const DecodeTu
     items = static_cast<int64_t>(g.N) * num_heads * p.head_tiles;
   }
   const int64_t most = items * (units + kItemOverhead);
-  p.pair = t.eight_bit && p.tile_rows > kDecodeHeadRows;
+  p.eight_waves = t.eight_bit && head_dim == 64 && p.tile_rows == kDecodeHeadRows && p.split == DecodeSplit::kItem &&
+                  items <= kDecodeWgs / 2 && units > 4;
+  p.pair = pair && p.tile_rows > kDecodeHeadRows;
   const double bytes = 2. * g.N * g.M * num_heads * g.B * head_dim;
   const bool both = p.pair && p.split == DecodeSplit::kLine && bytes >= kBothBytes;
   if (both) p.pair = false;
@@ -167,6 +170,10 @@ omnimem_status_t plan_decode(const omnimem_seq_cache_t* sc, const SeqGeom& g, in
 // 58.3 us; an item of one goes twice as far: a window of 1,560 tokens, 256 items 23.6 -> 12.7, 4 items
 // 10.2 -> 11.6, but a launch less.  Two column tiles of 128-dim heads need a CU's registers for one workgroup:
 // 16 sequences of 3,000 to 9,000 tokens, 17 query heads on each of 4, bf16, 36.0 -> 32.9 (two spill).
+// Column tiles in pairs of waves leave an item two waves for each, so it is a workgroup's for two thirds of
+// that length: 24 query heads, 17 units 16.7 against 14.6, 10 units 11.4 / 14.5.  A CU takes in an item of
+// 128-dim heads no faster with eight waves, one of 64 does: a window of 1,560 tokens, 32 items, fp32 11.8 ->
+// 10.3, bf16 10.1 -> 8.7, but 240 items 12.8 -> 13.0, 3 units 5.0 -> 5.3.
 // Windows make items of one length: 256 of 2,400 tokens, bf16 heads of 128, 36.2 -> 28.1, fp32 heads of
 // 64 28.3 -> 17.1, where 32 items lose (15.4 -> 20.1, 14.0 -> 15.0).
 omnimem_status_t plan_decode(const omnimem_seq_cache_quant_t* sc, const SeqGeom& g, int32_t num_q_heads, int32_t window,

@@ -37,6 +37,7 @@ struct DecodePlan {
   DecodeSplit split;
   int join_rows;     // query heads of a workgroup that joins shares
   bool long_items;   // 8-bit pages: items of many shares, joined by larger workgroups a head
+  bool eight_waves;  // 8-bit pages: a workgroup's item is eight waves', not four
   bool pair;         // 8-bit pages: of two column tiles, each is every other wave's
   size_t off_part, off_starts, total;
   size_t slot_floats;  // one workgroup's partial result of one item: O [rows][d], max [rows], sum [rows]

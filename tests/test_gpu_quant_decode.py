@@ -125,7 +125,7 @@ def test_lengths_around_every_border(dev, dtype, d, B, H, G):
 @pytest.mark.parametrize("G", [2, 15, 16, 17, 32, 33, 40])
 def test_query_heads_per_key_head(dev, dtype, d, G):
     # items of a workgroup, shares of a line, and of a line over a table of half a gigabyte and more
-    for lens, more in (([200, 0, 70, 900], 1), ([200, 0, 70, 3000], 1), ([200, 0, 70, 3000], 9000)):
+    for lens, more in (([200, 0, 70, 600], 1), ([200, 0, 70, 1000], 1), ([200, 0, 70, 3000], 1), ([200, 0, 70, 3000], 9000)):
         say(f"decode groups {dtype} d={d} G={G} lens={lens} M={more}")
         cache, g = build(dev, 2, d, 64, 64, lens, 2, extra_blocks=more)
         check(cache, queries(dev, dtype, 4, 2 * G, d, g))
