@@ -117,7 +117,7 @@ __global__ __launch_bounds__(kAppendThreads) void k_append_kv(const SeqGeom g, c
 // 8-bit pages took 150 us, and a grid of every piece, which does not need that, 6 us more for a call
 // without a copy.
 constexpr int kCopyThreads = 256, kCopyUnroll = 4, kCopyPiece = kCopyThreads * kCopyUnroll;
-constexpr int kCopyMaxWgs = 1536;
+constexpr int kCopyMaxWgs = 1536, kCopyFewWgs = 2048;
 
 // A workgroup's piece: 16 KB of a page, from its chunk `at` on, and with a page's first piece of the
 // first pool its scales.
@@ -130,13 +130,14 @@ struct Piece {
   bool real;
 };
 
-__device__ __forceinline__ Piece piece_of(const CopyLaunch& a, int pieces, int pools, int64_t per_pair, int64_t w) {
-  const int64_t p = w / per_pair;
-  const int64_t rest = w - p * per_pair;
-  const int64_t lp = rest / pieces;
+template <typename I>
+__device__ __forceinline__ Piece piece_of(const CopyLaunch& a, int pieces, int pools, I per_pair, I w) {
+  const I p = w / per_pair;
+  const I rest = w - p * per_pair;
+  const I lp = rest / pieces;
   const int layer = static_cast<int>(lp / pools), pool = static_cast<int>(lp % pools);
   Piece x{};
-  x.at = (rest - lp * pieces) * kCopyPiece;
+  x.at = static_cast<int64_t>(rest - lp * pieces) * kCopyPiece;
   const int src = a.pairs[2 * p], dst = a.pairs[2 * p + 1];
   x.real = src >= 0 && src < a.num_pages && dst >= 0 && dst < a.num_pages;
   uint4* base = static_cast<uint4*>(pool == 0 ? a.k_pages : a.v_pages) + layer * a.layer_chunks;
@@ -160,11 +161,10 @@ __device__ __forceinline__ void load_piece(const CopyLaunch& a, const Piece& x, 
   }
 }
 
-// The next piece's loads are out before the present one is stored.
-template <bool PAST>
-__device__ __forceinline__ void copy_pieces(const CopyLaunch& a, int pieces, int pools, int64_t per_pair,
-                                            int64_t total) {
-  int64_t w = blockIdx.x;
+// The next piece's loads are out before the present one is stored.  ONE: a workgroup has one at most.
+template <bool PAST, bool ONE, typename I>
+__device__ __forceinline__ void copy_pieces(const CopyLaunch& a, int pieces, int pools, I per_pair, I total) {
+  I w = blockIdx.x;
   if (w >= total) return;
   Piece x = piece_of(a, pieces, pools, per_pair, w);
   uint4 data[kCopyUnroll] = {};
@@ -175,7 +175,7 @@ __device__ __forceinline__ void copy_pieces(const CopyLaunch& a, int pieces, int
     Piece next{};
     uint4 next_data[kCopyUnroll] = {};
     float2 next_scale{};
-    if (w < total) {
+    if (!ONE && w < total) {
       next = piece_of(a, pieces, pools, per_pair, w);
       load_piece(a, next, next_data, next_scale);
     }
@@ -190,7 +190,7 @@ __device__ __forceinline__ void copy_pieces(const CopyLaunch& a, int pieces, int
         for (int64_t h = threadIdx.x + kCopyThreads; h < a.page_scales; h += kCopyThreads) x.to_scales[h] = x.from_scales[h];
       }
     }
-    if (w >= total) return;
+    if (ONE || w >= total) return;
     x = next;
     scale = next_scale;
 #pragma unroll
@@ -203,9 +203,16 @@ __global__ __launch_bounds__(kCopyThreads) void k_copy_pages(const CopyLaunch a,
   const int pairs = a.count == nullptr ? a.max_pairs : min(max(*a.count, 0), a.max_pairs);
   const int64_t per_pair = static_cast<int64_t>(pieces) * pools * a.layers, total = per_pair * pairs;
   if (a.page_chunks * 16 * pools * a.layers * pairs > kPastBytes)
-    copy_pieces<true>(a, pieces, pools, per_pair, total);
+    copy_pieces<true, false>(a, pieces, pools, per_pair, total);
   else
-    copy_pieces<false>(a, pieces, pools, per_pair, total);
+    copy_pieces<false, false>(a, pieces, pools, per_pair, total);
+}
+
+__global__ __launch_bounds__(kCopyThreads) void k_copy_few(const CopyLaunch a, int pieces) {
+  const int pools = a.v_pages != nullptr ? 2 : 1;
+  const int pairs = a.count == nullptr ? a.max_pairs : min(max(*a.count, 0), a.max_pairs);
+  const int per_pair = pieces * pools * a.layers;
+  copy_pieces<false, true>(a, pieces, pools, per_pair, per_pair * pairs);
 }
 
 // ---------------------------------------------------------------- tables
@@ -650,9 +657,10 @@ hipError_t launch_append_kv(const SeqGeom& g, const AppendLaunch& a, hipStream_t
 hipError_t launch_copy_pages(const CopyLaunch& a, hipStream_t stream) {
   const int64_t pieces = (a.page_chunks + kCopyPiece - 1) / kCopyPiece;
   if (pieces > 0x7fffffff) return hipErrorInvalidConfiguration;
-  const double units = static_cast<double>(pieces) * 2 * a.layers * a.max_pairs;
-  const int wgs = units < kCopyMaxWgs ? static_cast<int>(units) : kCopyMaxWgs;
-  return launch_kernel(k_copy_pages, dim3(wgs), dim3(kCopyThreads), 0, stream, a, static_cast<int>(pieces));
+  const double units = static_cast<double>(pieces) * (a.v_pages != nullptr ? 2 : 1) * a.layers * a.max_pairs;
+  if (units <= kCopyFewWgs)
+    return launch_kernel(k_copy_few, dim3(static_cast<int>(units)), dim3(kCopyThreads), 0, stream, a, static_cast<int>(pieces));
+  return launch_kernel(k_copy_pages, dim3(kCopyMaxWgs), dim3(kCopyThreads), 0, stream, a, static_cast<int>(pieces));
 }
 
 hipError_t launch_seq_update(const SeqGeom& g, const SeqPlan& p, const SeqUpdateLaunch& a, void* workspace,
