@@ -85,12 +85,15 @@ constexpr int64_t kDecodeWgs = 256, kDecodeManyWgs = 512;
 // 60 tokens, 24 query heads, 17.2 -> 11.8 us (4 query heads 10.6 -> 8.2, one fp32 17.4 -> 13.8); 512
 // items 9.0 / 8.9 (5.9 / 6.8, 9.5 / 10.8), 64 items of 120 tokens 4.9 -> 9.0.
 constexpr int64_t kItemUnitsMost = 20, kWaveUnitsMost = 8, kWaveItems = 1024;
-// Two column tiles over 8-bit pages, from this many bytes of the table's capacity on both a wave's, which is
+// Two column tiles over 8-bit pages, from this many bytes of K and V on both a wave's, which is
 // then held up less by memory than by a key's and a value's widening, once for both; below, each every
-// other wave's.  24 query heads a key head, bf16, 4 sequences of 60 to 90 thousand tokens (620 MB) 116 us
-// against 143, 7 of 3 to 21 thousand (131 MB) 40.8 / 44.8; 40 of 1 to 3 thousand (145 MB) 49.0 / 52.0, fp32 65.6 /
-// 55.5; 49 of up to 1,752 (19 MB) 23.2 / 20.4, fp32 28.1 / 22.3.
-constexpr double kBothBytes = 256 << 20;
+// other wave's.  The bytes are what a call can read at most: of the blocks that a window leaves, half the threshold,
+// since sequences are mostly longer than it; else of the table's capacity, which they seldom fill.  24 query heads a key
+// head, bf16, pairs and both: 4 sequences of 60 to 90 thousand tokens, 8 key heads (704 MB of capacity) 141.6 / 114.6 us,
+// 16 of 3 to 20 thousand (628 MB) 81.8 / 68.2, 16 of an eighth to all of 256 MB 42.7 / 40.8, of 192 MB 33.2 / 38.0; windows over
+// tables of 1 GB and more, 16 sequences: 256 MB 78.4 / 62.7, 128 MB 46.5 / 42.2, 96 MB 36.7 / 37.5, 1,560 tokens (52 MB) 27.3 /
+// 31.0; heads of 64, 16 key heads, 4,000 tokens (128 MB) 47.5 / 43.5.
+constexpr double kBothBytes = 256 << 20, kBothWindowBytes = 128 << 20;
 constexpr int64_t kItemOverhead = 64;  // of an item's length on the line, no less than the kernel adds
 
 // What a plan goes by, of a kind of pages: tokens of a unit; units of the longest item that is a
@@ -138,8 +141,8 @@ omnimem_status_t plan_decode(int32_t num_heads, int32_t head_dim, const DecodeTu
   p.eight_waves = t.eight_bit && head_dim == 64 && p.tile_rows == kDecodeHeadRows && p.split == DecodeSplit::kItem &&
                   items <= kDecodeWgs / 2 && units > 4;
   p.pair = pair && p.tile_rows > kDecodeHeadRows;
-  const double bytes = 2. * g.N * g.M * num_heads * g.B * head_dim;
-  const bool both = p.pair && p.split == DecodeSplit::kLine && bytes >= kBothBytes;
+  const double bytes = 2. * g.N * blocks * num_heads * g.B * head_dim;
+  const bool both = p.pair && p.split == DecodeSplit::kLine && bytes >= (blocks < g.M ? kBothWindowBytes : kBothBytes);
   if (both) p.pair = false;
   const int64_t wgs = both && head_dim == 128 ? kDecodeWgs : items > kDecodeWgs ? t.many_wgs : t.wgs;
   if (most > wgs * 0x7fffffff) return OMNIMEM_EINVAL;  // a workgroup's share of the line in 31 bits
