@@ -92,17 +92,22 @@ constexpr int64_t kItemUnitsMost = 20, kWaveUnitsMost = 8, kWaveItems = 1024;
 // head, bf16, pairs and both: 4 sequences of 60 to 90 thousand tokens, 8 key heads (704 MB of capacity) 141.6 / 114.6 us,
 // 16 of 3 to 20 thousand (628 MB) 81.8 / 68.2, 16 of an eighth to all of 256 MB 42.7 / 40.8, of 192 MB 33.2 / 38.0; windows over
 // tables of 1 GB and more, 16 sequences: 256 MB 78.4 / 62.7, 128 MB 46.5 / 42.2, 96 MB 36.7 / 37.5, 1,560 tokens (52 MB) 27.3 /
-// 31.0; heads of 64, 16 key heads, 4,000 tokens (128 MB) 47.5 / 43.5.
-constexpr double kBothBytes = 256 << 20, kBothWindowBytes = 128 << 20;
+// 31.0; heads of 64, 16 key heads, 4,000 tokens (128 MB) 47.5 / 43.5.  fp32 queries of 128 dims hold three pieces of both
+// tiles, which leaves one workgroup a CU and less to gain: 16 sequences of an eighth to all of 512 MB 74.3 / 79.0, 4 of 60
+// to 90 thousand tokens (704 MB) 161.4 / 158.6; more items than CUs end more often, 40 sequences of 384 MB 61.8 / 77.0, of 768 MB
+// 100.5 / 118.2; windows, 16 sequences, 192 MB 67.3 / 71.2, 384 MB 113.4 / 112.8.  Of 64 dims they are as bf16: 512 MB 74.9 / 67.2,
+// windows of 128 MB 51.2 / 47.7.
+constexpr double kBothBytes = 256 << 20, kBothBytesF32 = 640 << 20, kBothBytesF32Many = 1024 << 20;
 constexpr int64_t kItemOverhead = 64;  // of an item's length on the line, no less than the kernel adds
 
 // What a plan goes by, of a kind of pages: tokens of a unit; units of the longest item that is a
 // workgroup's, and of one that a window bounds where there is an item for each CU; workgroups of a line
 // where there are no more items than CUs and where there are; whether these are 8-bit pages, whose
-// kernels have one column tile a wave and joins of their own.
+// kernels have forms and joins of their own; of those, kBothBytes for the queries' type, in both places.
 struct DecodeTuning {
   int64_t unit, item_units, window_units, wgs, many_wgs;
   bool eight_bit;
+  double both_bytes, many_both_bytes;
 };
 
 omnimem_status_t plan_decode(int32_t num_heads, int32_t head_dim, const DecodeTuning& t, const SeqGeom& g,
@@ -142,9 +147,11 @@ omnimem_status_t plan_decode(int32_t num_heads, int32_t head_dim, const DecodeTu
                   items <= kDecodeWgs / 2 && units > 4;
   p.pair = pair && p.tile_rows > kDecodeHeadRows;
   const double bytes = 2. * g.N * blocks * num_heads * g.B * head_dim;
-  const bool both = p.pair && p.split == DecodeSplit::kLine && bytes >= (blocks < g.M ? kBothWindowBytes : kBothBytes);
+  const double both_bytes = items > kDecodeWgs ? t.many_both_bytes : t.both_bytes;
+  const bool both = p.pair && p.split == DecodeSplit::kLine && bytes >= (blocks < g.M ? both_bytes / 2 : both_bytes);
   if (both) p.pair = false;
-  const int64_t wgs = both && head_dim == 128 ? kDecodeWgs : items > kDecodeWgs ? t.many_wgs : t.wgs;
+  const int64_t most_wgs = items > kDecodeWgs ? t.many_wgs : t.wgs;
+  const int64_t wgs = both && head_dim == 128 ? kDecodeWgs : most_wgs;
   if (most > wgs * 0x7fffffff) return OMNIMEM_EINVAL;  // a workgroup's share of the line in 31 bits
   p.wgs = static_cast<int>(p.split == DecodeSplit::kLine   ? (most < wgs ? most : wgs)
                            : p.split == DecodeSplit::kItem ? items
@@ -155,7 +162,8 @@ omnimem_status_t plan_decode(int32_t num_heads, int32_t head_dim, const DecodeTu
   p.slot_floats = static_cast<size_t>(p.rows) * (head_dim + 2);
   p.slot_floats = (p.slot_floats + 3) / 4 * 4;
   p.off_part = 0;
-  const size_t shares = p.split == DecodeSplit::kLine ? p.wgs : 0;
+  // of either form: the workspace's size is asked for without the queries' type
+  const size_t shares = p.split != DecodeSplit::kLine ? 0 : most < most_wgs ? most : most_wgs;
   p.off_starts = align256(shares * 2 * p.slot_floats * sizeof(float));
   p.total = shares == 0 ? 256 : p.off_starts + align256(shares * sizeof(DecodeStart)) + 512;
   return OMNIMEM_OK;
@@ -164,7 +172,7 @@ omnimem_status_t plan_decode(int32_t num_heads, int32_t head_dim, const DecodeTu
 omnimem_status_t plan_decode(const omnimem_seq_cache_t* sc, const SeqGeom& g, int32_t num_q_heads, int32_t window,
                              DecodePlan& p) {
   const DecodeTuning t{sc->dtype == OMNIMEM_BF16 && sc->head_dim == 64 ? 64 : 32, kItemUnitsMost, kItemUnitsMost, kDecodeWgs,
-                       kDecodeManyWgs, false};
+                       kDecodeManyWgs, false, 0, 0};
   return plan_decode(sc->num_heads, sc->head_dim, t, g, num_q_heads, window, p);
 }
 
@@ -179,10 +187,12 @@ omnimem_status_t plan_decode(const omnimem_seq_cache_t* sc, const SeqGeom& g, in
 // 10.3, bf16 10.1 -> 8.7, but 240 items 12.8 -> 13.0, 3 units 5.0 -> 5.3.
 // Windows make items of one length: 256 of 2,400 tokens, bf16 heads of 128, 36.2 -> 28.1, fp32 heads of
 // 64 28.3 -> 17.1, where 32 items lose (15.4 -> 20.1, 14.0 -> 15.0).
-omnimem_status_t plan_decode(const omnimem_seq_cache_quant_t* sc, const SeqGeom& g, int32_t num_q_heads, int32_t window,
-                             DecodePlan& p) {
-  const DecodeTuning t = sc->head_dim == 64 ? DecodeTuning{64, 28, 48, kDecodeManyWgs, kDecodeManyWgs, true}
-                                            : DecodeTuning{64, 20, 48, kDecodeWgs, kDecodeManyWgs, true};
+omnimem_status_t plan_decode(const omnimem_seq_cache_quant_t* sc, int32_t dtype, const SeqGeom& g, int32_t num_q_heads,
+                             int32_t window, DecodePlan& p) {
+  const bool f32 = dtype == OMNIMEM_F32 && sc->head_dim == 128;
+  const double both = f32 ? kBothBytesF32 : kBothBytes, many_both = f32 ? kBothBytesF32Many : kBothBytes;
+  const DecodeTuning t = sc->head_dim == 64 ? DecodeTuning{64, 28, 48, kDecodeManyWgs, kDecodeManyWgs, true, both, many_both}
+                                            : DecodeTuning{64, 20, 48, kDecodeWgs, kDecodeManyWgs, true, both, many_both};
   return plan_decode(sc->num_heads, sc->head_dim, t, g, num_q_heads, window, p);
 }
 
@@ -223,7 +233,7 @@ size_t decode_quant_workspace_bytes(const omnimem_seq_cache_quant_t* sc, int32_t
   SeqGeom g;
   DecodePlan p;
   if (window < 0 || resolve_quant_cache(sc, g, true) != OMNIMEM_OK ||
-      plan_decode(sc, g, num_q_heads, window, p) != OMNIMEM_OK)
+      plan_decode(sc, OMNIMEM_BF16, g, num_q_heads, window, p) != OMNIMEM_OK)
     return 0;
   return p.total;
 }
@@ -267,7 +277,7 @@ omnimem_status_t check_decode_attn_quant(const omnimem_seq_cache_quant_t* sc, in
                                          DecodeLaunch& a) {
   if (!known_dtype(dtype)) return OMNIMEM_EUNSUPPORTED;
   omnimem_status_t st = resolve_quant_cache(sc, g, false);
-  if (st == OMNIMEM_OK) st = plan_decode(sc, g, num_q_heads, window, p);
+  if (st == OMNIMEM_OK) st = plan_decode(sc, dtype, g, num_q_heads, window, p);
   if (st != OMNIMEM_OK) return st;
   a = DecodeLaunch{dtype, sc->num_heads, sc->head_dim, sc->k_pages, sc->v_pages, sc->scales,
                    q,     q_stride,      num_q_heads,  window,      scale,       out, lse};

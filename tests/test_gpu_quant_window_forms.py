@@ -1,5 +1,5 @@
-"""omnimem_decode_attn_quant for more than 16 query heads a key head under windows, over tables far longer than them: the
-form is chosen by what the window leaves."""
+"""omnimem_decode_attn_quant for more than 16 query heads a key head: its forms are chosen by what a window leaves of a table
+and by the queries' type."""
 import pytest
 import torch
 
@@ -20,3 +20,13 @@ def test_windows_over_long_tables(dev, dtype, d, G):  # noqa: F811
         say(f"decode windows {dtype} d={d} G={G} window={window}")
         check(cache, q, window)
     assert all(torch.equal(a, b) for a, b in zip(check(cache, q, 2 ** 31 - 1), check(cache, q)))
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("d", [64, 128])
+def test_more_items_than_cus(dev, dtype, d):  # noqa: F811
+    """264 items over 346 MB of capacity (heads of 128): both column tiles in a wave for bf16, pairs for fp32."""
+    lens = [13 * i for i in range(33)]
+    say(f"decode items {dtype} d={d}")
+    cache, g = build(dev, 8, d, 64, 64, lens, 14, extra_blocks=73)
+    check(cache, queries(dev, dtype, 33, 8 * 24, d, g))

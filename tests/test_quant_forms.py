@@ -52,6 +52,53 @@ def test_windows(shim, dtype, n, heads, hi, window, d, pairs, both):
     assert (split, rows) == (0, 32) and bool(pair) == (pairs < both)
 
 
+# the same without a window: type, sequences, key heads, bytes of capacity / 2^20, dims, us in pairs, us with both in a wave;
+# lengths from an eighth of the capacity to all of it, evenly spaced on a logarithmic scale, or (7 sequences) all of it
+TABLES = [
+    (F32, 16, 8, 256, 128, 46.6, 52.8),
+    (F32, 16, 8, 512, 128, 74.3, 79.0),
+    (F32, 40, 8, 256, 128, 49.6, 63.0),
+    (F32, 40, 8, 768, 128, 100.5, 118.2),
+    (F32, 7, 8, 256, 128, 79.8, 82.4),
+    (F32, 7, 8, 768, 128, 207.1, 203.5),
+    (F32, 16, 8, 512, 64, 74.9, 67.2),
+    (F32, 40, 8, 384, 64, 64.6, 61.2),
+    (F32, 16, 8, 64, 64, 23.7, 25.6),
+    (BF16, 16, 8, 384, 128, 55.0, 50.4),
+    (BF16, 16, 8, 192, 128, 33.2, 38.0),
+    (BF16, 40, 8, 512, 128, 71.5, 67.0),
+    (BF16, 40, 8, 192, 128, 37.1, 43.6),
+    (BF16, 16, 8, 384, 64, 51.2, 45.8),
+    (BF16, 40, 8, 128, 64, 30.0, 32.0),
+]
+
+
+@pytest.mark.parametrize("dtype,n,heads,mb,d,pairs,both", TABLES)
+def test_tables(shim, dtype, n, heads, mb, d, pairs, both):
+    split, rows, pair, *_ = form(shim, dtype, n, heads, mb * 2 ** 20 // (2 * n * heads * 64 * d) + 1, 0, d)
+    assert (split, rows) == (0, 32) and bool(pair) == (pairs < both)
+
+
+def test_the_workspace_serves_both_types(shim):
+    """Its size is asked for without a type, so every type's regions lie inside it."""
+    forms = set()
+    for heads in (1, 8, 9, 40, 300):
+        for n in (1, 16, 40):
+            for m in (30, 200, 400, 800, 3000, 20000):
+                for window in (0, 1560, 40000):
+                    for d in (64, 128):
+                        for G in (1, 17, 40):
+                            sizes = set()
+                            for dtype in (BF16, F32):
+                                split, _, pair, wgs, at, shares, starts, need = form(shim, dtype, n, heads, m, window, d, G)
+                                if split == 0:
+                                    assert at + shares <= starts and starts + 24 * wgs <= need   # a record has 24 bytes
+                                    forms.add((dtype, pair))
+                                sizes.add(need)
+                            assert len(sizes) == 1
+    assert len(forms) == 4
+
+
 def test_a_window_that_bounds_nothing_is_none(shim):
     for dtype in (BF16, F32):
         for d in (64, 128):
