@@ -23,7 +23,7 @@
 //   ROW, KEYS, UNIT     bytes of a key in its page, keys of a tile, tokens of a unit (KEYS divides it)
 //   RT, QS, VW          16-key row tiles, 16-byte words of a lane's part of a query, 16-dim tiles of O
 //   kScaled             pages have scales: codes count times them
-//   wgs(NT)             workgroups that a CU shall hold
+//   wgs(NT)             waves that a SIMD shall hold: workgroups a CU where one has four waves
 //   kTwoPolicies        pages that sequences share are looked for (a second loop)
 //   load_q, load_k, load_v, clear_v_below, scores, pv, key, dim
 #pragma once

@@ -47,7 +47,8 @@ struct TileQuant {
   static constexpr int P_PIECES = kF32 ? 3 : 2;
   static constexpr int wgs(int nt) { return nt == 2 && D == 128 ? 1 : 2; }
   // fp32 queries of 128 dims leave no registers for a second loop (56 spilled: 32 windows of 2,500
-  // tokens, 8 key heads, 147 us instead of 38)
+  // tokens, 8 key heads, 147 us instead of 38); the one that is left spills two or three over a line, 8 to 12 bytes of
+  // scratch memory a lane: four rollouts of 47 to 94 thousand tokens, 12 heads, 135 us, 129 with bf16 queries
   static constexpr bool kTwoPolicies = !(kF32 && D == 128);
   typedef uint32_t vraw __attribute__((ext_vector_type(VW / 4)));  // a lane's V dims of one key
   u32x4 k[KB][2][KC];

@@ -22,7 +22,7 @@ struct SeqGeom {
 
 // ---------------------------------------------------------------- decode
 // The (sequence, key/value head, tile of query heads) items of a call, each of them its
-// sequence's units of 32 tokens (64 for bf16 heads of 64) in turn, form one line, which `wgs`
+// sequence's units of 32 tokens (64 for bf16 heads of 64 and for 8-bit pages) in turn, form one line, which `wgs`
 // workgroups share evenly; or, where sequences are short, an item is a workgroup's, or a wave's.
 enum class DecodeSplit { kLine, kItem, kWave };
 constexpr int kDecodeWaves = 4;
