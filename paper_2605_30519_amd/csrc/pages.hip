@@ -116,7 +116,8 @@ __global__ __launch_bounds__(kAppendThreads) void k_append_kv(const SeqGeom g, c
 // scales 139 us.  The next piece's loads are out before the present one is stored: without,
 // 8-bit pages took 150 us, and a grid of every piece, which does not need that, 6 us more for a call
 // without a copy.  Where there is a workgroup for every piece there is no next one: 50 pages 8.2 -> 7.7 us, 16
-// of fp32 5.3 -> 5.1 (in a graph).
+// of fp32 5.3 -> 5.1 (in a graph); lists that are no longer than that anyway have a kernel of fewer registers and less
+// code, 16 pages 4.5 -> 4.4.
 constexpr int kCopyThreads = 256, kCopyUnroll = 4, kCopyPiece = kCopyThreads * kCopyUnroll;
 constexpr int kCopyMaxWgs = 1536;
 
@@ -209,6 +210,14 @@ __global__ __launch_bounds__(kCopyThreads) void k_copy_pages(const CopyLaunch a,
     copy_pieces<true, false>(a, pieces, pools, per_pair, total);
   else
     copy_pieces<false, false>(a, pieces, pools, per_pair, total);
+}
+
+// Lists of which every piece has a workgroup.
+__global__ __launch_bounds__(kCopyThreads) void k_copy_few(const CopyLaunch a, int pieces) {
+  const int pools = a.v_pages != nullptr ? 2 : 1;
+  const int pairs = a.count == nullptr ? a.max_pairs : min(max(*a.count, 0), a.max_pairs);
+  const int per_pair = pieces * pools * a.layers;
+  copy_pieces<false, true>(a, pieces, pools, per_pair, per_pair * pairs);
 }
 
 // ---------------------------------------------------------------- tables
@@ -655,7 +664,8 @@ hipError_t launch_copy_pages(const CopyLaunch& a, hipStream_t stream) {
   if (pieces > 0x7fffffff) return hipErrorInvalidConfiguration;
   const double units = static_cast<double>(pieces) * 2 * a.layers * a.max_pairs;
   const int wgs = units < kCopyMaxWgs ? static_cast<int>(units) : kCopyMaxWgs;
-  return launch_kernel(k_copy_pages, dim3(wgs), dim3(kCopyThreads), 0, stream, a, static_cast<int>(pieces));
+  return launch_kernel(units <= kCopyMaxWgs ? k_copy_few : k_copy_pages, dim3(wgs), dim3(kCopyThreads), 0, stream, a,
+                       static_cast<int>(pieces));
 }
 
 hipError_t launch_seq_update(const SeqGeom& g, const SeqPlan& p, const SeqUpdateLaunch& a, void* workspace,
