@@ -606,7 +606,8 @@ size_t omnimem_decode_quant_workspace_bytes(const omnimem_seq_cache_quant_t* sc,
  * omnimem_decode_attn over an 8-bit cache; q and out are of `dtype` (omnimem_dtype_t).  Scales need not
  * be powers of two.  Slots that hold none of the attended tokens, and scales of pages that hold none,
  * do not matter, NaN included.
- * Codes take part exactly.  bf16: P enters PV in two bf16 pieces, 2^-15 off; f32: Q and P in three, which
+ * Codes take part exactly; <q, c_k> is formed before it is multiplied by scale * s_k, and both have to be in
+ * fp32's range.  bf16: P enters PV in two bf16 pieces, 2^-15 off; f32: Q and P in three, which
  * hold all of their bits; sums are fp32.  V's scale is multiplied into P in front of that, so that what scales
  * below 2^-90 leave of P's last pieces may be below bf16's range and lost.
  */
